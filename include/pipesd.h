@@ -361,6 +361,86 @@ int pipesd_bo_posterior(const double *x, const double *y, int32_t n, double leng
 int pipesd_bo_suggest(const double *x, const double *y, int32_t n, double length_scale, double noise,
                       double xi, int32_t grid, double *next_out, double *ei_out);
 
+/* ---- A cache held in 4 bits --------------------------------------------------------------------
+ *
+ * For contexts, or numbers of clients, that a bf16 cache has no room or no time for: 4.25 bits a value instead of 16.
+ * Keys and values are held as e2m1 numbers (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) times a power of two that 32
+ * neighbouring channels of a token and head share: the smallest 2^e with max|x| <= 7 * 2^e, -125 <= e <= 125; a value is
+ * rounded to the nearest such number, ties to the even code (0, 1, 2, 4 before 0.5, 1.5, 3, 6), at most 6 * 2^e.  The format
+ * has finite values only: an infinity is stored as the largest float would be, NaN as 0.
+ *
+ * The operators work on a layer's keys, values and queries as a caller's own forward has them (keys already rotated if the
+ * model rotates them), of the config's dtype (PIPESD_F32 or PIPESD_BF16).  A forward over new rows of some clients is a
+ * PASS: pipesd_kv4_extend makes room for the rows, then, layer by layer, pipesd_kv4_append rounds that layer's keys and
+ * values into the cache and pipesd_kv4_attend lets its queries read it.  Rows of a pass lie one client after the other, in
+ * the order of pipesd_kv4_extend.  A pass ends when the next begins, or when one of its clients is cut.
+ *
+ * All device work of a handle has to be ordered by its caller: one stream, or events between streams.  Nothing in here
+ * waits for the device but creation, destruction and where stated; pointers to device memory need 16-byte alignment
+ * (4-byte for float and int32 arrays), strides are in elements and whole multiples of 16 bytes. */
+typedef struct pipesd_kv4 pipesd_kv4;
+enum { PIPESD_KV4_MAX_PASS_SEQS = 256, PIPESD_KV4_MAX_ROWS = 2048 };
+
+/* Bytes of a block of block_tokens (16) tokens: all layers and heads, keys and values.  0 for what pipesd_kv4_create refuses. */
+size_t pipesd_kv4_block_bytes(const pipesd_config *cfg, int32_t block_tokens);
+
+/* Cache of up to max_seqs clients over a caller-allocated device pool of floor(pool_bytes / block bytes) blocks (borrowed until
+ * pipesd_kv4_destroy).  Of the config it takes n_layers, n_q_heads, n_kv_heads, head_dim (64 or 128) and dtype.  Beside the
+ * pool it allocates the block tables and what passes of up to PIPESD_MAX_ROWS rows by 16 clients need.  pool == NULL: bookkeeping only.
+ * EINVAL: an unsupported config, block_tokens != 16, max_seqs < 1, no room for one block, a pool that is not 256-byte
+ * aligned or of 2^31 tokens or table entries (2 * max_seqs * blocks) and more; ENOMEM: an allocation failed. */
+int pipesd_kv4_create(const pipesd_config *cfg, int32_t max_seqs, int32_t block_tokens, void *pool, size_t pool_bytes,
+                      pipesd_kv4 **out);
+int pipesd_kv4_destroy(pipesd_kv4 *kv);
+
+/* Begin a pass: client seq_ids[i] (pairwise distinct, 1 <= n_seqs <= 256) gets n_new[i] >= 0 more tokens, at least one in all.
+ * A pass in which no client gets more than PIPESD_KV4_MAX_ROWS can attend; others only append.  Larger passes than
+ * pipesd_kv4_create provided for grow the handle's scratch, which waits for the device.
+ * ENOMEM: the pool has too few free blocks, or the scratch cannot grow. */
+int pipesd_kv4_extend(pipesd_kv4 *kv, int32_t n_seqs, const int32_t *seq_ids, const int32_t *n_new, void *stream);
+
+/* Round the pass's keys and values of one layer into the cache: k, v device [rows][n_kv_heads * head_dim], rows k_stride and
+ * v_stride elements apart.  ESTATE: no pass, or no pool. */
+int pipesd_kv4_append(pipesd_kv4 *kv, int32_t layer, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                      void *stream);
+
+/* Attention of the pass's queries over one layer of the cache: q, out device [rows][n_q_heads * head_dim], softmax of
+ * q . k / sqrt(head_dim), query head g reads head g / (n_q_heads / n_kv_heads) of the cache.
+ *   limits  device int32 [rows]: how many of its client's tokens (from the first) a row sees, cut to 0 .. its length; NULL:
+ *           all up to the row's own.  A row that sees nothing gets zeros.
+ *   mass    device fp32 [max_seqs][n_layers][n_kv_heads][mass_stride], or NULL: what weight the cached tokens were given.  For
+ *           each client of the pass, at this layer, mass[t] = decay * mass[t] + (sum of token t's weights over the client's rows
+ *           and the query heads of the cache head), 0 <= decay <= 1; the pass's own tokens, and all with decay 0, start at 0
+ *           whatever the buffer held.
+ * A row's result depends on its client and, in which order sums are formed, on the most rows that a client of the pass has.
+ * EINVAL: also a client longer than mass_stride, or a decay outside [0, 1]; ESTATE: no pass that can attend, no pool. */
+int pipesd_kv4_attend(pipesd_kv4 *kv, int32_t layer, const void *q, int64_t q_stride, const int32_t *limits, void *out,
+                      int64_t out_stride, float *mass, int64_t mass_stride, float decay, void *stream);
+
+/* The numbers that tokens first[i] .. first[i] + count[i] - 1 of client seq_ids[i] are held as, of layers layer0 .. layer0 +
+ * n_layers - 1: k_out, v_out device [n_layers][sum of count][n_kv_heads][head_dim], in the config's dtype (exact in either).
+ * ESTATE: a range beyond a client's length, no pool. */
+int pipesd_kv4_read(const pipesd_kv4 *kv, int32_t n_seqs, const int32_t *seq_ids, const int32_t *first, const int32_t *count,
+                    int32_t layer0, int32_t n_layers, void *k_out, void *v_out, void *stream);
+
+/* Cut clients to `keep` tokens: per layer and cache head the newest `recent` stay and, of the others, the keep - recent
+ * with the most weight in `mass` (as pipesd_kv4_attend accumulates it; the lower index first among equals, NaN counts as 0), in their
+ * order.  The result becomes client into[i], which loses what it held; into[i] == seq_ids[i] cuts in place, otherwise
+ * seq_ids[i] stays as it is.  The kept tokens go to fresh blocks: ceil(keep / 16) per client have to be free (a target's
+ * old blocks count, a client's own that is cut in place do not).  The kept weights go to the target's `mass`, and the kept
+ * indices to device int32 kept [n_seqs][n_layers][n_kv_heads][keep].
+ * EINVAL: also into[i] that is another client being cut, or a client longer than mass_stride; ESTATE: a client of fewer than
+ * `keep` tokens, no pool; ENOMEM: too few free blocks. */
+int pipesd_kv4_evict(pipesd_kv4 *kv, int32_t n_seqs, const int32_t *seq_ids, const int32_t *into, int32_t keep, int32_t recent,
+                     float *mass, int64_t mass_stride, int32_t *kept, void *stream);
+
+/* Forget the tokens of clients from new_len[i] (0 .. its length, else ESTATE) on: drafts that were rejected, or with 0 the client.
+ * Host bookkeeping only. */
+int pipesd_kv4_truncate(pipesd_kv4 *kv, int32_t n_seqs, const int32_t *seq_ids, const int32_t *new_len);
+int pipesd_kv4_len(const pipesd_kv4 *kv, int32_t seq, int32_t *len);
+int pipesd_kv4_free_blocks(const pipesd_kv4 *kv, int32_t *n_free);
+int pipesd_kv4_seq_blocks(const pipesd_kv4 *kv, int32_t seq, int32_t *n_blocks);
+
 const char *pipesd_strerror(int status);
 /* Text of the HIP call that made this thread's most recent call return PIPESD_EHIP ("" if none). */
 const char *pipesd_last_hip_error(void);

@@ -8,21 +8,16 @@
 #include <vector>
 
 #include "common.h"
+#include "status.h"
 
 using namespace pipesd;
 
 // text of the most recent failing HIP call of this thread, for pipesd_last_hip_error()
 static thread_local char g_hip_msg[256] = "";
-static int hip_fail(hipError_t e, const char* what) {
+int pipesd::hip_fail(hipError_t e, const char* what) {
   snprintf(g_hip_msg, sizeof(g_hip_msg), "%s: %s", what, hipGetErrorString(e));
   return PIPESD_EHIP;
 }
-
-#define HIP_TRY(expr)                                 \
-  do {                                                \
-    hipError_t _e = (expr);                           \
-    if (_e != hipSuccess) return hip_fail(_e, #expr); \
-  } while (0)
 
 extern "C" const char* pipesd_last_hip_error(void) { return g_hip_msg; }
 

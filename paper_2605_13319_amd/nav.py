@@ -85,6 +85,21 @@ _SIGS = {
                                       C.POINTER(C.c_double), C.c_int32, C.POINTER(C.c_double), C.POINTER(C.c_double)]),
     "pipesd_bo_suggest": (C.c_int, [C.POINTER(C.c_double), C.POINTER(C.c_double), C.c_int32, C.c_double, C.c_double,
                                     C.c_double, C.c_int32, C.POINTER(C.c_double), C.POINTER(C.c_double)]),
+    "pipesd_kv4_block_bytes": (C.c_size_t, [C.POINTER(Config), C.c_int32]),
+    "pipesd_kv4_create": (C.c_int, [C.POINTER(Config), C.c_int32, C.c_int32, C.c_void_p, C.c_size_t, C.POINTER(C.c_void_p)]),
+    "pipesd_kv4_destroy": (C.c_int, [C.c_void_p]),
+    "pipesd_kv4_extend": (C.c_int, [C.c_void_p, C.c_int32, _i32p, _i32p, C.c_void_p]),
+    "pipesd_kv4_append": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]),
+    "pipesd_kv4_attend": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64,
+                                    C.c_void_p, C.c_int64, C.c_float, C.c_void_p]),
+    "pipesd_kv4_read": (C.c_int, [C.c_void_p, C.c_int32, _i32p, _i32p, _i32p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
+                                  C.c_void_p]),
+    "pipesd_kv4_evict": (C.c_int, [C.c_void_p, C.c_int32, _i32p, _i32p, C.c_int32, C.c_int32, C.c_void_p, C.c_int64,
+                                   C.c_void_p, C.c_void_p]),
+    "pipesd_kv4_truncate": (C.c_int, [C.c_void_p, C.c_int32, _i32p, _i32p]),
+    "pipesd_kv4_len": (C.c_int, [C.c_void_p, C.c_int32, _i32p]),
+    "pipesd_kv4_free_blocks": (C.c_int, [C.c_void_p, _i32p]),
+    "pipesd_kv4_seq_blocks": (C.c_int, [C.c_void_p, C.c_int32, _i32p]),
     "pipesd_strerror": (C.c_char_p, [C.c_int]),
     "pipesd_last_hip_error": (C.c_char_p, []),
 }
@@ -490,6 +505,158 @@ class KVCache:
         _check(_lib.pipesd_kv_read(self.model.handle, self.handle, seq, layer, pos, _ptr(k, _f32p), _ptr(v, _f32p)),
                "pipesd_kv_read")
         return k, v
+
+
+class KV4Cache:
+    """Paged cache of keys and values in 4 bits (e2m1 numbers, a power of two per 32 channels) over a torch-allocated
+    device pool (or bookkeeping only), and the operators that write, read and cut it.  Tensors are of the shape's dtype
+    (float32 or bfloat16) and on the pool's device; rows of a pass lie one client after the other."""
+
+    def __init__(self, shape, max_seqs: int, n_blocks: int, block_tokens: int = 16, device: str = "cuda:0",
+                 on_device: bool = True):
+        self.shape, self.max_seqs = shape, max_seqs
+        self.handle = C.c_void_p()
+        cfg = config_of(shape)
+        bb = _lib.pipesd_kv4_block_bytes(C.byref(cfg), block_tokens)
+        if bb == 0:
+            raise PipesdError(EINVAL, "pipesd_kv4_block_bytes")
+        self.block_bytes = bb
+        self.dtype = torch.float32 if shape.dtype == 0 else torch.bfloat16
+        self.pool = None
+        pool_ptr = None
+        if on_device:
+            torch.cuda.set_device(device)
+            self.pool = torch.empty(n_blocks * bb, dtype=torch.uint8, device=device)
+            self.device = self.pool.device
+            pool_ptr = self.pool.data_ptr()
+        _check(_lib.pipesd_kv4_create(C.byref(cfg), max_seqs, block_tokens, pool_ptr, n_blocks * bb, C.byref(self.handle)),
+               "pipesd_kv4_create")
+        self._rows = 0
+
+    def close(self) -> None:
+        if self.handle:
+            _lib.pipesd_kv4_destroy(self.handle)
+            self.handle = C.c_void_p()
+            self.pool = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _tensor(self, t, heads: int, name: str):
+        """(address, elements between rows) of a tensor [rows][heads][head_dim] or [rows][heads * head_dim], the heads of a
+        row side by side."""
+        hd = self.shape.head_dim
+        if t.dtype is not self.dtype or not t.is_cuda or t.device != self.device:
+            raise TypeError(f"{name}: a {self.dtype} tensor on {self.device}, not {t.dtype} on {t.device}")
+        size, stride = t.shape, t.stride()
+        if len(size) == 3:
+            if size[1] != heads or size[2] != hd or stride[2] != 1 or (stride[1] != hd and heads > 1):
+                raise ValueError(f"{name}: rows of {heads} heads of {hd} side by side, not {tuple(size)} with strides {stride}")
+        elif len(size) != 2 or size[1] != heads * hd or stride[1] != 1:
+            raise ValueError(f"{name}: rows of {heads} heads of {hd}, not {tuple(size)} with strides {stride}")
+        if size[0] != self._rows:
+            raise ValueError(f"{name}: {size[0]} rows, the pass has {self._rows}")
+        return t.data_ptr(), (stride[0] if size[0] > 1 else heads * hd)
+
+    def extend(self, seqs: Sequence[int], n_new: Sequence[int]) -> None:
+        """Begin a pass: n_new[i] more tokens for client seqs[i]."""
+        (s, n), (c, m) = _ints(seqs), _ints(n_new)
+        if n != m:
+            raise ValueError(f"{n} clients, {m} numbers of tokens")
+        _check(_lib.pipesd_kv4_extend(self.handle, n, s, c, _stream() if self.pool is not None else None), "pipesd_kv4_extend")
+        self._rows = int(sum(n_new))
+
+    def append(self, layer: int, k, v) -> None:
+        """Round the pass's keys and values of a layer into the cache."""
+        heads = self.shape.n_kv_heads
+        kp, ks = self._tensor(k, heads, "k")
+        vp, vs = self._tensor(v, heads, "v")
+        _check(_lib.pipesd_kv4_append(self.handle, layer, kp, ks, vp, vs, _stream()), "pipesd_kv4_append")
+
+    def attend(self, layer: int, q, out=None, limits=None, mass=None, decay: float = 1.0):
+        """Attention of the pass's queries over a layer of the cache; returns `out` (a new tensor like q if None).
+        limits: int32 [rows], tokens that each row sees.  mass: float32 [max_seqs][n_layers][n_kv_heads][tokens], the weight
+        that cached tokens were given, accumulated."""
+        heads = self.shape.n_q_heads
+        qp, qs = self._tensor(q, heads, "q")
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        op, os_ = self._tensor(out, heads, "out")
+        lp = mp = None
+        tokens = 0
+        if limits is not None:
+            if limits.dtype is not torch.int32 or limits.device != self.device or limits.shape != (self._rows,) or not limits.is_contiguous():
+                raise ValueError(f"limits: a contiguous int32 tensor of {self._rows} on {self.device}")
+            lp = limits.data_ptr()
+        if mass is not None:
+            mp, tokens = self._mass(mass)
+        _check(_lib.pipesd_kv4_attend(self.handle, layer, qp, qs, lp, op, os_, mp, tokens, decay, _stream()), "pipesd_kv4_attend")
+        return out
+
+    def _mass(self, mass):
+        s = self.shape
+        if (mass.dtype is not torch.float32 or mass.device != self.device or mass.dim() != 4 or not mass.is_contiguous()
+                or mass.shape[:3] != (self.max_seqs, s.n_layers, s.n_kv_heads)):
+            raise ValueError(f"mass: a contiguous float32 tensor [{self.max_seqs}][{s.n_layers}][{s.n_kv_heads}][tokens] on {self.device}")
+        return mass.data_ptr(), mass.shape[3]
+
+    def read(self, seqs: Sequence[int], first: Sequence[int], count: Sequence[int], layer0: int = 0, n_layers: Optional[int] = None):
+        """(keys, values) [n_layers][sum of count][n_kv_heads][head_dim] that ranges of the clients' tokens are held as."""
+        s = self.shape
+        n_layers = s.n_layers - layer0 if n_layers is None else n_layers
+        (ids, n), (f, nf), (c, nc) = _ints(seqs), _ints(first), _ints(count)
+        if n != nf or n != nc:
+            raise ValueError(f"{n} clients, {nf} and {nc} ends of ranges")
+        size = (max(n_layers, 0), max(int(sum(count)), 0), s.n_kv_heads, s.head_dim)
+        k = torch.empty(size, dtype=self.dtype, device=self.device)
+        v = torch.empty(size, dtype=self.dtype, device=self.device)
+        # (a tensor of no elements has no address)
+        _check(_lib.pipesd_kv4_read(self.handle, n, ids, f, c, layer0, n_layers, k.data_ptr() or self.pool.data_ptr(),
+                                    v.data_ptr() or self.pool.data_ptr(), _stream()), "pipesd_kv4_read")
+        return k, v
+
+    def evict(self, seqs: Sequence[int], into: Sequence[int], keep: int, recent: int, mass, kept=None):
+        """Cut clients to `keep` tokens, the newest `recent` and the heaviest others per layer and head, into clients `into`.
+        Returns the kept indices, int32 [clients][n_layers][n_kv_heads][keep]."""
+        s = self.shape
+        (ids, n), (to, m) = _ints(seqs), _ints(into)
+        if n != m:
+            raise ValueError(f"{n} clients into {m}")
+        mp, tokens = self._mass(mass)
+        size = (n, s.n_layers, s.n_kv_heads, keep)
+        if kept is None:
+            if keep < 1:
+                raise PipesdError(EINVAL, "pipesd_kv4_evict")
+            kept = torch.empty(size, dtype=torch.int32, device=self.device)
+        elif kept.dtype is not torch.int32 or kept.device != self.device or kept.shape != size or not kept.is_contiguous():
+            raise ValueError(f"kept: a contiguous int32 tensor {size} on {self.device}")
+        _check(_lib.pipesd_kv4_evict(self.handle, n, ids, to, keep, recent, mp, tokens, kept.data_ptr(), _stream()), "pipesd_kv4_evict")
+        return kept
+
+    def truncate(self, seqs: Sequence[int], lengths: Sequence[int]) -> None:
+        """Forget the clients' tokens from lengths[i] on."""
+        (s, n), (c, m) = _ints(seqs), _ints(lengths)
+        if n != m:
+            raise ValueError(f"{n} clients, {m} lengths")
+        _check(_lib.pipesd_kv4_truncate(self.handle, n, s, c), "pipesd_kv4_truncate")
+
+    def length(self, seq: int) -> int:
+        n = C.c_int32()
+        _check(_lib.pipesd_kv4_len(self.handle, seq, C.byref(n)), "pipesd_kv4_len")
+        return n.value
+
+    def free_blocks(self) -> int:
+        n = C.c_int32()
+        _check(_lib.pipesd_kv4_free_blocks(self.handle, C.byref(n)), "pipesd_kv4_free_blocks")
+        return n.value
+
+    def seq_blocks(self, seq: int) -> int:
+        n = C.c_int32()
+        _check(_lib.pipesd_kv4_seq_blocks(self.handle, seq, C.byref(n)), "pipesd_kv4_seq_blocks")
+        return n.value
 
 
 def spec_accept(p, q, drafts: Sequence[int], uniforms) -> tuple:
