@@ -13,7 +13,7 @@ struct Kv4Seq {
   int32_t len = 0;
   std::vector<int32_t> blocks;  // in token order
   int32_t which = 0;            // of the client's two block tables
-  int32_t synced = 0;           // entries of it that the device has
+  std::vector<int32_t> sent[2]; // what the device has in them
   bool in_pass = false;         // of the pass that store and attend work on
 };
 template <class F>
@@ -37,10 +37,6 @@ struct pipesd_kv4 {
   int n_cu = 256;
   // device memory of the library
   int32_t* table = nullptr;  // [2 max_seqs][n_blocks]
-  Kv4Row* rows = nullptr;    // of the pass
-  size_t rows_cap = 0;
-  Kv4Item* items = nullptr;
-  size_t items_cap = 0;
   float* part = nullptr;
   size_t part_cap = 0;  // floats
   unsigned* counters = nullptr;
@@ -49,7 +45,7 @@ struct pipesd_kv4 {
   size_t lse_cap = 0;
   // the pass
   std::vector<Kv4Client> pass;
-  int32_t pass_rows = 0, n_few = 0, n_many = 0, few_tiles = 1, many_tiles = 1;
+  std::vector<Kv4Launch> launches;
   bool pass_open = false, attends = false;
 
   int32_t table_off(int32_t seq) const { return (2 * seq + seqs[seq].which) * n_blocks; }
@@ -73,7 +69,6 @@ static void kv4_release(pipesd_kv4* kv, Kv4Seq& s, int32_t tokens) {
     kv->free_list.push_back(s.blocks.back());  // (has room for every block)
     s.blocks.pop_back();
   }
-  s.synced = std::min(s.synced, keep);
   s.len = tokens;
 }
 static void kv4_close_pass(pipesd_kv4* kv) {
@@ -94,7 +89,7 @@ extern "C" size_t pipesd_kv4_block_bytes(const pipesd_config* cfg, int32_t block
 
 // grows a buffer of the pass; the device may still be using the old one
 template <class T>
-static int kv4_grow(T** p, size_t* cap, size_t want, bool zero, hipStream_t st) {
+static int kv4_grow(T** p, size_t* cap, size_t want, bool zero) {
   if (want <= *cap) return PIPESD_OK;
   want += want / 2;
   T* fresh = nullptr;
@@ -111,7 +106,6 @@ static int kv4_grow(T** p, size_t* cap, size_t want, bool zero, hipStream_t st) 
   if (*p) (void)hipFree(*p);
   *p = fresh;
   *cap = want;
-  (void)st;
   return PIPESD_OK;
 }
 
@@ -119,7 +113,7 @@ extern "C" int pipesd_kv4_destroy(pipesd_kv4* kv) {
   if (!kv) return PIPESD_EINVAL;
   if (kv->pool) {
     (void)hipDeviceSynchronize();
-    for (void* p : {(void*)kv->table, (void*)kv->rows, (void*)kv->items, (void*)kv->part, (void*)kv->counters, (void*)kv->lse})
+    for (void* p : {(void*)kv->table, (void*)kv->part, (void*)kv->counters, (void*)kv->lse})
       if (p) (void)hipFree(p);
   }
   delete kv;
@@ -155,24 +149,21 @@ extern "C" int pipesd_kv4_create(const pipesd_config* cfg, int32_t max_seqs, int
       return PIPESD_ENOMEM;
     }
     HIP_TRY(hipMemset(kv->table, 0, entries * 4));
-    // what passes of up to PIPESD_MAX_ROWS rows a client take
-    Kv4Client c{};
-    size_t items = 0, tiles = 0, counts = 0;
-    for (int32_t m = 1; m <= kMaxRows; ++m) {
-      c.n_rows = m;
-      c.len = (int32_t)std::min<size_t>(n * kBlockTokens, (size_t)1 << 24);
-      kv4_plan_client(c, cfg->dtype, cfg->n_q_heads, cfg->n_kv_heads, kv->n_cu);
-      items = std::max(items, (size_t)c.nsplit * c.groups);
-      tiles = std::max(tiles, (size_t)cfg->n_kv_heads * c.groups * c.nsplit * c.tiles);
-      counts = std::max(counts, (size_t)cfg->n_kv_heads * c.groups);
-    }
-    const size_t many = (size_t)std::min(max_seqs, (int32_t)PIPESD_KV4_MAX_PASS_SEQS);
+    // what passes of up to PIPESD_MAX_ROWS rows by 16 clients take: a client alone has the most splits
+    size_t tiles = 0, counts = 0;
+    const int32_t clients = std::min(max_seqs, 16);
+    std::vector<Kv4Launch> scratch;
+    for (int32_t n : {1, clients})
+      for (int32_t m = 1; m <= kMaxRows; ++m) {
+        std::vector<Kv4Client> c(n, Kv4Client{0, m, 0, (int32_t)std::min<size_t>((size_t)kv->n_blocks * kBlockTokens, (size_t)1 << 24)});
+        const Kv4PlanNeeds need = kv4_plan(c.data(), n, cfg->dtype, cfg->n_q_heads, cfg->n_kv_heads, kv->n_cu, scratch);
+        tiles = std::max(tiles, need.part_tiles);
+        counts = std::max(counts, need.counters);
+      }
     int e;
-    if ((e = kv4_grow(&kv->rows, &kv->rows_cap, many * kMaxRows, false, nullptr))) return e;
-    if ((e = kv4_grow(&kv->items, &kv->items_cap, many * items, false, nullptr))) return e;
-    if ((e = kv4_grow(&kv->part, &kv->part_cap, std::min(many, (size_t)16) * tiles * 16 * (cfg->head_dim + kKv4PartPad), false, nullptr))) return e;
-    if ((e = kv4_grow(&kv->counters, &kv->counters_cap, many * counts, true, nullptr))) return e;
-    return kv4_grow(&kv->lse, &kv->lse_cap, many * kMaxRows * cfg->n_q_heads, false, nullptr);
+    if ((e = kv4_grow(&kv->part, &kv->part_cap, tiles * 16 * (cfg->head_dim + kKv4PartPad), false))) return e;
+    if ((e = kv4_grow(&kv->counters, &kv->counters_cap, counts, true))) return e;
+    return kv4_grow(&kv->lse, &kv->lse_cap, (size_t)clients * kMaxRows * cfg->n_q_heads, false);
   });
   if (rc) {
     pipesd_kv4_destroy(kv);
@@ -215,34 +206,30 @@ extern "C" int pipesd_kv4_truncate(pipesd_kv4* kv, int32_t n_seqs, const int32_t
   });
 }
 
-// sends what is new of the block tables and (if `clients`) the pass, some per launch
-static int kv4_send(pipesd_kv4* kv, const std::vector<int32_t>& seq_ids, const Kv4Client* clients, int32_t n_clients, hipStream_t st) {
-  Kv4PassUpdate u;
-  u.n_clients = u.n_entries = 0;
+// sends what is new of the block tables, some per launch.  (A block that a client gave back and got again is there already.)
+static int kv4_send(pipesd_kv4* kv, int32_t n, const int32_t* seq_ids, const int32_t* from, hipStream_t st) {
+  Kv4TableUpdate u;
+  u.n = 0;
   auto flush = [&]() -> int {
-    if (u.n_clients + u.n_entries == 0) return PIPESD_OK;
-    HIP_TRY(launch_kv4_begin(u, kv->table, kv->rows, kv->items, st));
-    u.n_clients = u.n_entries = 0;
+    if (u.n) HIP_TRY(launch_kv4_table(u, kv->table, st));
+    u.n = 0;
     return PIPESD_OK;
   };
-  for (int32_t seq : seq_ids) {
-    Kv4Seq& s = kv->seqs[seq];
-    const int32_t off = kv->table_off(seq);
-    for (int32_t i = s.synced; i < (int32_t)s.blocks.size(); ++i) {
-      if (u.n_entries == kKv4EntriesPerLaunch)
+  for (int32_t k = 0; k < n; ++k) {
+    Kv4Seq& s = kv->seqs[seq_ids[k]];
+    const int32_t off = kv->table_off(seq_ids[k]);
+    std::vector<int32_t>& sent = s.sent[s.which];
+    const int32_t nb = (int32_t)s.blocks.size();
+    if ((int32_t)sent.size() < nb) sent.resize(nb, -1);
+    for (int32_t i = from ? from[k] : 0; i < nb; ++i) {
+      if (sent[i] == s.blocks[i]) continue;
+      if (u.n == kKv4EntriesPerLaunch)
         if (int rc = flush()) return rc;
-      u.at[u.n_entries] = off + i;
-      u.v[u.n_entries++] = s.blocks[i];
+      u.at[u.n] = off + i;
+      u.v[u.n++] = sent[i] = s.blocks[i];
     }
   }
-  for (int32_t i = 0; i < n_clients; ++i) {
-    if (u.n_clients == kKv4ClientsPerLaunch)
-      if (int rc = flush()) return rc;
-    u.client[u.n_clients++] = clients[i];
-  }
-  if (int rc = flush()) return rc;
-  for (int32_t seq : seq_ids) kv->seqs[seq].synced = (int32_t)kv->seqs[seq].blocks.size();
-  return PIPESD_OK;
+  return flush();
 }
 
 extern "C" int pipesd_kv4_extend(pipesd_kv4* kv, int32_t n_seqs, const int32_t* seq_ids, const int32_t* n_new, void* stream) {
@@ -263,57 +250,31 @@ extern "C" int pipesd_kv4_extend(pipesd_kv4* kv, int32_t n_seqs, const int32_t* 
     if (total < 1 || total > INT32_MAX) return PIPESD_EINVAL;
     if (blocks > (int64_t)kv->free_list.size()) return PIPESD_ENOMEM;
 
-    // the plan: first the clients of few tiles, then those of many
     std::vector<Kv4Client> plan;
-    std::vector<int32_t> ids(seq_ids, seq_ids + n_seqs);
+    std::vector<Kv4Launch> launches;
+    std::vector<int32_t> had(n_seqs);
     plan.reserve(n_seqs);
     int32_t row = 0;
-    int few_tiles = 1, many_tiles = 1;
     for (int32_t i = 0; i < n_seqs; ++i) {
-      Kv4Client c{};
-      c.seq = seq_ids[i];
-      c.n_rows = n_new[i];
-      c.row_off = row;
-      c.len = kv->seqs[c.seq].len + n_new[i];
-      c.table_off = kv->table_off(c.seq);
+      had[i] = (int32_t)kv->seqs[seq_ids[i]].blocks.size();
+      if (n_new[i]) plan.push_back(Kv4Client{seq_ids[i], n_new[i], row, kv->seqs[seq_ids[i]].len + n_new[i]});
       row += n_new[i];
-      if (n_new[i] == 0) continue;
-      plan.push_back(c);
     }
-    size_t items = 0, counts = 0, tiles = 0;
-    int32_t n_few = 0, n_many = 0;
-    if (attends) {
-      for (Kv4Client& c : plan) {
-        kv4_plan_client(c, cfg.dtype, cfg.n_q_heads, cfg.n_kv_heads, kv->n_cu);
-        if (c.wide) many_tiles = c.tiles;
-        else few_tiles = std::max(few_tiles, c.tiles);
-      }
-      for (int wide = 0; wide < 2; ++wide)
-        for (Kv4Client& c : plan) {
-          if (c.wide != wide) continue;
-          if (!wide && c.tiles != few_tiles) {  // one kernel for all: the largest client's tiles a workgroup
-            c.tiles = few_tiles;
-            c.groups = std::max(1, (attn_query_tiles(cfg.n_q_heads / cfg.n_kv_heads, c.n_rows) + few_tiles - 1) / few_tiles);
-          }
-          c.item_off = (int32_t)items;
-          c.count_off = (int32_t)counts;
-          c.part_off = (int32_t)tiles;
-          (wide ? n_many : n_few) += c.nsplit * c.groups;
-          items += (size_t)c.nsplit * c.groups;
-          counts += (size_t)cfg.n_kv_heads * c.groups;
-          if (c.nsplit > 1) tiles += (size_t)cfg.n_kv_heads * c.groups * c.nsplit * c.tiles;
-          if (tiles > (size_t)INT32_MAX || items > (size_t)INT32_MAX) return PIPESD_ENOMEM;
-        }
-    }
-    if (kv->pool) {
+    if (kv->pool && attends) {
+      const Kv4PlanNeeds need = kv4_plan(plan.data(), (int)plan.size(), cfg.dtype, cfg.n_q_heads, cfg.n_kv_heads, kv->n_cu, launches);
+      if (need.part_tiles > (size_t)INT32_MAX || need.counters > (size_t)INT32_MAX) return PIPESD_ENOMEM;
+      for (Kv4Launch& l : launches)
+        for (int32_t j = 0; j < l.c.n; ++j) l.c.table_off[j] = kv->table_off(l.c.seq[j]);
       int e;
-      if ((e = kv4_grow(&kv->rows, &kv->rows_cap, (size_t)total, false, st))) return e;
-      if ((e = kv4_grow(&kv->items, &kv->items_cap, items, false, st))) return e;
-      if ((e = kv4_grow(&kv->part, &kv->part_cap, tiles * 16 * (cfg.head_dim + kKv4PartPad), false, st))) return e;
-      if ((e = kv4_grow(&kv->counters, &kv->counters_cap, counts, true, st))) return e;
-      if (attends && (e = kv4_grow(&kv->lse, &kv->lse_cap, (size_t)total * cfg.n_q_heads, false, st))) return e;
+      if ((e = kv4_grow(&kv->part, &kv->part_cap, need.part_tiles * 16 * (cfg.head_dim + kKv4PartPad), false))) return e;
+      if ((e = kv4_grow(&kv->counters, &kv->counters_cap, need.counters, true))) return e;
+      if ((e = kv4_grow(&kv->lse, &kv->lse_cap, (size_t)total * cfg.n_q_heads, false))) return e;
     }
-    for (int32_t i = 0; i < n_seqs; ++i) kv->seqs[seq_ids[i]].blocks.reserve(kv4_blocks(kv->seqs[seq_ids[i]].len + n_new[i]));
+    for (int32_t i = 0; i < n_seqs; ++i) {
+      Kv4Seq& s = kv->seqs[seq_ids[i]];
+      s.blocks.reserve(kv4_blocks(s.len + n_new[i]));
+      s.sent[s.which].reserve(kv4_blocks(s.len + n_new[i]));
+    }
 
     // from here on only the launches can fail: what they have not done is taken back
     for (int32_t i = 0; i < n_seqs; ++i) {
@@ -325,12 +286,11 @@ extern "C" int pipesd_kv4_extend(pipesd_kv4* kv, int32_t n_seqs, const int32_t* 
       }
     }
     kv4_close_pass(kv);
-    if (!attends)  // (rows to store, nothing to attend: no workgroups)
-      for (Kv4Client& c : plan) c.nsplit = c.groups = 0;
     if (kv->pool) {
-      if (int rc = kv4_send(kv, ids, plan.data(), (int32_t)plan.size(), st)) {
+      if (int rc = kv4_send(kv, n_seqs, seq_ids, had.data(), st)) {
         for (int32_t i = 0; i < n_seqs; ++i) {
           Kv4Seq& s = kv->seqs[seq_ids[i]];
+          std::fill(s.sent[s.which].begin() + had[i], s.sent[s.which].end(), -1);
           kv4_release(kv, s, s.len - n_new[i]);
         }
         return rc;
@@ -338,11 +298,7 @@ extern "C" int pipesd_kv4_extend(pipesd_kv4* kv, int32_t n_seqs, const int32_t* 
     }
     for (int32_t i = 0; i < n_seqs; ++i) kv->seqs[seq_ids[i]].in_pass = true;
     kv->pass.swap(plan);
-    kv->pass_rows = (int32_t)total;
-    kv->n_few = n_few;
-    kv->n_many = n_many;
-    kv->few_tiles = few_tiles;
-    kv->many_tiles = many_tiles;
+    kv->launches.swap(launches);
     kv->attends = attends;
     kv->pass_open = true;
     return PIPESD_OK;
@@ -354,13 +310,29 @@ static bool kv4_rows_ok(const pipesd_config& c, const void* p, int64_t stride, i
   return p && ((uintptr_t)p & 15) == 0 && stride >= (int64_t)heads * c.head_dim && (stride * e) % 16 == 0;
 }
 
+static void kv4_add_range(Kv4Ranges& r, int32_t table_off, int32_t first, int32_t count, int32_t row_off) {
+  r.table_off[r.n] = table_off;
+  r.first[r.n] = first;
+  r.count[r.n] = count;
+  r.row_off[r.n++] = row_off;
+  r.most = std::max(r.most, count);
+}
+
 extern "C" int pipesd_kv4_append(pipesd_kv4* kv, int32_t layer, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                                  void* stream) {
   if (!kv || layer < 0 || layer >= kv->cfg.n_layers) return PIPESD_EINVAL;
   if (!kv4_rows_ok(kv->cfg, k, k_stride, kv->cfg.n_kv_heads) || !kv4_rows_ok(kv->cfg, v, v_stride, kv->cfg.n_kv_heads)) return PIPESD_EINVAL;
   if (!kv->pool || !kv->pass_open) return PIPESD_ESTATE;
-  HIP_TRY(launch_kv4_store(kv->cfg.dtype, kv->cfg.head_dim, kv->view(), layer, kv->pass_rows, kv->rows, k, v, k_stride, v_stride,
-                           (hipStream_t)stream));
+  Kv4Ranges r;
+  r.n = r.most = 0;
+  for (size_t i = 0; i < kv->pass.size(); ++i) {
+    const Kv4Client& c = kv->pass[i];
+    kv4_add_range(r, kv->table_off(c.seq), c.len - c.n_rows, c.n_rows, c.row_off);
+    if (r.n == kKv4ClientsPerLaunch || i + 1 == kv->pass.size()) {
+      HIP_TRY(launch_kv4_store(kv->cfg.dtype, kv->cfg.head_dim, kv->view(), layer, r, k, v, k_stride, v_stride, (hipStream_t)stream));
+      r.n = r.most = 0;
+    }
+  }
   return PIPESD_OK;
 }
 
@@ -387,42 +359,15 @@ extern "C" int pipesd_kv4_attend(pipesd_kv4* kv, int32_t layer, const void* q, i
   a.q_stride = q_stride;
   a.out_stride = out_stride;
   a.limits = limits;
-  a.items = kv->items;
   a.part = kv->part;
   a.counters = kv->counters;
   a.lse = mass ? kv->lse : nullptr;
   a.mass = mass;
   a.mass_stride = mass_stride;
   a.decay = decay;
-  if (kv->n_few) {
-    a.item0 = 0;
-    a.n_items = kv->n_few;
-    a.wide = 0;
-    a.tiles = kv->few_tiles;
-    HIP_TRY(launch_kv4_attend(a, st));
-  }
-  if (kv->n_many) {
-    a.item0 = kv->n_few;
-    a.n_items = kv->n_many;
-    a.wide = 1;
-    a.tiles = kv->many_tiles;
-    HIP_TRY(launch_kv4_attend(a, st));
-  }
-  if (!mass) return PIPESD_OK;
-  Kv4MassClients cl;
-  cl.n = cl.most = 0;
-  for (size_t i = 0; i < kv->pass.size(); ++i) {
-    const Kv4Client& c = kv->pass[i];
-    cl.seq[cl.n] = c.seq;
-    cl.table_off[cl.n] = c.table_off;
-    cl.n_rows[cl.n] = c.n_rows;
-    cl.row_off[cl.n] = c.row_off;
-    cl.len[cl.n++] = c.len;
-    cl.most = std::max(cl.most, c.len);
-    if (cl.n == kKv4SeqsPerLaunch || i + 1 == kv->pass.size()) {
-      HIP_TRY(launch_kv4_mass(a, cl, st));
-      cl.n = cl.most = 0;
-    }
+  for (const Kv4Launch& l : kv->launches) {
+    HIP_TRY(launch_kv4_attend(a, l, st));
+    if (mass) HIP_TRY(launch_kv4_mass(a, l.c, st));
   }
   return PIPESD_OK;
 }
@@ -446,14 +391,10 @@ extern "C" int pipesd_kv4_read(const pipesd_kv4* kv, int32_t n_seqs, const int32
   int32_t row = 0;
   for (int32_t i = 0; i < n_seqs; ++i) {
     if (count[i] > 0) {
-      r.table_off[r.n] = kv->table_off(seq_ids[i]);
-      r.first[r.n] = first[i];
-      r.count[r.n] = count[i];
-      r.row_off[r.n++] = row;
-      r.most = std::max(r.most, count[i]);
+      kv4_add_range(r, kv->table_off(seq_ids[i]), first[i], count[i], row);
       row += count[i];
     }
-    if (r.n == kKv4SeqsPerLaunch || (i + 1 == n_seqs && r.n > 0)) {
+    if (r.n == kKv4ClientsPerLaunch || (i + 1 == n_seqs && r.n > 0)) {
       HIP_TRY(launch_kv4_read(c.dtype, c.head_dim, kv->view(), layer0, n_layers, r, total, k_out, v_out, (hipStream_t)stream));
       r.n = r.most = 0;
     }
@@ -485,8 +426,9 @@ extern "C" int pipesd_kv4_evict(pipesd_kv4* kv, int32_t n_seqs, const int32_t* s
     if ((int64_t)nb * n_seqs > have) return PIPESD_ENOMEM;
 
     std::vector<std::vector<int32_t>> fresh(n_seqs);
-    std::vector<int32_t> ids(into, into + n_seqs);
     for (auto& f : fresh) f.reserve(nb);
+    for (int32_t i = 0; i < n_seqs; ++i)
+      for (auto& sent : kv->seqs[into[i]].sent) sent.reserve(nb);
     for (int32_t i = 0; i < n_seqs; ++i)
       if (into[i] != seq_ids[i]) kv->seqs[into[i]].blocks.reserve(nb);
     std::vector<int32_t> from_off(n_seqs), len(n_seqs);
@@ -508,16 +450,16 @@ extern "C" int pipesd_kv4_evict(pipesd_kv4* kv, int32_t n_seqs, const int32_t* s
       old[i].swap(t.blocks);
       t.blocks.swap(fresh[i]);
       t.which ^= 1;
-      t.synced = 0;
+      std::fill(t.sent[t.which].begin(), t.sent[t.which].end(), -1);
     }
     auto launch = [&]() -> int {
-      if (int rc = kv4_send(kv, ids, nullptr, 0, st)) return rc;
+      if (int rc = kv4_send(kv, n_seqs, into, nullptr, st)) return rc;
       Kv4Cuts cuts;
       cuts.keep = keep;
       cuts.recent = recent;
       const int64_t per = (int64_t)kv->cfg.n_layers * kv->cfg.n_kv_heads * keep;
-      for (int32_t i0 = 0; i0 < n_seqs; i0 += kKv4SeqsPerLaunch) {
-        cuts.n = std::min(n_seqs - i0, kKv4SeqsPerLaunch);
+      for (int32_t i0 = 0; i0 < n_seqs; i0 += kKv4ClientsPerLaunch) {
+        cuts.n = std::min(n_seqs - i0, kKv4ClientsPerLaunch);
         for (int32_t i = 0; i < cuts.n; ++i) {
           cuts.seq[i] = seq_ids[i0 + i];
           cuts.into[i] = into[i0 + i];
@@ -536,7 +478,6 @@ extern "C" int pipesd_kv4_evict(pipesd_kv4* kv, int32_t n_seqs, const int32_t* s
       if (rc) {  // back to the blocks before
         t.blocks.swap(old[i]);
         t.which ^= 1;
-        t.synced = (int32_t)t.blocks.size();
       } else {
         t.len = keep;
       }

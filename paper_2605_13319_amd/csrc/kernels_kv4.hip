@@ -1,25 +1,14 @@
-// The 4-bit cache: beginning a pass, rounding rows into it, reading them back, and cutting a client to a budget.
+// The 4-bit cache: block tables, rounding rows into it, reading them back, and cutting a client to a budget.
 #include "kv4.h"
 
 namespace pipesd {
 
-// ------------------------------------------------------------------------------------------------
-// a pass begins: table entries, where its rows go, its workgroups
-// ------------------------------------------------------------------------------------------------
-// (workgroup c: client c of the update; the table's entries are divided among all.  Nobody reads the table in here.)
-__global__ __launch_bounds__(256) void kv4_begin_kernel(Kv4PassUpdate u, int32_t* table, Kv4Row* rows, Kv4Item* items) {
-  for (int i = blockIdx.x * 256 + threadIdx.x; i < u.n_entries; i += gridDim.x * 256) table[u.at[i]] = u.v[i];
-  if ((int)blockIdx.x >= u.n_clients) return;
-  const Kv4Client c = u.client[blockIdx.x];
-  for (int r = threadIdx.x; r < c.n_rows; r += 256) rows[c.row_off + r] = Kv4Row{c.table_off, c.len - c.n_rows + r};
-  // the groups of a split side by side: they read the same tokens
-  for (int i = threadIdx.x; i < c.nsplit * c.groups; i += 256)
-    items[c.item_off + i] = Kv4Item{c.row_off, c.n_rows, c.len, c.table_off, i % c.groups, c.groups, c.span, i / c.groups,
-                                    c.nsplit, c.part_off, c.count_off, c.seq};
+__global__ __launch_bounds__(256) void kv4_table_kernel(Kv4TableUpdate u, int32_t* table) {
+  if ((int)threadIdx.x < u.n) table[u.at[threadIdx.x]] = u.v[threadIdx.x];
 }
-
-hipError_t launch_kv4_begin(const Kv4PassUpdate& u, int32_t* table, Kv4Row* rows, Kv4Item* items, hipStream_t st) {
-  kv4_begin_kernel<<<std::max(1, u.n_clients), 256, 0, st>>>(u, table, rows, items);
+static_assert(kKv4EntriesPerLaunch <= 256, "a thread an entry");
+hipError_t launch_kv4_table(const Kv4TableUpdate& u, int32_t* table, hipStream_t st) {
+  kv4_table_kernel<<<1, 256, 0, st>>>(u, table);
   return hipGetLastError();
 }
 
@@ -112,17 +101,18 @@ using unit_t = typename std::conditional<HD == 128, uint32_t, uint16_t>::type;
 // store: a wave takes 4 neighbouring rows of a head, 16 lanes each
 // ------------------------------------------------------------------------------------------------
 template <int HD, typename T>
-__global__ __launch_bounds__(256) void kv4_store_kernel(Kv4View v, int layer, int n_rows, const Kv4Row* rows, const T* k, const T* val,
-                                                        int64_t k_stride, int64_t v_stride) {
+__global__ __launch_bounds__(256) void kv4_store_kernel(Kv4View v, int layer, Kv4Ranges rg, const T* k, const T* val, int64_t k_stride,
+                                                        int64_t v_stride) {
   constexpr int N = HD / 16;
   const int lane = threadIdx.x & 63, r = lane & 15;
-  const int kvh = blockIdx.x, row = (blockIdx.y * 4 + (threadIdx.x >> 6)) * 4 + (lane >> 4);
-  if (row >= n_rows) return;  // (whole groups of 16 lanes)
-  const Kv4Row at = rows[row];
+  const int kvh = blockIdx.x, c = blockIdx.z, i = (blockIdx.y * 4 + (threadIdx.x >> 6)) * 4 + (lane >> 4);
+  if (i >= rg.count[c]) return;  // (whole groups of 16 lanes)
+  const int64_t row = rg.row_off[c] + i;
+  const int pos = rg.first[c] + i, tok = pos % kBlockTokens;
   float x[N], y[N];
   load_unit<HD>(k + row * k_stride + kvh * HD + r * N, x);
   load_unit<HD>(val + row * v_stride + kvh * HD + r * N, y);
-  const int blk = v.table[at.table_off + at.pos / kBlockTokens], tok = at.pos % kBlockTokens;
+  const int blk = v.table[rg.table_off[c] + pos / kBlockTokens];
   uint8_t* rec = v.pool + kv4_record<HD>(v, layer, blk, kvh);
   uint32_t kp, vp;
   const uint32_t kc = encode_unit<HD>(x, kp), vc = encode_unit<HD>(y, vp);
@@ -134,23 +124,39 @@ __global__ __launch_bounds__(256) void kv4_store_kernel(Kv4View v, int layer, in
   }
 }
 
-hipError_t launch_kv4_store(int dtype, int head_dim, const Kv4View& v, int layer, int n_rows, const Kv4Row* rows, const void* k,
-                            const void* val, int64_t k_stride, int64_t v_stride, hipStream_t st) {
-  for (int r0 = 0; r0 < n_rows; r0 += 65535 * 16) {
-    const int n = std::min(n_rows - r0, 65535 * 16);
-    const dim3 grid(v.n_kv_heads, (n + 15) / 16);
-    auto go = [&](auto hd, auto t) {
+template <class F>
+static void by_type(int dtype, int head_dim, F go) {
+  typedef std::integral_constant<int, 64> H64;
+  typedef std::integral_constant<int, 128> H128;
+  if (head_dim == 128) {
+    if (dtype == PIPESD_F32) go(H128{}, float{}); else go(H128{}, uint16_t{});
+  } else {
+    if (dtype == PIPESD_F32) go(H64{}, float{}); else go(H64{}, uint16_t{});
+  }
+}
+
+// (a grid has at most 65535 workgroups in y: rows by the piece)
+static Kv4Ranges part_of(const Kv4Ranges& r, int i0, int n) {
+  Kv4Ranges p = r;
+  p.most = std::min(r.most - i0, n);
+  for (int c = 0; c < r.n; ++c) {
+    p.first[c] += i0;
+    p.row_off[c] += i0;
+    p.count[c] = std::max(0, std::min(r.count[c] - i0, n));
+  }
+  return p;
+}
+
+hipError_t launch_kv4_store(int dtype, int head_dim, const Kv4View& v, int layer, const Kv4Ranges& r, const void* k, const void* val,
+                            int64_t k_stride, int64_t v_stride, hipStream_t st) {
+  constexpr int kMost = 65535 * 16;
+  for (int i0 = 0; i0 < r.most; i0 += kMost) {
+    const Kv4Ranges p = part_of(r, i0, kMost);
+    by_type(dtype, head_dim, [&](auto hd, auto t) {
       typedef decltype(t) T;
-      kv4_store_kernel<decltype(hd)::value, T><<<grid, 256, 0, st>>>(v, layer, n, rows + r0, (const T*)k + r0 * k_stride,
-                                                                     (const T*)val + r0 * v_stride, k_stride, v_stride);
-    };
-    typedef std::integral_constant<int, 64> H64;
-    typedef std::integral_constant<int, 128> H128;
-    if (head_dim == 128) {
-      if (dtype == PIPESD_F32) go(H128{}, float{}); else go(H128{}, uint16_t{});
-    } else {
-      if (dtype == PIPESD_F32) go(H64{}, float{}); else go(H64{}, uint16_t{});
-    }
+      kv4_store_kernel<decltype(hd)::value, T><<<dim3(v.n_kv_heads, (p.most + 15) / 16, p.n), 256, 0, st>>>(v, layer, p, (const T*)k, (const T*)val,
+                                                                                                       k_stride, v_stride);
+    });
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -174,11 +180,11 @@ __device__ __forceinline__ void store_unit(T* p, const uint32_t (&w)[HD / 32]) {
 }
 
 template <int HD, typename T>
-__global__ __launch_bounds__(256) void kv4_read_kernel(Kv4View v, int layer0, Kv4Ranges rg, int client0, int64_t total_rows, T* k,
+__global__ __launch_bounds__(256) void kv4_read_kernel(Kv4View v, int layer0, Kv4Ranges rg, int64_t total_rows, T* k,
                                                        T* val) {
   constexpr int N = HD / 16;
   const int lane = threadIdx.x & 63, r = lane & 15, wave = threadIdx.x >> 6;
-  const int c = client0 + blockIdx.z, layer = blockIdx.y / v.n_kv_heads, kvh = blockIdx.y % v.n_kv_heads;
+  const int c = blockIdx.z, layer = blockIdx.y / v.n_kv_heads, kvh = blockIdx.y % v.n_kv_heads;
   const int i = (blockIdx.x * 4 + wave) * 4 + (lane >> 4);
   if (i >= rg.count[c]) return;
   const int pos = rg.first[c] + i, tok = pos % kBlockTokens;
@@ -201,18 +207,11 @@ hipError_t launch_kv4_read(int dtype, int head_dim, const Kv4View& v, int layer0
   for (int l0 = 0; l0 < n_layers; l0 += per) {
     const int nl = std::min(per, n_layers - l0);
     const dim3 grid((r.most + 15) / 16, nl * v.n_kv_heads, r.n);
-    auto go = [&](auto hd, auto t) {
+    by_type(dtype, head_dim, [&](auto hd, auto t) {
       typedef decltype(t) T;
       const int64_t off = (int64_t)l0 * total_rows * v.n_kv_heads * head_dim;
-      kv4_read_kernel<decltype(hd)::value, T><<<grid, 256, 0, st>>>(v, layer0 + l0, r, 0, total_rows, (T*)k + off, (T*)val + off);
-    };
-    typedef std::integral_constant<int, 64> H64;
-    typedef std::integral_constant<int, 128> H128;
-    if (head_dim == 128) {
-      if (dtype == PIPESD_F32) go(H128{}, float{}); else go(H128{}, uint16_t{});
-    } else {
-      if (dtype == PIPESD_F32) go(H64{}, float{}); else go(H64{}, uint16_t{});
-    }
+      kv4_read_kernel<decltype(hd)::value, T><<<grid, 256, 0, st>>>(v, layer0 + l0, r, total_rows, (T*)k + off, (T*)val + off);
+    });
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

@@ -40,66 +40,121 @@ __device__ __forceinline__ int64_t kv4_record(const Kv4View& v, int layer, int b
 
 // ---- the plan of a pass ------------------------------------------------------------------------
 // A client's query rows are taken with the heads that share a head of the cache: row rr of a cache head is pass row rr /
-// group, head rr % group of the group; 16 of them make a tile.  Few tiles: the four waves of a workgroup take every fourth
-// 32 tokens of a span for the same T tiles and join their sums.  Many tiles: each wave takes T tiles of its own.
-constexpr int kKv4Waves = 4;
-constexpr int kKv4TilesBf16 = 4, kKv4TilesF32 = 2;  // tiles of a wave at most
-constexpr int kKv4ManyTiles = 16;  // from here on they do
+// group, head rr % group of the group; 16 of them make a tile.
+//   few tiles    the waves of a workgroup take every WAVES-th 32 tokens of a span for the same one or two tiles, and
+//                join their sums
+//   many tiles   each of four waves takes tiles of its own
+constexpr int kKv4ManyTiles = 16;  // (from here on)
+constexpr int kKv4WideWaves = 4;
+constexpr int kKv4WideTilesBf16 = 4, kKv4WideTilesF32 = 2;  // of a wave
 constexpr int kKv4MaxSplits = 64;
+constexpr int kKv4FewMaxTiles = 2;
+inline int kv4_few_waves(int tiles) { return tiles == 1 ? 8 : 4; }
 
+// Clients of a launch, by value.  Workgroups: (cache head, item); a client's items are its splits, the groups of tiles of a
+// split side by side, for they read the same tokens.
+constexpr int kKv4ClientsPerLaunch = 32;
+struct Kv4Clients {
+  int32_t n, items, span;  // span: tokens of a split
+  int32_t first[kKv4ClientsPerLaunch];  // item (beyond the last client: the number of items)
+  int32_t seq[kKv4ClientsPerLaunch], table_off[kKv4ClientsPerLaunch], len[kKv4ClientsPerLaunch];  // len: with the pass's own rows
+  int32_t n_rows[kKv4ClientsPerLaunch], row_off[kKv4ClientsPerLaunch];
+  int32_t groups[kKv4ClientsPerLaunch], nsplit[kKv4ClientsPerLaunch];
+  int32_t part_off[kKv4ClientsPerLaunch];   // tiles; the client's partials are [cache head][group][split][tiles of a workgroup]
+  int32_t count_off[kKv4ClientsPerLaunch];  // arrival counters [cache head][group]
+};
 struct Kv4Client {
-  int32_t seq, n_rows, row_off, len;  // len: cached tokens, the pass's own rows included
-  int32_t table_off;                  // entries to the client's block table
-  int32_t wide, tiles, groups;        // tiles of a workgroup; workgroups for all tiles of a cache head
-  int32_t span, nsplit;               // tokens of a split
-  int32_t item_off, count_off;        // first item, first arrival counter
-  int32_t part_off;                   // partial sums, in tiles of 16 rows
+  int32_t seq, n_rows, row_off, len;
 };
-struct Kv4Item {  // one workgroup per cache head
-  int32_t row_off, n_rows, len, table_off;
-  int32_t group, groups, span, split;
-  int32_t nsplit, part_off, count_off, seq;  // the client's: partials [cache head][group][split][tile], counters [cache head][group]
+struct Kv4Launch {
+  int32_t wide, tiles;  // tiles: of a workgroup (few), of a wave (many)
+  Kv4Clients c;
+};
+struct Kv4PlanNeeds {
+  size_t part_tiles, counters;
 };
 
-// The split of one client; its results do not depend on who shares the pass.
-inline void kv4_plan_client(Kv4Client& c, int dtype, int n_q_heads, int n_kv_heads, int n_cu) {
-  const int most = dtype == PIPESD_F32 ? kKv4TilesF32 : kKv4TilesBf16;
-  const int nqt = std::max(1, attn_query_tiles(n_q_heads / n_kv_heads, c.n_rows));
-  c.wide = nqt >= kKv4ManyTiles;
-  c.tiles = c.wide ? kKv4Waves * most : std::min(nqt, most);
-  c.groups = (nqt + c.tiles - 1) / c.tiles;
-  const int step = c.wide ? 32 : kKv4Waves * 32;
-  const int least = c.wide ? 512 : 128 * c.tiles;
-  const long want = std::min<long>(kKv4MaxSplits, std::max<long>(1, 4L * n_cu / ((long)n_kv_heads * c.groups)));
-  const long span = std::max<long>(least, (c.len + want - 1) / want);
-  c.span = (int)((span + step - 1) / step * step);
-  c.nsplit = std::max(1, (c.len + c.span - 1) / c.span);
+// The launches of a pass: clients of few and of many tiles apart, at most kKv4ClientsPerLaunch in one.  All splits of a kind
+// are as long: as short as leaves the workgroups of the pass one round on the device, and no shorter than a step of the
+// workgroup.  So what a row's sums are cut into depends on the pass, not on timing.
+template <class Out>  // std::vector<Kv4Launch>
+inline Kv4PlanNeeds kv4_plan(const Kv4Client* cl, int n, int dtype, int n_q_heads, int n_kv_heads, int n_cu, Out& out) {
+  out.clear();
+  const int group = n_q_heads / n_kv_heads;
+  Kv4PlanNeeds need{0, 0};
+  for (int wide = 0; wide < 2; ++wide) {
+    auto tiles_of = [&](const Kv4Client& c) { return attn_query_tiles(group, c.n_rows); };
+    auto mine = [&](const Kv4Client& c) { return c.n_rows > 0 && (tiles_of(c) >= kKv4ManyTiles) == (wide != 0); };
+    auto workgroups = [&](int tiles, int64_t span) {
+      int64_t w = 0;
+      for (int i = 0; i < n; ++i)
+        if (mine(cl[i])) w += (int64_t)n_kv_heads * ((tiles_of(cl[i]) + tiles - 1) / tiles) * ((cl[i].len + span - 1) / span);
+      return w;
+    };
+    int most_tiles = 0, longest = 0;
+    for (int i = 0; i < n; ++i)
+      if (mine(cl[i])) most_tiles = std::max(most_tiles, tiles_of(cl[i])), longest = std::max(longest, (int)cl[i].len);
+    if (most_tiles == 0) continue;
+    int tiles, wg_tiles, step;
+    if (wide) {
+      tiles = dtype == PIPESD_F32 ? kKv4WideTilesF32 : kKv4WideTilesBf16;
+      wg_tiles = kKv4WideWaves * tiles;
+      step = 512;
+    } else {
+      tiles = most_tiles == 1 || workgroups(1, kv4_few_waves(1) * 32) <= 2L * n_cu ? 1 : 2;
+      wg_tiles = tiles;
+      step = kv4_few_waves(tiles) * 32;
+    }
+    int64_t span = step;
+    while (workgroups(wg_tiles, span) > 2L * n_cu && span < longest) span += span < 16 * step ? step : span / 16 / step * step;
+    span = std::max<int64_t>(span, ((longest + kKv4MaxSplits - 1) / kKv4MaxSplits + step - 1) / step * step);
+    Kv4Launch l{};
+    auto flush = [&] {
+      if (l.c.n == 0) return;
+      for (int i = l.c.n; i < kKv4ClientsPerLaunch; ++i) l.c.first[i] = l.c.items;
+      out.push_back(l);
+      l = Kv4Launch{};
+    };
+    for (int i = 0; i < n; ++i) {
+      if (!mine(cl[i])) continue;
+      if (l.c.n == kKv4ClientsPerLaunch) flush();
+      const int j = l.c.n++;
+      l.wide = wide;
+      l.tiles = tiles;
+      l.c.span = (int)span;
+      l.c.first[j] = l.c.items;
+      l.c.seq[j] = cl[i].seq;
+      l.c.len[j] = cl[i].len;
+      l.c.n_rows[j] = cl[i].n_rows;
+      l.c.row_off[j] = cl[i].row_off;
+      l.c.groups[j] = (tiles_of(cl[i]) + wg_tiles - 1) / wg_tiles;
+      l.c.nsplit[j] = (int)((cl[i].len + span - 1) / span);
+      l.c.items += l.c.groups[j] * l.c.nsplit[j];
+      l.c.part_off[j] = (int)need.part_tiles;
+      l.c.count_off[j] = (int)need.counters;
+      need.counters += (size_t)n_kv_heads * l.c.groups[j];
+      if (l.c.nsplit[j] > 1) need.part_tiles += (size_t)n_kv_heads * l.c.groups[j] * l.c.nsplit[j] * wg_tiles;
+    }
+    flush();
+  }
+  return need;
 }
 
-// What begins a pass: block-table entries that changed and the clients, some per launch (by value: no copy that the host
-// would have to keep).
-constexpr int kKv4ClientsPerLaunch = 32, kKv4EntriesPerLaunch = 256;
-struct Kv4PassUpdate {
-  int32_t n_clients, n_entries;
-  Kv4Client client[kKv4ClientsPerLaunch];
+// block-table entries that changed, by value: no copy that the host would have to keep
+constexpr int kKv4EntriesPerLaunch = 256;
+struct Kv4TableUpdate {
+  int32_t n;
   int32_t at[kKv4EntriesPerLaunch], v[kKv4EntriesPerLaunch];  // table[at[i]] = v[i]
 };
-// where a new row goes, and whose it is
-struct Kv4Row {
-  int32_t table_off, pos;
-};
-hipError_t launch_kv4_begin(const Kv4PassUpdate& u, int32_t* table, Kv4Row* rows, Kv4Item* items, hipStream_t st);
+hipError_t launch_kv4_table(const Kv4TableUpdate& u, int32_t* table, hipStream_t st);
 
 // ---- the operators -----------------------------------------------------------------------------
-hipError_t launch_kv4_store(int dtype, int head_dim, const Kv4View& v, int layer, int n_rows, const Kv4Row* rows, const void* k,
-                            const void* val, int64_t k_stride, int64_t v_stride, hipStream_t st);
-
-constexpr int kKv4SeqsPerLaunch = 64;
-struct Kv4Ranges {
-  int32_t n;
-  int32_t table_off[kKv4SeqsPerLaunch], first[kKv4SeqsPerLaunch], count[kKv4SeqsPerLaunch], row_off[kKv4SeqsPerLaunch];
-  int32_t most;  // largest count
+struct Kv4Ranges {  // tokens of clients, and the rows that stand for them
+  int32_t n, most;  // most: largest count
+  int32_t table_off[kKv4ClientsPerLaunch], first[kKv4ClientsPerLaunch], count[kKv4ClientsPerLaunch], row_off[kKv4ClientsPerLaunch];
 };
+hipError_t launch_kv4_store(int dtype, int head_dim, const Kv4View& v, int layer, const Kv4Ranges& r, const void* k, const void* val,
+                            int64_t k_stride, int64_t v_stride, hipStream_t st);
 // out [n_layers][total_rows][n_kv_heads][head_dim]
 hipError_t launch_kv4_read(int dtype, int head_dim, const Kv4View& v, int layer0, int n_layers, const Kv4Ranges& r, int64_t total_rows,
                            void* k, void* val, hipStream_t st);
@@ -111,30 +166,22 @@ struct Kv4AttendCall {
   void* out;
   int64_t q_stride, out_stride;  // elements between rows
   const int32_t* limits;         // tokens that each row sees, or nullptr: all up to its own
-  const Kv4Item* items;
-  int32_t item0, n_items;        // this launch's
-  int32_t wide, tiles;
   float* part;
   unsigned* counters;
   float* lse;                    // [rows][n_q_heads], or nullptr: base-2 logarithm of each row's sum of weights
-  // weights given to the cached tokens (launch_kv4_mass; clients one after the other)
+  // weights given to the cached tokens (launch_kv4_mass)
   float* mass;                   // [max_seqs][n_layers][n_kv_heads][mass_stride]
   int64_t mass_stride;
   float decay;
 };
 constexpr int kKv4PartPad = 4;  // a partial row is [head_dim values, max, sum, 2 unused]
-hipError_t launch_kv4_attend(const Kv4AttendCall& c, hipStream_t st);
-
-struct Kv4MassClients {
-  int32_t n, most;  // most: the largest len
-  int32_t seq[kKv4SeqsPerLaunch], table_off[kKv4SeqsPerLaunch], n_rows[kKv4SeqsPerLaunch], row_off[kKv4SeqsPerLaunch], len[kKv4SeqsPerLaunch];
-};
-hipError_t launch_kv4_mass(const Kv4AttendCall& c, const Kv4MassClients& clients, hipStream_t st);
+hipError_t launch_kv4_attend(const Kv4AttendCall& c, const Kv4Launch& l, hipStream_t st);
+hipError_t launch_kv4_mass(const Kv4AttendCall& c, const Kv4Clients& clients, hipStream_t st);
 
 struct Kv4Cuts {
   int32_t n, keep, recent;
-  int32_t seq[kKv4SeqsPerLaunch], into[kKv4SeqsPerLaunch], len[kKv4SeqsPerLaunch];
-  int32_t from_off[kKv4SeqsPerLaunch], to_off[kKv4SeqsPerLaunch];  // entries to the tables of the old and of the new blocks
+  int32_t seq[kKv4ClientsPerLaunch], into[kKv4ClientsPerLaunch], len[kKv4ClientsPerLaunch];
+  int32_t from_off[kKv4ClientsPerLaunch], to_off[kKv4ClientsPerLaunch];  // entries to the tables of the old and of the new blocks
 };
 // kept [n][n_layers][n_kv_heads][keep]
 hipError_t launch_kv4_select(const Kv4View& v, const Kv4Cuts& c, float* mass, int64_t mass_stride, int32_t* kept, hipStream_t st);
