@@ -385,7 +385,8 @@ enum { PIPESD_KV4_MAX_PASS_SEQS = 256, PIPESD_KV4_MAX_ROWS = 2048 };
 size_t pipesd_kv4_block_bytes(const pipesd_config *cfg, int32_t block_tokens);
 
 /* Cache of up to max_seqs clients over a caller-allocated device pool of floor(pool_bytes / block bytes) blocks (borrowed until
- * pipesd_kv4_destroy).  Of the config it takes n_layers, n_q_heads, n_kv_heads, head_dim (64 or 128) and dtype.  Beside the
+ * pipesd_kv4_destroy).  Of the config it takes n_layers, n_q_heads, n_kv_heads (at most 256
+ * query heads each), head_dim (64 or 128) and dtype.  Beside the
  * pool it allocates the block tables and what passes of up to PIPESD_MAX_ROWS rows by 16 clients need.  pool == NULL: bookkeeping only.
  * EINVAL: an unsupported config, block_tokens != 16, max_seqs < 1, no room for one block, a pool that is not 256-byte
  * aligned or of 2^31 tokens or table entries (2 * max_seqs * blocks) and more; ENOMEM: an allocation failed. */

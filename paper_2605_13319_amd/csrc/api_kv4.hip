@@ -79,7 +79,7 @@ static void kv4_close_pass(pipesd_kv4* kv) {
 static bool kv4_config_ok(const pipesd_config* c) {
   return c->n_layers >= 1 && c->n_kv_heads >= 1 && c->n_q_heads >= 1 && c->n_q_heads % c->n_kv_heads == 0 &&
          (c->head_dim == 64 || c->head_dim == 128) && (c->dtype == PIPESD_F32 || c->dtype == PIPESD_BF16) && c->n_kv_heads <= 65535 &&
-         c->n_layers <= 65535 && (int64_t)c->n_layers * c->n_kv_heads <= INT32_MAX && c->n_q_heads <= (1 << 20);
+         c->n_layers <= 65535 && (int64_t)c->n_layers * c->n_kv_heads <= INT32_MAX && c->n_q_heads / c->n_kv_heads <= 256;
 }
 
 extern "C" size_t pipesd_kv4_block_bytes(const pipesd_config* cfg, int32_t block_tokens) {
@@ -156,7 +156,7 @@ extern "C" int pipesd_kv4_create(const pipesd_config* cfg, int32_t max_seqs, int
     for (int32_t n : {1, clients})
       for (int32_t m = 1; m <= kMaxRows; ++m) {
         std::vector<Kv4Client> c(n, Kv4Client{0, m, 0, (int32_t)std::min<size_t>((size_t)kv->n_blocks * kBlockTokens, (size_t)1 << 24)});
-        const Kv4PlanNeeds need = kv4_plan(c.data(), n, cfg->dtype, cfg->n_q_heads, cfg->n_kv_heads, kv->n_cu, scratch);
+        const Kv4PlanNeeds need = kv4_plan(c.data(), n, cfg->dtype, cfg->head_dim, cfg->n_q_heads, cfg->n_kv_heads, kv->n_cu, scratch);
         tiles = std::max(tiles, need.part_tiles);
         counts = std::max(counts, need.counters);
       }
@@ -261,7 +261,7 @@ extern "C" int pipesd_kv4_extend(pipesd_kv4* kv, int32_t n_seqs, const int32_t* 
       row += n_new[i];
     }
     if (kv->pool && attends) {
-      const Kv4PlanNeeds need = kv4_plan(plan.data(), (int)plan.size(), cfg.dtype, cfg.n_q_heads, cfg.n_kv_heads, kv->n_cu, launches);
+      const Kv4PlanNeeds need = kv4_plan(plan.data(), (int)plan.size(), cfg.dtype, cfg.head_dim, cfg.n_q_heads, cfg.n_kv_heads, kv->n_cu, launches);
       if (need.part_tiles > (size_t)INT32_MAX || need.counters > (size_t)INT32_MAX) return PIPESD_ENOMEM;
       for (Kv4Launch& l : launches)
         for (int32_t j = 0; j < l.c.n; ++j) l.c.table_off[j] = kv->table_off(l.c.seq[j]);
@@ -353,6 +353,7 @@ extern "C" int pipesd_kv4_attend(pipesd_kv4* kv, int32_t layer, const void* q, i
   a.dtype = kv->cfg.dtype;
   a.head_dim = kv->cfg.head_dim;
   a.n_q_heads = kv->cfg.n_q_heads;
+  a.group = kv->cfg.n_q_heads / kv->cfg.n_kv_heads;
   a.layer = layer;
   a.q = q;
   a.out = out;

@@ -46,10 +46,9 @@ __device__ __forceinline__ int64_t kv4_record(const Kv4View& v, int layer, int b
 //   many tiles   each of four waves takes tiles of its own
 constexpr int kKv4ManyTiles = 16;  // (from here on)
 constexpr int kKv4WideWaves = 4;
-constexpr int kKv4WideTilesBf16 = 4, kKv4WideTilesF32 = 2;  // of a wave
+constexpr int kv4_wide_tiles(int dtype, int head_dim) { return dtype == PIPESD_BF16 && head_dim == 64 ? 3 : 2; }  // of a wave
 constexpr int kKv4MaxSplits = 64;
-constexpr int kKv4FewMaxTiles = 2;
-inline int kv4_few_waves(int tiles) { return tiles == 1 ? 8 : 4; }
+constexpr int kv4_few_waves(int tiles) { return tiles == 1 ? 8 : 4; }
 
 // Clients of a launch, by value.  Workgroups: (cache head, item); a client's items are its splits, the groups of tiles of a
 // split side by side, for they read the same tokens.
@@ -74,11 +73,21 @@ struct Kv4PlanNeeds {
   size_t part_tiles, counters;
 };
 
+// One tile a workgroup or two.  Two share the conversion of keys and values (a step of 32 tokens takes 1.5 times as long, not
+// twice), but leave registers for half the waves and twice the rows to join: measured on a device of 256 compute units, a
+// launch takes 8 us + 0.14 us per step and compute unit of one tile, 14 us + 0.215 us of two (head dim 64: 0.086 and 0.10).
+// Two in fp32 were never faster: 4 clients of 9 rows behind 4096 tokens 32.9 us, 21.9 with one.
+inline int kv4_few_tiles(int dtype, int head_dim, double work1, double work2, int n_cu) {
+  if (dtype == PIPESD_F32) return 1;
+  const double one = head_dim == 128 ? 0.14 : 0.086, two = head_dim == 128 ? 0.215 : 0.10;
+  return 8 + one * work1 / n_cu <= 14 + two * work2 / n_cu ? 1 : 2;
+}
+
 // The launches of a pass: clients of few and of many tiles apart, at most kKv4ClientsPerLaunch in one.  All splits of a kind
 // are as long: as short as leaves the workgroups of the pass one round on the device, and no shorter than a step of the
 // workgroup.  So what a row's sums are cut into depends on the pass, not on timing.
 template <class Out>  // std::vector<Kv4Launch>
-inline Kv4PlanNeeds kv4_plan(const Kv4Client* cl, int n, int dtype, int n_q_heads, int n_kv_heads, int n_cu, Out& out) {
+inline Kv4PlanNeeds kv4_plan(const Kv4Client* cl, int n, int dtype, int head_dim, int n_q_heads, int n_kv_heads, int n_cu, Out& out) {
   out.clear();
   const int group = n_q_heads / n_kv_heads;
   Kv4PlanNeeds need{0, 0};
@@ -91,21 +100,29 @@ inline Kv4PlanNeeds kv4_plan(const Kv4Client* cl, int n, int dtype, int n_q_head
         if (mine(cl[i])) w += (int64_t)n_kv_heads * ((tiles_of(cl[i]) + tiles - 1) / tiles) * ((cl[i].len + span - 1) / span);
       return w;
     };
+    auto work = [&](int tiles) {  // steps of 32 tokens of all workgroups' sets of tiles
+      double w = 0;
+      for (int i = 0; i < n; ++i)
+        if (mine(cl[i])) w += (double)n_kv_heads * ((tiles_of(cl[i]) + tiles - 1) / tiles) * cl[i].len / 32;
+      return w;
+    };
     int most_tiles = 0, longest = 0;
     for (int i = 0; i < n; ++i)
       if (mine(cl[i])) most_tiles = std::max(most_tiles, tiles_of(cl[i])), longest = std::max(longest, (int)cl[i].len);
     if (most_tiles == 0) continue;
     int tiles, wg_tiles, step;
     if (wide) {
-      tiles = dtype == PIPESD_F32 ? kKv4WideTilesF32 : kKv4WideTilesBf16;
+      tiles = kv4_wide_tiles(dtype, head_dim);
       wg_tiles = kKv4WideWaves * tiles;
       step = 512;
     } else {
-      tiles = most_tiles == 1 || workgroups(1, kv4_few_waves(1) * 32) <= 2L * n_cu ? 1 : 2;
+      tiles = kv4_few_tiles(dtype, head_dim, work(1), work(2), n_cu);
       wg_tiles = tiles;
       step = kv4_few_waves(tiles) * 32;
     }
-    int64_t span = step;
+    // (a split costs what joins it, about the time of three steps: none below 768 tokens)
+    int64_t span = std::max<int64_t>(step, longest <= 768 ? longest : 0);
+    span = (span + step - 1) / step * step;
     while (workgroups(wg_tiles, span) > 2L * n_cu && span < longest) span += span < 16 * step ? step : span / 16 / step * step;
     span = std::max<int64_t>(span, ((longest + kKv4MaxSplits - 1) / kKv4MaxSplits + step - 1) / step * step);
     Kv4Launch l{};
@@ -161,7 +178,7 @@ hipError_t launch_kv4_read(int dtype, int head_dim, const Kv4View& v, int layer0
 
 struct Kv4AttendCall {
   Kv4View view;
-  int dtype, head_dim, n_q_heads, layer;
+  int dtype, head_dim, n_q_heads, group, layer;  // group: query heads of a cache head
   const void* q;
   void* out;
   int64_t q_stride, out_stride;  // elements between rows
