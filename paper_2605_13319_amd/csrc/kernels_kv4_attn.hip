@@ -21,24 +21,19 @@ typedef __attribute__((ext_vector_type(4))) unsigned k4u32x4;
 typedef __attribute__((ext_vector_type(2))) unsigned k4u32x2;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 
-template <int HD, int NP>
-struct Queries {  // one tile of 16 rows as operand B: piece p, step s
-  k4u32x4 q[NP][HD / 32];
-};
-
 template <int HD>
 __device__ __forceinline__ float kv4_scale() { return (HD == 128 ? 0.08838834764831845f : 0.125f) * 1.44269504088896341f; }  // log2(e) / sqrt(HD)
 
-// Lane (c, g) of a product's operands holds 8 channels of row c; in step s these are g * HD / 4 + 8 s .. + 7, so that what a lane
-// needs of a key in all steps is one load, and of one power.
-template <int HD, int NP, typename T>
-__device__ __forceinline__ void load_queries(const T* row, bool live, int g, Queries<HD, NP>& out) {
+// Queries as operand B.  A lane holds 8 channels of its row in each step of a product; in step s these are 8 s .. + 7 of the
+// lane's own part of the row, so that what it needs of a key in all steps is one load.
+template <int NP, int NS, typename T>
+__device__ __forceinline__ void load_queries(const T* part, bool live, k4u32x4 (&out)[NP][NS]) {
 #pragma unroll
-  for (int s = 0; s < HD / 32; ++s) {
-    const T* p = row + g * (HD / 4) + s * 8;
+  for (int s = 0; s < NS; ++s) {
+    const T* p = part + s * 8;
     if constexpr (sizeof(T) == 2) {
       const k4u32x4 x = *(const k4u32x4*)p;
-      out.q[0][s] = live ? x : k4u32x4{0u, 0u, 0u, 0u};
+      out[0][s] = live ? x : k4u32x4{0u, 0u, 0u, 0u};
     } else {
       const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
       float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
@@ -54,7 +49,7 @@ __device__ __forceinline__ void load_queries(const T* row, bool live, int g, Que
           x[2 * i] -= __uint_as_float(lo & 0xffff0000u);
           x[2 * i + 1] -= __uint_as_float(hi & 0xffff0000u);
         }
-        out.q[m][s] = k4u32x4{w[0], w[1], w[2], w[3]};
+        out[m][s] = k4u32x4{w[0], w[1], w[2], w[3]};
       }
     }
   }
@@ -126,27 +121,15 @@ __device__ __forceinline__ void drop_values(Codes& v, unsigned& powers, int left
 
 // Wait states behind the last products of sums, tied to all of them: whoever reads them next may be in another basic block,
 // where the compiler pads too few.
-template <int TILES, int HT>
-__device__ __forceinline__ void settle(f32x4 (&acc)[TILES][HT]) {
+template <int N, int M, class V>
+__device__ __forceinline__ void settle(V (&x)[N][M]) {
 #pragma unroll
-  for (int t = TILES - 1; t >= 0; --t) {
-    auto& x = acc[t];
-    if (t == 0) {
-      if constexpr (HT == 8)
-        asm volatile("s_nop 15\n\ts_nop 1" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(x[4]), "+v"(x[5]), "+v"(x[6]), "+v"(x[7]));
-      else if constexpr (HT == 2)
-        asm volatile("s_nop 15\n\ts_nop 1" : "+v"(x[0]), "+v"(x[1]));
-      else
-        asm volatile("s_nop 15\n\ts_nop 1" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]));
-    } else {
-      if constexpr (HT == 2)
-        asm volatile("" : "+v"(x[0]), "+v"(x[1]));
-      else if constexpr (HT == 8)
-        asm volatile("" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(x[4]), "+v"(x[5]), "+v"(x[6]), "+v"(x[7]));
-      else
-        asm volatile("" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]));
-    }
-  }
+  for (int i = 0; i < N * M; ++i)
+    if (i > 0) asm volatile("" : "+v"(x[i / M][i % M]));
+  asm volatile("s_nop 15\n\ts_nop 1" : "+v"(x[0][0]));  // (in order: the products of all others come before)
+#pragma unroll
+  for (int i = 0; i < N * M; ++i)
+    if (i > 0) asm volatile("" : "+v"(x[i / M][i % M]));
 }
 
 // where lane (c, g) finds its part of a record
@@ -225,296 +208,37 @@ __device__ __forceinline__ Kv4Item find_item(const Kv4Clients& cl, int item, int
   return Kv4Item{ci, groups - 1 - (i - split * groups), split};  // (the last rows see most: first)
 }
 
-// A wave walks tokens 32 at a time.  Per tile of 16 query rows it keeps a running maximum, sum and O^T in registers; the maximum moves
-// only when a score passes it by 2^8 (any scale will do for fp32 sums: most steps then need no exchange between lanes and
-// no rescaling).
-// FEW tiles: the waves share them and join their states through LDS at the end.  MANY: each wave has its own; keys and values
-// are converted once, by the four waves in turn (one a block's keys, one its values), into operands in LDS that all read:
-// two steps by turns, one barrier a step.
-// LDS: states [tile][wave][row], later what joins the splits, or operands [2 steps]([2 blocks][steps of a product][lane] keys,
-// [tile of channels][lane] values); then the queries that registers do not hold; words
-template <int HD, int TILES, int WAVES, bool WIDE>
-constexpr size_t state_floats() {
-  return WIDE ? 2 * (2 * (HD / 32) + HD / 16) * 64 * 4 : (size_t)TILES * WAVES * 16 * (HD + kKv4PartPad);
-}
+// A wave walks tokens 32 at a time (a step): scores of the step, weights, products with the values.
 template <typename T>
 constexpr int pieces() { return sizeof(T) == 4 ? 3 : 1; }
-template <int HD, typename T, int TILES, bool WIDE>
-constexpr bool queries_in_lds() { return !WIDE && TILES * pieces<T>() * (HD / 8) > 32; }
-template <int HD, typename T, int TILES, int WAVES, bool WIDE>
-constexpr size_t attend_lds_bytes() {
-  return state_floats<HD, TILES, WAVES, WIDE>() * sizeof(float) + (queries_in_lds<HD, T, TILES, WIDE>() ? (size_t)TILES * sizeof(Queries<HD, pieces<T>()>) * 64 : 0) + 32;
-}
-template <int HD, typename T, int TILES, bool WIDE>
-constexpr int attend_waves_per_simd() { return WIDE ? (sizeof(T) == 4 ? 2 : 3) : TILES == 1 ? 4 : 2; }
 
-template <int HD, typename T, int TILES, int WAVES, bool WIDE>
-__global__ __launch_bounds__(WAVES * 64, (attend_waves_per_simd<HD, T, TILES, WIDE>())) void kv4_attend_kernel(Kv4AttendCall a, Kv4Clients clients) {
-  constexpr int NP = pieces<T>(), NS = HD / 32, HT = HD / 16, ROW = HD + kKv4PartPad;
-  constexpr bool Q_LDS = queries_in_lds<HD, T, TILES, WIDE>();
-  constexpr int WG_TILES = WIDE ? WAVES * TILES : TILES;
-  constexpr int STEP = WIDE ? 32 : WAVES * 32;
-  typedef typename std::conditional<HD == 128, k4u32x4, k4u32x2>::type Codes;
-  extern __shared__ float lds[];
-  int* last_lds = (int*)((char*)lds + attend_lds_bytes<HD, T, TILES, WAVES, WIDE>() - 32);
+// What a workgroup knows of its client, and how rows leave it.
+template <int HD, typename T>
+struct Work {
+  const Kv4AttendCall& a;
+  int kvh, len, n_rows, row_off, groups, nsplit, group_rows, first_row;  // group_rows: query rows of the cache head; first_row: the group's first
+  float group_rinv;
+  const int32_t* table;
+  float* all;   // partial rows of the group's splits: [split][tiles of a workgroup][16][ROW]
+  unsigned* counter;
+  static constexpr int ROW = HD + kKv4PartPad;
 
-  const int kvh = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int c = lane & 15, g = lane >> 4;
-  const Kv4Item it = find_item(clients, blockIdx.y, lane);
-  const int len = clients.len[it.ci], n_rows = clients.n_rows[it.ci], row_off = clients.row_off[it.ci];
-  const int groups = clients.groups[it.ci], nsplit = clients.nsplit[it.ci];
-  const int group = a.group;
-  const float group_rinv = __builtin_amdgcn_rcpf((float)group);
-  const int R = n_rows * group;
-  const int tile0 = it.group * WG_TILES + (WIDE ? w * TILES : 0);
-  const int span0 = it.split * clients.span;
-  const int32_t* table = a.view.table + clients.table_off[it.ci];
-
-  const int first = span0 + (WIDE ? 0 : w * 32);
-  // the records of 64 steps' blocks sit in the lanes: lane L has where the two of step L begin
-  int64_t step_rec[2];
-  const int64_t block_bytes = (int64_t)a.view.n_kv_heads * Kv4Record<HD>::kBytes;
-  const uint8_t* head_base = a.view.pool + (int64_t)a.layer * a.view.n_blocks * block_bytes + kvh * Kv4Record<HD>::kBytes;
-  auto load_blocks = [&](int it0) {
-#pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
-      const int64_t tok = (int64_t)first + (int64_t)(it0 + lane) * STEP + tt * 16;
-      step_rec[tt] = table[tok < len ? (int)(tok / kBlockTokens) : 0] * block_bytes;
-    }
-  };
-  load_blocks(0);
-
-  // ---- queries, and how far each row sees ----
-  // (in registers, or where the sums leave no room for them in LDS: [tile][piece][step][lane])
-  Queries<HD, NP> q[Q_LDS ? 1 : TILES];
-  k4u32x4* q_lds = (k4u32x4*)(lds + state_floats<HD, TILES, WAVES, WIDE>()) + lane;
-  int lim[TILES];
-  int lo = len, hi = 0;
-#pragma unroll
-  for (int t = 0; t < TILES; ++t) {
-    const TileRow tr = tile_row((tile0 + t) * 16 + c, group, group_rinv, n_rows, row_off, kvh);
-    load_queries<HD, NP>((const T*)a.q + tr.row * a.q_stride + tr.head * HD, tr.live, g, q[Q_LDS ? 0 : t]);
-    if constexpr (Q_LDS) {  // (the waves of one set of tiles write the same)
-#pragma unroll
-      for (int i = 0; i < NP * NS; ++i) q_lds[(t * NP * NS + i) * 64] = q[0].q[i / NS][i % NS];
-    }
-    lim[t] = row_limit(a.limits, tr.row, row_off, n_rows, len);
-    if (tr.live) lo = min(lo, lim[t]), hi = max(hi, lim[t]);
+  __device__ __forceinline__ Work(const Kv4AttendCall& call, const Kv4Clients& c, const Kv4Item& it, int kvh_, int wg_tiles)
+      : a(call), kvh(kvh_), len(c.len[it.ci]), n_rows(c.n_rows[it.ci]), row_off(c.row_off[it.ci]), groups(c.groups[it.ci]),
+        nsplit(c.nsplit[it.ci]) {
+    group_rows = n_rows * a.group;
+    first_row = it.group * wg_tiles * 16;
+    group_rinv = __builtin_amdgcn_rcpf((float)a.group);
+    table = a.view.table + c.table_off[it.ci];
+    all = a.part + ((size_t)c.part_off[it.ci] + ((size_t)kvh * groups + it.group) * nsplit * wg_tiles) * (16 * ROW);
+    counter = a.counters + c.count_off[it.ci] + kvh * groups + it.group;
   }
-#pragma unroll
-  for (int m = 1; m < 16; m *= 2) lo = min(lo, __shfl_xor(lo, m)), hi = max(hi, __shfl_xor(hi, m));
-  lo = __builtin_amdgcn_readfirstlane(lo);
-  hi = __builtin_amdgcn_readfirstlane(hi);
-  const int wave_hi = hi;
-  if constexpr (WIDE) {  // all waves walk as far as one of them has to
-    if (lane == 0) last_lds[w] = hi;
-    __syncthreads();
-#pragma unroll
-    for (int ww = 0; ww < WAVES; ++ww) hi = max(hi, last_lds[ww]);
-    hi = __builtin_amdgcn_readfirstlane(hi);
-  }
-  const int end = min(min(span0 + clients.span, len), hi);
-  const int nsteps = end > first ? (end - first + STEP - 1) / STEP : 0;
+  __device__ __forceinline__ TileRow row(int rr) const { return tile_row(rr, a.group, group_rinv, n_rows, row_off, kvh); }
+  __device__ __forceinline__ int limit(const TileRow& tr) const { return row_limit(a.limits, tr.row, row_off, n_rows, len); }
 
-  f32x4 acc[TILES][HT];
-  // per row: -(running maximum) (0 while nothing has been seen), the score that moves it, the sum of weights
-  float neg_m[TILES], moves[TILES], l_run[TILES];
-#pragma unroll
-  for (int t = 0; t < TILES; ++t) {
-    neg_m[t] = 0.f;
-    moves[t] = -INFINITY;
-    l_run[t] = 0.f;
-#pragma unroll
-    for (int j = 0; j < HT; ++j) acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-  auto query = [&](int t, int piece, int st) {
-    if constexpr (Q_LDS) return __builtin_bit_cast(bf16x8, q_lds[((t * NP + piece) * NS + st) * 64]);
-    else return __builtin_bit_cast(bf16x8, q[t].q[piece][st]);
-  };
-  const LaneOffsets<HD> at(c, g);
-  const float c1 = kv4_scale<HD>();
-
-  struct Raw {
-    Codes k[2], v[2];
-    unsigned kp[2], vp[2];
-  };
-  // (Keys and values of a step travel from where those of the step before have been used until they are.)
-  constexpr int DEPTH = 1;
-  Raw raw[DEPTH];
-  Raw& r = raw[0];  // (MANY)
-  auto record = [&](int i, int tt) {
-    const unsigned lo = __builtin_amdgcn_readlane((unsigned)step_rec[tt], i & 63), hi = __builtin_amdgcn_readlane((unsigned)(step_rec[tt] >> 32), i & 63);
-    return head_base + (int64_t)(((uint64_t)hi << 32) | lo);
-  };
-  auto request_keys = [&](Raw& r, int i) {
-    if (i >= nsteps) return;
-    if (i > 0 && (i & 63) == 0) load_blocks(i);
-#pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
-      const uint8_t* rec = record(i, tt);
-      r.k[tt] = *(const Codes*)(rec + at.k);
-      r.kp[tt] = rec[at.kp];
-    }
-  };
-  auto request_values = [&](Raw& r, int i) {
-    if (i >= nsteps) return;
-#pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
-      const uint8_t* rec = record(i, tt);
-      r.v[tt] = *(const Codes*)(rec + at.v);
-      r.vp[tt] = *(const unsigned*)(rec + at.vp);
-    }
-  };
-  // MANY: this wave's part of a step is one block's keys (tt), or its values
-  k4u32x4* ops = (k4u32x4*)lds;
-  constexpr int OPS = (2 * NS + HT) * 64;  // of a step
-  auto part_of_step = [&](int i) { return (w + 2 * (i & 1)) & 3; };
-  auto request_part = [&](int i) {
-    if (i >= nsteps) return;
-    if (i > 0 && (i & 63) == 0) load_blocks(i);
-    const int part = part_of_step(i);
-    const uint8_t* rec = record(i, part & 1);
-    if (part < 2) {
-      r.k[0] = *(const Codes*)(rec + at.k);
-      r.kp[0] = rec[at.kp];
-    } else {
-      r.k[0] = *(const Codes*)(rec + at.v);
-      r.kp[0] = *(const unsigned*)(rec + at.vp);
-    }
-  };
-  auto convert_part = [&](int i) {
-    if (i >= nsteps) return;
-    const int part = part_of_step(i), tt = part & 1;
-    k4u32x4* to = ops + (i & 1) * OPS + lane;
-    if (part < 2) {
-      const float power = __uint_as_float(r.kp[0] << 23);
-#pragma unroll
-      for (int st = 0; st < NS; ++st) to[(tt * NS + st) * 64] = __builtin_bit_cast(k4u32x4, key_operand(r.k[0][st], power));
-    } else {
-      const int left = len - (first + i * STEP + tt * 16);
-      if (left < 16) drop_values<HD>(r.k[0], r.kp[0], left - g * 4);
-#pragma unroll
-      for (int b = 0; b < HT / 2; ++b) {
-        k4u32x2 even, odd;
-        value_operands<HD>(r.k[0], r.kp[0], b, even, odd);
-        ((k4u32x2*)(to + (2 * NS + 2 * b) * 64))[tt] = even;
-        ((k4u32x2*)(to + (2 * NS + 2 * b + 1) * 64))[tt] = odd;
-      }
-    }
-  };
-  if constexpr (WIDE) {
-    request_part(0);
-    convert_part(0);
-    request_part(1);
-  } else {
-#pragma unroll
-    for (int d = 0; d < DEPTH; ++d) {
-      request_keys(raw[d], d);
-      request_values(raw[d], d);
-    }
-  }
-  auto step = [&](Raw& r, int i) {
-    const int tok0 = first + i * STEP;
-    const k4u32x4* op = ops + (i & 1) * OPS + lane;
-    if constexpr (WIDE) {
-      __syncthreads();  // step i's operands are there, and those of step i - 1 have been read
-      convert_part(i + 1);
-      request_part(i + 2);
-      if (tok0 >= wave_hi) return;
-    }
-    const bool masked = tok0 + 32 > lo;  // (of the wave) some row does not see all 32 tokens
-    bf16x8 ph[TILES], pl[TILES];
-    f32x4 score[TILES][2];
-#pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
-      const float power = WIDE ? 0.f : __uint_as_float(r.kp[tt] << 23);
-#pragma unroll
-      for (int t = 0; t < TILES; ++t) score[t][tt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int st = 0; st < NS; ++st) {
-        bf16x8 k;
-        if constexpr (WIDE) k = __builtin_bit_cast(bf16x8, op[(tt * NS + st) * 64]);
-        else k = key_operand(r.k[tt][st], power);
-#pragma unroll
-        for (int m = NP - 1; m >= 0; --m)
-#pragma unroll
-          for (int t = 0; t < TILES; ++t) score[t][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, query(t, m, st), score[t][tt], 0, 0, 0);
-      }
-    }
-    settle(score);
-    if constexpr (!WIDE) request_keys(r, i + DEPTH);
-#pragma unroll
-    for (int t = 0; t < TILES; ++t) {
-      const f32x4 s0 = score[t][0], s1 = score[t][1];
-      float sc[8] = {s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]};
-      if (masked) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (tok0 + (i >> 2) * 16 + g * 4 + (i & 3) >= lim[t]) sc[i] = -INFINITY;
-      }
-      float top = max3(max3(sc[0], sc[1], sc[2]), max3(sc[3], sc[4], sc[5]), max3(sc[6], sc[7], sc[7]));
-      if (__ballot(top > moves[t]) != 0) {
-        const float m_old = moves[t] == -INFINITY ? -INFINITY : -neg_m[t];
-        const float m_new = fmaxf(m_old, fold_groups(top, LaneMax{}) * c1);
-        const float alpha = m_new == m_old ? 1.f : __builtin_amdgcn_exp2f(m_old - m_new);
-        if (m_new != -INFINITY) {
-          neg_m[t] = -m_new;
-          moves[t] = (m_new + 8.f) * (1.f / c1);
-        }
-        l_run[t] *= alpha;
-#pragma unroll
-        for (int j = 0; j < HT; ++j) acc[t][j] *= alpha;
-      }
-      float p[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c1, neg_m[t]));
-      l_run[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-      unsigned h[4], l[4];
-      split_weights(p, h, l);
-      ph[t] = __builtin_bit_cast(bf16x8, k4u32x4{h[0], h[1], h[2], h[3]});
-      pl[t] = __builtin_bit_cast(bf16x8, k4u32x4{l[0], l[1], l[2], l[3]});
-    }
-    if (!WIDE && masked) {
-#pragma unroll
-      for (int tt = 0; tt < 2; ++tt) drop_values<HD>(r.v[tt], r.vp[tt], len - (tok0 + tt * 16 + g * 4));
-    }
-#pragma unroll
-    for (int b = 0; b < HT / 2; ++b) {
-      bf16x8 even, odd;
-      if constexpr (WIDE) {
-        even = __builtin_bit_cast(bf16x8, op[(2 * NS + 2 * b) * 64]);
-        odd = __builtin_bit_cast(bf16x8, op[(2 * NS + 2 * b + 1) * 64]);
-      } else {
-        k4u32x2 even2[2], odd2[2];
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt) value_operands<HD>(r.v[tt], r.vp[tt], b, even2[tt], odd2[tt]);
-        even = both_blocks(even2);
-        odd = both_blocks(odd2);
-      }
-#pragma unroll
-      for (int t = 0; t < TILES; ++t) {
-        acc[t][2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, ph[t], acc[t][2 * b], 0, 0, 0);
-        acc[t][2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, ph[t], acc[t][2 * b + 1], 0, 0, 0);
-        acc[t][2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, pl[t], acc[t][2 * b], 0, 0, 0);
-        acc[t][2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, pl[t], acc[t][2 * b + 1], 0, 0, 0);
-      }
-    }
-    settle(acc);
-    if constexpr (!WIDE) request_values(r, i + DEPTH);
-  };
-  for (int i = 0; i < nsteps; i += DEPTH)
-#pragma unroll
-    for (int d = 0; d < DEPTH; ++d)
-      if (i + d < nsteps) step(raw[d], i + d);
-#pragma unroll
-  for (int t = 0; t < TILES; ++t) l_run[t] = fold_groups(l_run[t], LaneAdd{});
-  auto maximum = [&](int t) { return moves[t] == -INFINITY ? -INFINITY : -neg_m[t]; };
-
-  // ---- what leaves the workgroup: rows, or a split's partial rows (written through) ----
-  float* all = a.part + ((size_t)clients.part_off[it.ci] + ((size_t)kvh * groups + it.group) * nsplit * WG_TILES) * (16 * ROW);
-  float* part = all + (size_t)it.split * WG_TILES * 16 * ROW;
-  auto finish = [&](int rr, int e0, const f32x4& o, float m, float l) {  // 4 channels of a row
-    const TileRow tr = tile_row(rr, group, group_rinv, n_rows, row_off, kvh);
+  // 4 channels of a row: o / l, and once a row what launch_kv4_mass needs
+  __device__ __forceinline__ void finish(int rr, int e0, const f32x4& o, float m, float l) const {
+    const TileRow tr = row(rr);
     if (!tr.live) return;
     float inv = __builtin_amdgcn_rcpf(l);
     inv = l == 0.f ? 0.f : inv * (2.f - l * inv);
@@ -523,190 +247,696 @@ __global__ __launch_bounds__(WAVES * 64, (attend_waves_per_simd<HD, T, TILES, WI
     if constexpr (sizeof(T) == 4) *(f32x4*)out = y;
     else *(uint2*)out = make_uint2(pack2_bf16(y[0], y[1]), pack2_bf16(y[2], y[3]));
     if (a.lse && e0 == 0) a.lse[(size_t)tr.row * a.n_q_heads + tr.head] = l == 0.f ? INFINITY : m + __builtin_amdgcn_logf(l);
-  };
-  if constexpr (WIDE) {
-#pragma unroll
-    for (int t = 0; t < TILES; ++t) {
-      if ((tile0 + t) * 16 >= R) break;
-      const float m = maximum(t);
-      float* dst = part + ((size_t)(w * TILES + t) * 16 + c) * ROW;
-      // lane (c, g): channels (4 g + i) * HT + j of row c
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < HT; j += 4) {
-          const int ch = (4 * g + i) * HT + j;
-          const f32x4 o = f32x4{acc[t][j][i], acc[t][j + 1][i], acc[t][j + 2][i], acc[t][j + 3][i]};
-          if (nsplit == 1) finish((tile0 + t) * 16 + c, ch, o, m, l_run[t]);
-          else if (wave_hi > first) Xwg<true>::st4f(dst + ch, o);  // (nothing seen: nothing to read)
-        }
-      if (nsplit > 1 && g == 0) Xwg<true>::st4f(dst + HD, f32x4{m, l_run[t], 0.f, 0.f});
-    }
-  } else {
-    float(*states)[WAVES][16][ROW] = (float(*)[WAVES][16][ROW])lds;  // a row: its channels, its maximum and sum
-#pragma unroll
-    for (int t = 0; t < TILES; ++t) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < HT; j += 4)
-          *(f32x4*)&states[t][w][c][(4 * g + i) * HT + j] = f32x4{acc[t][j][i], acc[t][j + 1][i], acc[t][j + 2][i], acc[t][j + 3][i]};
-      if (g == 0) *(f32x2*)&states[t][w][c][HD] = f32x2{maximum(t), l_run[t]};
-    }
-    __syncthreads();
-    const int live = min(WG_TILES * 16, R - tile0 * 16) * (HD / 4);
-#pragma unroll 1
-    for (int k = tid; k < live; k += WAVES * 64) {  // (row, 4 channels)
-      const int mr = k / (HD / 4), e0 = (k % (HD / 4)) * 4;
-      const float(*rows)[16][ROW] = states[mr / 16];
-      f32x2 ml[WAVES];
-      float m = -INFINITY;
-#pragma unroll
-      for (int ww = 0; ww < WAVES; ++ww) {
-        ml[ww] = *(const f32x2*)&rows[ww][mr % 16][HD];
-        m = fmaxf(m, ml[ww].x);
-      }
-      const float m_ref = m == -INFINITY ? 0.f : m;
-      float l = 0.f;
-      f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int ww = 0; ww < WAVES; ++ww) {
-        const float sw = __builtin_amdgcn_exp2f(ml[ww].x - m_ref);
-        l += ml[ww].y * sw;
-        o += *(const f32x4*)&rows[ww][mr % 16][e0] * sw;
-      }
-      if (nsplit == 1) {
-        finish(tile0 * 16 + mr, e0, o, m, l);
-      } else {
-        float* dst = part + (size_t)mr * ROW;
-        Xwg<true>::st4f(dst + e0, o);
-        if (e0 == 0) Xwg<true>::st4f(dst + HD, f32x4{m, l, 0.f, 0.f});
-      }
-    }
   }
-  if (nsplit == 1) return;
 
-  // ---- count in; the last of the splits to arrive joins them ----
-  Xwg<true>::drain();
-  __syncthreads();
-  if (tid == 0) {
-    unsigned* counter = a.counters + clients.count_off[it.ci] + kvh * groups + it.group;
-    const unsigned prev = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const int last = prev == (unsigned)nsplit - 1u;
-    if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // ready for the next launch
-    *last_lds = last;
+  // The partial rows have been written through; whoever of the splits arrives last joins them.  All threads of the workgroup.
+  __device__ __forceinline__ bool arrives_last(int* word) const {
+    Xwg<true>::drain();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      const unsigned prev = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      const int last = prev == (unsigned)nsplit - 1u;
+      if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // ready for the next launch
+      *word = last;
+    }
+    __syncthreads();
+    return *word != 0;
+  }
+};
+
+// The running softmax of a tile of 16 query rows: its state, per row (lane's column), and a step's weights.
+template <int HT>
+struct Running {
+  f32x4 acc[HT];  // O^T
+  // -(running maximum) (0 while nothing has been seen), the score that moves it, the lane's own sum of weights
+  float neg_m, moves, l;
+
+  __device__ __forceinline__ void clear() {
+    neg_m = 0.f;
+    moves = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int j = 0; j < HT; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  __device__ __forceinline__ float maximum() const { return moves == -INFINITY ? -INFINITY : -neg_m; }
+  // The maximum moves only when a score passes it by 2^8 (any scale will do for fp32 sums: most steps then need no exchange
+  // between lanes and no rescaling).
+  __device__ __forceinline__ void move_to(float top, float c1) {  // all lanes
+    const float m_old = maximum(), m_new = fmaxf(m_old, fold_groups(top, LaneMax{}) * c1);
+    const float alpha = m_new == m_old ? 1.f : __builtin_amdgcn_exp2f(m_old - m_new);
+    if (m_new != -INFINITY) {
+      neg_m = -m_new;
+      moves = (m_new + 8.f) * (1.f / c1);
+    }
+    l *= alpha;
+#pragma unroll
+    for (int j = 0; j < HT; ++j) acc[j] *= alpha;
+  }
+  __device__ __forceinline__ void weights(const float (&sc)[8], float c1, bf16x8& hi, bf16x8& lo) {
+    float p[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c1, neg_m));
+    l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+    unsigned h[4], r[4];
+    split_weights(p, h, r);
+    hi = __builtin_bit_cast(bf16x8, k4u32x4{h[0], h[1], h[2], h[3]});
+    lo = __builtin_bit_cast(bf16x8, k4u32x4{r[0], r[1], r[2], r[3]});
+  }
+};
+__device__ __forceinline__ float top_of(const float (&sc)[8]) {
+  return max3(max3(sc[0], sc[1], sc[2]), max3(sc[3], sc[4], sc[5]), max3(sc[6], sc[7], sc[7]));
+}
+__device__ __forceinline__ void hide(float (&sc)[8], int tok, int lim) {  // tok: the lane's first token of the first block
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (tok + (i >> 2) * 16 + (i & 3) >= lim) sc[i] = -INFINITY;
+}
+template <int N, int HT>
+__device__ __forceinline__ void settle(Running<HT> (&x)[N]) {
+  f32x4 acc[N][HT];
+#pragma unroll
+  for (int t = 0; t < N; ++t)
+#pragma unroll
+    for (int j = 0; j < HT; ++j) acc[t][j] = x[t].acc[j];
+  settle(acc);
+#pragma unroll
+  for (int t = 0; t < N; ++t)
+#pragma unroll
+    for (int j = 0; j < HT; ++j) x[t].acc[j] = acc[t][j];
+}
+
+// ---- few tiles: the waves share them, take every WAVES-th 32 tokens of the span and join their states through LDS at the end ----
+// LDS: states [tile][wave][row], later what joins the splits; then the queries that registers do not hold; words
+template <int HD, int TILES, int WAVES>
+constexpr size_t state_floats() { return (size_t)TILES * WAVES * 16 * (HD + kKv4PartPad); }
+template <int HD, typename T, int TILES>
+constexpr bool queries_in_lds() { return TILES * pieces<T>() * (HD / 8) > 32; }
+template <int HD, typename T, int TILES, int WAVES>
+constexpr size_t few_lds_bytes() {
+  return state_floats<HD, TILES, WAVES>() * sizeof(float) + (queries_in_lds<HD, T, TILES>() ? (size_t)TILES * pieces<T>() * (HD / 32) * 1024 : 0) + 16;
+}
+
+template <int HD, typename T, int TILES, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, TILES == 1 ? 4 : 2) void kv4_attend_kernel(Kv4AttendCall a, Kv4Clients clients) {
+  constexpr int NP = pieces<T>(), NS = HD / 32, HT = HD / 16, ROW = HD + kKv4PartPad, STEP = WAVES * 32;
+  constexpr bool Q_LDS = queries_in_lds<HD, T, TILES>();
+  typedef typename std::conditional<HD == 128, k4u32x4, k4u32x2>::type Codes;
+  extern __shared__ float lds[];
+  int* word = (int*)((char*)lds + few_lds_bytes<HD, T, TILES, WAVES>() - 16);
+
+  const int kvh = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c = lane & 15, g = lane >> 4;
+  const Kv4Item it = find_item(clients, blockIdx.y, lane);
+  const Work<HD, T> wk(a, clients, it, kvh, TILES);
+  const int len = wk.len, span0 = it.split * clients.span, first = span0 + w * 32;
+
+  // the records of 64 steps' blocks sit in the lanes: lane L has where the two of step L begin
+  int64_t step_rec[2];
+  const int64_t block_bytes = (int64_t)a.view.n_kv_heads * Kv4Record<HD>::kBytes;
+  const uint8_t* head_base = a.view.pool + (int64_t)a.layer * a.view.n_blocks * block_bytes + kvh * Kv4Record<HD>::kBytes;
+  auto load_blocks = [&](int it0) {
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) {
+      const int64_t tok = (int64_t)first + (int64_t)(it0 + lane) * STEP + tt * 16;
+      step_rec[tt] = wk.table[tok < len ? (int)(tok / kBlockTokens) : 0] * block_bytes;
+    }
+  };
+  load_blocks(0);
+
+  // ---- queries, and how far each row sees ----
+  // (in registers, or where the sums leave no room for them in LDS: [tile][piece][step][lane])
+  k4u32x4 q[Q_LDS ? 1 : TILES][NP][NS];
+  k4u32x4* q_lds = (k4u32x4*)(lds + state_floats<HD, TILES, WAVES>()) + lane;
+  int lim[TILES];
+  int lo = len, hi = 0;
+#pragma unroll
+  for (int t = 0; t < TILES; ++t) {
+    const TileRow tr = wk.row(wk.first_row + t * 16 + c);
+    load_queries<NP, NS>((const T*)a.q + tr.row * a.q_stride + tr.head * HD + g * (HD / 4), tr.live, q[Q_LDS ? 0 : t]);
+    if constexpr (Q_LDS) {  // (the waves write the same)
+#pragma unroll
+      for (int i = 0; i < NP * NS; ++i) q_lds[(t * NP * NS + i) * 64] = q[0][i / NS][i % NS];
+    }
+    lim[t] = wk.limit(tr);
+    if (tr.live) lo = min(lo, lim[t]), hi = max(hi, lim[t]);
+  }
+#pragma unroll
+  for (int m = 1; m < 16; m *= 2) lo = min(lo, __shfl_xor(lo, m)), hi = max(hi, __shfl_xor(hi, m));
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  hi = __builtin_amdgcn_readfirstlane(hi);
+  const int end = min(min(span0 + clients.span, len), hi);
+  const int nsteps = end > first ? (end - first + STEP - 1) / STEP : 0;
+  auto query = [&](int t, int piece, int st) {
+    if constexpr (Q_LDS) return __builtin_bit_cast(bf16x8, q_lds[((t * NP + piece) * NS + st) * 64]);
+    else return __builtin_bit_cast(bf16x8, q[t][piece][st]);
+  };
+
+  Running<HT> run[TILES];
+#pragma unroll
+  for (int t = 0; t < TILES; ++t) run[t].clear();
+  const LaneOffsets<HD> at(c, g);
+  const float c1 = kv4_scale<HD>();
+
+  // (Keys and values of a step travel from where those of the step before have been used until they are.)
+  Codes k[2], v[2];
+  unsigned kp[2], vp[2];
+  auto record = [&](int i, int tt) {
+    const unsigned lo = __builtin_amdgcn_readlane((unsigned)step_rec[tt], i & 63), hi = __builtin_amdgcn_readlane((unsigned)(step_rec[tt] >> 32), i & 63);
+    return head_base + (int64_t)(((uint64_t)hi << 32) | lo);
+  };
+  auto request_keys = [&](int i) {
+    if (i >= nsteps) return;
+    if (i > 0 && (i & 63) == 0) load_blocks(i);
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) {
+      const uint8_t* rec = record(i, tt);
+      k[tt] = *(const Codes*)(rec + at.k);
+      kp[tt] = rec[at.kp];
+    }
+  };
+  auto request_values = [&](int i) {
+    if (i >= nsteps) return;
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) {
+      const uint8_t* rec = record(i, tt);
+      v[tt] = *(const Codes*)(rec + at.v);
+      vp[tt] = *(const unsigned*)(rec + at.vp);
+    }
+  };
+  request_keys(0);
+  request_values(0);
+  for (int i = 0; i < nsteps; ++i) {
+    const int tok0 = first + i * STEP;
+    const bool masked = tok0 + 32 > lo;  // (of the wave) some row does not see all 32 tokens
+    f32x4 score[TILES][2];
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) {
+      const float power = __uint_as_float(kp[tt] << 23);
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) score[t][tt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int st = 0; st < NS; ++st) {
+        const bf16x8 key = key_operand(k[tt][st], power);
+#pragma unroll
+        for (int m = NP - 1; m >= 0; --m)
+#pragma unroll
+          for (int t = 0; t < TILES; ++t) score[t][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, query(t, m, st), score[t][tt], 0, 0, 0);
+      }
+    }
+    settle(score);
+    request_keys(i + 1);
+    bf16x8 ph[TILES], pl[TILES];
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) {
+      const f32x4 s0 = score[t][0], s1 = score[t][1];
+      float sc[8] = {s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]};
+      if (masked) hide(sc, tok0 + g * 4, lim[t]);
+      const float top = top_of(sc);
+      if (__ballot(top > run[t].moves) != 0) run[t].move_to(top, c1);
+      run[t].weights(sc, c1, ph[t], pl[t]);
+    }
+    if (masked) {
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) drop_values<HD>(v[tt], vp[tt], len - (tok0 + tt * 16 + g * 4));
+    }
+#pragma unroll
+    for (int b = 0; b < HT / 2; ++b) {
+      k4u32x2 even2[2], odd2[2];
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) value_operands<HD>(v[tt], vp[tt], b, even2[tt], odd2[tt]);
+      const bf16x8 even = both_blocks(even2), odd = both_blocks(odd2);
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) {
+        f32x4& x = run[t].acc[2 * b];
+        f32x4& y = run[t].acc[2 * b + 1];
+        x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, ph[t], x, 0, 0, 0);
+        y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, ph[t], y, 0, 0, 0);
+        x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, pl[t], x, 0, 0, 0);
+        y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, pl[t], y, 0, 0, 0);
+      }
+    }
+    settle(run);
+    request_values(i + 1);
+  }
+
+  // ---- the waves' states joined: rows, or a split's partial rows (written through) ----
+  constexpr int ROWS = TILES * 16, TPR = HD / 4, NT = WAVES * 64;
+  const int rows_here = min(ROWS, wk.group_rows - wk.first_row), tasks = rows_here * TPR;  // a task: (row, 4 channels)
+  float(*states)[WAVES][16][ROW] = (float(*)[WAVES][16][ROW])lds;  // a row: its channels, its maximum and sum
+#pragma unroll
+  for (int t = 0; t < TILES; ++t) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < HT; j += 4)
+        *(f32x4*)&states[t][w][c][(4 * g + i) * HT + j] = f32x4{run[t].acc[j][i], run[t].acc[j + 1][i], run[t].acc[j + 2][i], run[t].acc[j + 3][i]};
+    const float l = fold_groups(run[t].l, LaneAdd{});
+    if (g == 0) *(f32x2*)&states[t][w][c][HD] = f32x2{run[t].maximum(), l};
   }
   __syncthreads();
-  if (*last_lds == 0) return;
-  const size_t split_stride = (size_t)WG_TILES * 16 * ROW;
-  constexpr int TPR = HD / 4, NT = WAVES * 64;
-  const int rows_here = min(WG_TILES * 16, R - it.group * WG_TILES * 16), tasks = rows_here * TPR;
-  if constexpr (!WIDE) {
-    // The maxima and sums of all (split, row) come to LDS at once; each thread then has 4 channels of a row, or of several
-    // one after the other, and takes its splits 8 at a time.  Threads that the rows leave over share the splits of a row:
-    // thread (share, row, 4 channels) takes splits share, share + shares, .., and the shares are joined through LDS in order.
-    constexpr int BATCH = 8, ROWS = WG_TILES * 16;
-    static_assert(2 * kKv4MaxSplits * ROWS + NT * 5 <= (int)state_floats<HD, TILES, WAVES, WIDE>(), "maxima, sums and shares fit the states' LDS");
-    f32x2* stats = (f32x2*)lds;                           // [split][row]
-    float* joined = lds + 2 * kKv4MaxSplits * ROWS;       // [share][row, 4 channels] 4 sums, the sum of weights
-    for (int i = tid; i < nsplit * ROWS; i += NT)
-      if (i % ROWS < rows_here) stats[i] = *(const f32x2*)(all + (size_t)i * ROW + HD);
-    int log_tasks = 31 - __builtin_clz(TPR);  // (rows made a power of two)
-    while ((1 << log_tasks) < tasks) ++log_tasks;
-    const int shares = max(1, NT >> log_tasks);
-    __syncthreads();
 #pragma unroll 1
-    for (int k0 = 0; k0 < tasks; k0 += NT) {
-      const int k = k0 + (tid & ((1 << log_tasks) - 1)), share = tid >> log_tasks;
-      const int mr = min(k / TPR, rows_here - 1), e0 = (k % TPR) * 4;
-      const float* p0 = all + (size_t)mr * ROW + e0;
-      float m = -INFINITY, l = 0.f;
+  for (int task = tid; task < tasks; task += NT) {
+    const int mr = task / TPR, e0 = (task % TPR) * 4;
+    const float(*rows)[16][ROW] = states[mr / 16];
+    f32x2 ml[WAVES];
+    float m = -INFINITY;
+#pragma unroll
+    for (int ww = 0; ww < WAVES; ++ww) {
+      ml[ww] = *(const f32x2*)&rows[ww][mr % 16][HD];
+      m = fmaxf(m, ml[ww].x);
+    }
+    const float m_ref = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ww = 0; ww < WAVES; ++ww) {
+      const float sw = __builtin_amdgcn_exp2f(ml[ww].x - m_ref);
+      l += ml[ww].y * sw;
+      o += *(const f32x4*)&rows[ww][mr % 16][e0] * sw;
+    }
+    if (wk.nsplit == 1) {
+      wk.finish(wk.first_row + mr, e0, o, m, l);
+    } else {
+      float* dst = wk.all + ((size_t)it.split * ROWS + mr) * ROW;
+      Xwg<true>::st4f(dst + e0, o);
+      if (e0 == 0) Xwg<true>::st4f(dst + HD, f32x4{m, l, 0.f, 0.f});
+    }
+  }
+  if (wk.nsplit == 1 || !wk.arrives_last(word)) return;
+
+  // ---- the splits joined ----
+  // Their maxima and sums come to LDS at once; each thread then has a task, or several one after the other, and takes its
+  // splits 8 at a time.  Threads that the tasks leave over share the splits of a task: thread (share, task) takes splits
+  // share, share + shares, .., and the shares are joined through LDS in order.
+  constexpr int BATCH = 8;
+  static_assert(2 * kKv4MaxSplits * ROWS + NT * 5 <= (int)state_floats<HD, TILES, WAVES>(), "maxima, sums and shares fit the states' LDS");
+  f32x2* stats = (f32x2*)lds;                      // [split][row]
+  float* joined = lds + 2 * kKv4MaxSplits * ROWS;  // [share][task] 4 sums, the sum of weights
+  for (int i = tid; i < wk.nsplit * ROWS; i += NT)
+    if (i % ROWS < rows_here) stats[i] = *(const f32x2*)(wk.all + (size_t)i * ROW + HD);
+  int log_tasks = 31 - __builtin_clz(TPR);  // (their number made a power of two)
+  while ((1 << log_tasks) < tasks) ++log_tasks;
+  const int shares = max(1, NT >> log_tasks);
+  __syncthreads();
+#pragma unroll 1
+  for (int k0 = 0; k0 < tasks; k0 += NT) {
+    const int task = k0 + (tid & ((1 << log_tasks) - 1)), share = tid >> log_tasks;
+    const int mr = min(task / TPR, rows_here - 1), e0 = (task % TPR) * 4;
+    const float* p0 = wk.all + (size_t)mr * ROW + e0;
+    float m = -INFINITY, l = 0.f;
 #pragma unroll 4
-      for (int sp = 0; sp < nsplit; ++sp) m = fmaxf(m, stats[sp * ROWS + mr].x);
-      f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int sp = 0; sp < wk.nsplit; ++sp) m = fmaxf(m, stats[sp * ROWS + mr].x);
+    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
-      for (int s0 = share; s0 < nsplit; s0 += BATCH * shares) {
-        f32x4 ob[BATCH];
+    for (int s0 = share; s0 < wk.nsplit; s0 += BATCH * shares) {
+      f32x4 ob[BATCH];
 #pragma unroll
-        for (int j = 0; j < BATCH; ++j) ob[j] = *(const f32x4*)(p0 + min(s0 + j * shares, nsplit - 1) * split_stride);
+      for (int j = 0; j < BATCH; ++j) ob[j] = *(const f32x4*)(p0 + (size_t)min(s0 + j * shares, wk.nsplit - 1) * (ROWS * ROW));
 #pragma unroll
-        for (int j = 0; j < BATCH; ++j) {
-          const int sp = s0 + j * shares;
-          const f32x2 ml = stats[min(sp, nsplit - 1) * ROWS + mr];
-          const float sw = sp < nsplit && ml.x != -INFINITY ? __builtin_amdgcn_exp2f(ml.x - m) : 0.f;
-          l += ml.y * sw;
-          o += ob[j] * sw;
-        }
+      for (int j = 0; j < BATCH; ++j) {
+        const int sp = s0 + j * shares;
+        const f32x2 ml = stats[min(sp, wk.nsplit - 1) * ROWS + mr];
+        const float sw = sp < wk.nsplit && ml.x != -INFINITY ? __builtin_amdgcn_exp2f(ml.x - m) : 0.f;
+        l += ml.y * sw;
+        o += ob[j] * sw;
       }
-      if (shares > 1) {
-        float* x = joined + (size_t)tid * 5;
-        x[0] = o[0], x[1] = o[1], x[2] = o[2], x[3] = o[3], x[4] = l;
-        __syncthreads();
-        if (share == 0)
-          for (int sh = 1; sh < shares; ++sh) {
-            const float* y = joined + (size_t)((sh << log_tasks) + tid) * 5;
-            o += f32x4{y[0], y[1], y[2], y[3]};
-            l += y[4];
-          }
-      }
-      if (share == 0 && k < tasks) finish(it.group * WG_TILES * 16 + mr, e0, o, m, l);
     }
-  } else {
-    constexpr int BATCH = 8;
-    for (int k = tid; k < tasks; k += NT) {
-      const int mr = k / TPR, e0 = (k % TPR) * 4;
-      const float* p0 = all + (size_t)mr * ROW;
-      float m = -INFINITY, l = 0.f;
-      f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-      for (int s0 = 0; s0 < nsplit; s0 += BATCH) {
-        f32x4 ob[BATCH];
-        f32x2 ml[BATCH];
-#pragma unroll
-        for (int j = 0; j < BATCH; ++j) {
-          const float* ps = p0 + min(s0 + j, nsplit - 1) * split_stride;
-          ml[j] = *(const f32x2*)(ps + HD);
-          ob[j] = *(const f32x4*)(ps + e0);
+    if (shares > 1) {
+      float* x = joined + (size_t)tid * 5;
+      x[0] = o[0], x[1] = o[1], x[2] = o[2], x[3] = o[3], x[4] = l;
+      __syncthreads();
+      if (share == 0)
+        for (int sh = 1; sh < shares; ++sh) {
+          const float* y = joined + (size_t)((sh << log_tasks) + tid) * 5;
+          o += f32x4{y[0], y[1], y[2], y[3]};
+          l += y[4];
         }
-        float m_new = m;
-#pragma unroll
-        for (int j = 0; j < BATCH; ++j)
-          if (s0 + j < nsplit) m_new = fmaxf(m_new, ml[j].x);
-        if (m_new == -INFINITY) continue;
-        const float alpha = __builtin_amdgcn_exp2f(m - m_new);
-        l *= alpha;
-        o *= alpha;
-        m = m_new;
-#pragma unroll
-        for (int j = 0; j < BATCH; ++j) {
-          if (s0 + j >= nsplit || ml[j].x == -INFINITY) continue;  // (a split that saw nothing wrote no values)
-          const float sw = __builtin_amdgcn_exp2f(ml[j].x - m);
-          l += ml[j].y * sw;
-          o += ob[j] * sw;
-        }
-      }
-      finish(it.group * WG_TILES * 16 + mr, e0, o, m, l);
     }
+    if (share == 0 && task < tasks) wk.finish(wk.first_row + mr, e0, o, m, l);
   }
 }
 
-template <int HD, typename T, int TILES, int WAVES, bool WIDE>
-static hipError_t attend_kernel(const Kv4AttendCall& c, const Kv4Clients& cl, hipStream_t st) {
-  constexpr size_t lds = attend_lds_bytes<HD, T, TILES, WAVES, WIDE>();
-  if constexpr (lds > 64 * 1024) {
-    static std::atomic<uint64_t> allowed{0};
-    const hipError_t e = allow_lds(allowed, (const void*)kv4_attend_kernel<HD, T, TILES, WAVES, WIDE>, lds);
+// ---- many rows: each of four waves has 32 or 64 of its own ----
+// Keys and values are converted once, a block by each wave, into operands in LDS that all read; one barrier for 64 tokens.  Products of 32 x 32: what a wave may issue is the bound, 8 cycles a product of either
+// size beside 4 to 5 an instruction of the vector unit.  The values of a step of 32 tokens are multiplied one step later, so
+// that those products, which depend on nothing of the step, travel with the weights' instructions.
+// Layout of a 32 x 32 x 16 product: operand lane (r, h) holds row (column) r, k = 8 h .. + 7; the result's register 4 u + i holds
+// row 8 u + 4 h + i of column r.  Scores: k is channel h * HD / 2 + 8 s .. of step s.  Values: row r of product j is channel
+// r * HD / 32 + j, and k the tokens 4 h .. + 3 and 8 + 4 h .. + 3 of a block, which is how the weights lie.
+// LDS: keys [2 times 64 tokens][2 steps][HD / 16][lane], values [3 times 64 tokens][2 steps][HD / 32][block][lane]: at head
+// dim 128 half of a compute unit's, to the byte (before and behind the walk it holds a few words)
+template <int HD>
+constexpr size_t many_lds_bytes() { return (size_t)10 * (HD / 16) * 64 * 16; }
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+
+template <int HD, typename T, int TILES>
+__global__ __launch_bounds__(kKv4WideWaves * 64, 2) void kv4_attend_many_kernel(Kv4AttendCall a, Kv4Clients clients) {
+  constexpr int NP = pieces<T>(), KS = HD / 16, HT = HD / 32, ROW = HD + kKv4PartPad, WAVES = kKv4WideWaves, WG_ROWS = WAVES * TILES * 32;
+  typedef typename std::conditional<HD == 128, k4u32x4, k4u32x2>::type Codes;
+  extern __shared__ float lds[];
+  k4u32x4* key_lds = (k4u32x4*)lds;
+  k4u32x4* value_lds = key_lds + 4 * KS * 64;
+  int* word = (int*)lds;
+
+  const int kvh = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c = lane & 15, g = lane >> 4, col = lane & 31, half = lane >> 5;
+  const Kv4Item it = find_item(clients, blockIdx.y, lane);
+  const Work<HD, T> wk(a, clients, it, kvh, WG_ROWS / 16);
+  const int len = wk.len, span0 = it.split * clients.span;
+
+  // the wave converts every fourth block: the records of its next 64 sit in the lanes
+  int64_t my_rec;
+  const int64_t block_bytes = (int64_t)a.view.n_kv_heads * Kv4Record<HD>::kBytes;
+  const uint8_t* head_base = a.view.pool + (int64_t)a.layer * a.view.n_blocks * block_bytes + kvh * Kv4Record<HD>::kBytes;
+  auto load_blocks = [&](int it0) {
+    const int64_t tok = (int64_t)span0 + (int64_t)(it0 + lane) * 64 + w * 16;
+    my_rec = wk.table[tok < len ? (int)(tok / kBlockTokens) : 0] * block_bytes;
+  };
+  load_blocks(0);
+
+  // ---- queries, and how far each row sees ----
+  k4u32x4 q[TILES][NP][KS];
+  int lim[TILES];
+  int lo = len, hi = 0;
+  const int row0 = wk.first_row + w * TILES * 32;
+#pragma unroll
+  for (int t = 0; t < TILES; ++t) {
+    const TileRow tr = wk.row(row0 + t * 32 + col);
+    load_queries<NP, KS>((const T*)a.q + tr.row * a.q_stride + tr.head * HD + half * (HD / 2), tr.live, q[t]);
+    lim[t] = wk.limit(tr);
+    if (tr.live) lo = min(lo, lim[t]), hi = max(hi, lim[t]);
+  }
+#pragma unroll
+  for (int m = 1; m < 32; m *= 2) lo = min(lo, __shfl_xor(lo, m)), hi = max(hi, __shfl_xor(hi, m));
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  hi = __builtin_amdgcn_readfirstlane(hi);
+  auto steps_to = [&](int seen) {
+    const int end = min(min(span0 + clients.span, len), seen);
+    return end > span0 ? (end - span0 + 31) / 32 : 0;
+  };
+  const int my_steps = steps_to(hi);
+  if (lane == 0) word[w] = hi;  // all waves walk as far as one of them has to
+  __syncthreads();
+#pragma unroll
+  for (int ww = 0; ww < WAVES; ++ww) hi = max(hi, word[ww]);
+  const int rounds = (steps_to(__builtin_amdgcn_readfirstlane(hi)) + 1) / 2;  // of 64 tokens
+  __syncthreads();
+
+  // O^T; per row: -(running maximum) (infinity while nothing has been seen), the lane's own sum of weights
+  f32x16 acc[TILES][HT];
+  float neg_m[TILES], sum[TILES];
+#pragma unroll
+  for (int t = 0; t < TILES; ++t) {
+    neg_m[t] = INFINITY;
+    sum[t] = 0.f;
+#pragma unroll
+    for (int j = 0; j < HT; ++j) acc[t][j] = f32x16{};
+  }
+  const LaneOffsets<HD> at(c, g);
+  const float c1 = kv4_scale<HD>();
+
+  // ---- this wave's block of a round ----
+  Codes k_raw, v_raw;
+  unsigned k_pow, v_pow;
+  auto request = [&](int i) {
+    if (i >= rounds) return;
+    if (i > 0 && (i & 63) == 0) load_blocks(i);
+    const unsigned lo = __builtin_amdgcn_readlane((unsigned)my_rec, i & 63), hi = __builtin_amdgcn_readlane((unsigned)(my_rec >> 32), i & 63);
+    const uint8_t* rec = head_base + (int64_t)(((uint64_t)hi << 32) | lo);
+    k_raw = *(const Codes*)(rec + at.k);
+    v_raw = *(const Codes*)(rec + at.v);
+    k_pow = rec[at.kp];
+    v_pow = *(const unsigned*)(rec + at.vp);
+  };
+  auto convert = [&](int i, int value_buf) {
+    if (i >= rounds) return;
+    const int tt = w & 1, st0 = w >> 1;  // block of a step, step of the round
+    {  // lane (token c, quarter g): channels g * HD / 4 + 8 st .. + 7
+      k4u32x4* to = key_lds + (((i & 1) * 2 + st0) * KS + (g & 1) * (KS / 2)) * 64 + (g >> 1) * 32 + tt * 16 + c;
+      const float power = __uint_as_float(k_pow << 23);
+#pragma unroll
+      for (int st = 0; st < KS / 2; ++st) to[st * 64] = __builtin_bit_cast(k4u32x4, key_operand(k_raw[st], power));
+    }
+    {  // lane (unit c, quarter g): channels c * HD / 16 .. of tokens 4 g .. + 3
+      const int left = len - (span0 + i * 64 + w * 16);
+      if (left < 16) drop_values<HD>(v_raw, v_pow, left - g * 4);
+      k4u32x2* to = (k4u32x2*)(value_lds + ((value_buf * 2 + st0) * HT * 2 + tt) * 64 + (g & 1) * 32 + 2 * c) + (g >> 1);
+#pragma unroll
+      for (int b = 0; b < HD / 32; ++b) {  // channels 2 b and 2 b + 1 of the unit: of row 2 c, then of row 2 c + 1
+        k4u32x2 even, odd;
+        value_operands<HD>(v_raw, v_pow, b, even, odd);
+        const int ch = 2 * b;
+        to[((ch % HT) * 2 * 64 + ch / HT) * 2] = even;
+        to[(((ch + 1) % HT) * 2 * 64 + (ch + 1) / HT) * 2] = odd;
+      }
+    }
+  };
+
+  bf16x8 ph[TILES][2], pl[TILES][2];  // the step before's weights, not yet multiplied
+#pragma unroll
+  for (int t = 0; t < TILES; ++t)
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) ph[t][tt] = pl[t][tt] = __builtin_bit_cast(bf16x8, k4u32x4{0u, 0u, 0u, 0u});
+  auto multiply = [&](int at_step) {  // (place of the step in the ring of values)
+    const k4u32x4* from = value_lds + at_step * HT * 2 * 64 + lane;
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+      for (int j = 0; j < HT; ++j) {
+        const bf16x8 value = __builtin_bit_cast(bf16x8, from[(j * 2 + tt) * 64]);
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) {
+          acc[t][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value, ph[t][tt], acc[t][j], 0, 0, 0);
+          acc[t][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value, pl[t][tt], acc[t][j], 0, 0, 0);
+        }
+      }
+  };
+  // a step's weights, as two sets of operands each, and the lane's sum of them
+  auto weights = [&](const float (&sc)[16], float neg, bf16x8 (&h)[2], bf16x8 (&l)[2]) {
+    float total = 0.f;
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) {
+      float p[8];
+      unsigned hw[4], lw[4];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(sc[tt * 8 + i], c1, neg));
+      total += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+      split_weights(p, hw, lw);
+      h[tt] = __builtin_bit_cast(bf16x8, k4u32x4{hw[0], hw[1], hw[2], hw[3]});
+      l[tt] = __builtin_bit_cast(bf16x8, k4u32x4{lw[0], lw[1], lw[2], lw[3]});
+    }
+    return total;
+  };
+
+  request(0);
+  convert(0, 0);
+  request(1);
+  int place = 0;  // of step n in the ring of 6
+  auto step = [&](int n) {
+    const int last = n == 0 ? 0 : place == 0 ? 5 : place - 1;
+    if (n >= my_steps) {
+      if (n == my_steps && n > 0) {
+        multiply(last);
+        settle(acc);
+      }
+      return;
+    }
+    const int tok0 = span0 + n * 32;
+    const bool masked = tok0 + 32 > lo;  // (of the wave) some row does not see all 32 tokens
+    f32x16 score[TILES][1];
+    const k4u32x4* keys = key_lds + (n & 3) * KS * 64 + lane;
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) score[t][0] = f32x16{};
+    // (all reads first: left to itself the compiler reads two operands at a time and waits for each pair)
+    k4u32x4 key[KS];
+#pragma unroll
+    for (int st = 0; st < KS; ++st) key[st] = keys[st * 64];
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int st = 0; st < KS; ++st) {
+#pragma unroll
+      for (int m = NP - 1; m >= 0; --m)
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+          score[t][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, key[st]), __builtin_bit_cast(bf16x8, q[t][m][st]), score[t][0], 0, 0, 0);
+    }
+    settle(score);
+    float sc[TILES][16];
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) sc[t][j] = score[t][0][j];
+      if (masked) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          if (tok0 + (j >> 2) * 8 + half * 4 + (j & 3) >= lim[t]) sc[t][j] = -INFINITY;
+      }
+    }
+    // The step before's products with this step's weights in between: chunks that the compiler keeps in this order.
+    bf16x8 nh[TILES][2], nl[TILES][2];
+    float total[TILES], p[TILES][8];
+    bool move = false;
+    {
+      const k4u32x4* from = value_lds + last * HT * 2 * 64 + lane;
+      // (a product and the next are of different sums: one that adds to its predecessor's would wait for it, and the wave with it)
+      constexpr int CHUNKS = 4 * HT;  // (block, upper or lower weights, channels' tile)
+      k4u32x4 value[2][HT];
+#pragma unroll
+      for (int j = 0; j < HT; ++j) value[0][j] = from[j * 2 * 64];
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) total[t] = 0.f;
+#pragma unroll
+      for (int m = 0; m < CHUNKS; ++m) {
+        const int block = m / (2 * HT), lower = m / HT % 2, j = m % HT;
+        __builtin_amdgcn_sched_barrier(0);
+        if (m < HT) value[1][j] = from[(j * 2 + 1) * 64];
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+          acc[t][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, value[block][j]), lower ? pl[t][block] : ph[t][block], acc[t][j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) {
+#pragma unroll
+          for (int k = m * 16 / CHUNKS; k < (m + 1) * 16 / CHUNKS; ++k) {
+            p[t][k % 8] = __builtin_amdgcn_exp2f(fmaf(sc[t][k], c1, neg_m[t]));
+            total[t] += p[t][k % 8];
+          }
+          if ((m + 1) * 16 / CHUNKS % 8 == 0) {
+            const int tt = m * 16 / CHUNKS / 8;
+            unsigned hw[4], lw[4];
+            split_weights(p[t], hw, lw);
+            nh[t][tt] = __builtin_bit_cast(bf16x8, k4u32x4{hw[0], hw[1], hw[2], hw[3]});
+            nl[t][tt] = __builtin_bit_cast(bf16x8, k4u32x4{lw[0], lw[1], lw[2], lw[3]});
+          }
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) move |= !(total[t] <= 4096.f);
+    }
+    settle(acc);
+    // A maximum moves only when the weights it leaves have grown to 2^12 (any scale will do for fp32 sums), or when a row sees
+    // something for the first time: an infinite total, or none.
+    if (__ballot(move) != 0) {
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) {
+        float top = max3(max3(sc[t][0], sc[t][1], sc[t][2]), max3(sc[t][3], sc[t][4], sc[t][5]), max3(sc[t][6], sc[t][7], sc[t][8]));
+        top = max3(top, max3(sc[t][9], sc[t][10], sc[t][11]), max3(sc[t][12], sc[t][13], max3(sc[t][14], sc[t][15], top)));
+        const float m_old = -neg_m[t], m_new = fmaxf(m_old, fold32(top, LaneMax{}) * c1);
+        const float alpha = m_new == m_old ? 1.f : __builtin_amdgcn_exp2f(m_old - m_new);
+        neg_m[t] = -m_new;
+        sum[t] *= alpha;
+#pragma unroll
+        for (int j = 0; j < HT; ++j) acc[t][j] *= alpha;
+        total[t] = weights(sc[t], m_new == -INFINITY ? 0.f : -m_new, nh[t], nl[t]);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) {
+      sum[t] += total[t];
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) ph[t][tt] = nh[t][tt], pl[t][tt] = nl[t][tt];
+    }
+  };
+  for (int i = 0; i <= rounds; ++i) {
+    // This round's operands are there; the keys of the round before have been read, and the values of the one before that.
+    __syncthreads();
+    convert(i + 1, place == 4 ? 0 : place / 2 + 1);
+    request(i + 2);
+#pragma unroll 1
+    for (int n = 2 * i; n < 2 * i + 2; ++n) {
+      step(n);
+      place = place == 5 ? 0 : place + 1;
+    }
+  }
+  __syncthreads();  // (the words go where operands were)
+
+  // ---- rows, or a split's partial rows (written through): lane (col, half) has channels (8 u + 4 half + i) * HT + j of row col ----
+#pragma unroll
+  for (int t = 0; t < TILES; ++t) {
+    if (row0 + t * 32 >= wk.group_rows) break;
+    const float m = -neg_m[t], l = fold32(sum[t], LaneAdd{});
+    float* dst = wk.all + ((size_t)it.split * WG_ROWS + (w * TILES + t) * 32 + col) * ROW;
+    const bool live = row0 + t * 32 + col < wk.group_rows;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; i += 4 / HT) {
+        const int ch = (8 * u + 4 * half + i) * HT;
+        f32x4 o;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] = acc[t][j % HT][4 * u + i + j / HT];
+        if (wk.nsplit == 1) wk.finish(row0 + t * 32 + col, ch, o, m, l);
+        else if (my_steps > 0 && live) Xwg<true>::st4f(dst + ch, o);  // (nothing seen: nothing to read)
+      }
+    if (wk.nsplit > 1 && half == 0 && live) Xwg<true>::st4f(dst + HD, f32x4{m, l, 0.f, 0.f});
+  }
+  if (wk.nsplit == 1 || !wk.arrives_last(word)) return;
+
+  // ---- the splits joined: a thread has 4 channels of a row at a time ----
+  constexpr int TPR = HD / 4, NT = WAVES * 64, BATCH = 8;
+  const int tasks = min(WG_ROWS, wk.group_rows - wk.first_row) * TPR;
+  for (int task = tid; task < tasks; task += NT) {
+    const int mr = task / TPR, e0 = (task % TPR) * 4;
+    const float* p0 = wk.all + (size_t)mr * ROW;
+    float m = -INFINITY, l = 0.f;
+    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < wk.nsplit; s0 += BATCH) {
+      f32x4 ob[BATCH];
+      f32x2 ml[BATCH];
+#pragma unroll
+      for (int j = 0; j < BATCH; ++j) {
+        const float* ps = p0 + (size_t)min(s0 + j, wk.nsplit - 1) * (WG_ROWS * ROW);
+        ml[j] = *(const f32x2*)(ps + HD);
+        ob[j] = *(const f32x4*)(ps + e0);
+      }
+      float m_new = m;
+#pragma unroll
+      for (int j = 0; j < BATCH; ++j)
+        if (s0 + j < wk.nsplit) m_new = fmaxf(m_new, ml[j].x);
+      if (m_new == -INFINITY) continue;
+      const float alpha = __builtin_amdgcn_exp2f(m - m_new);
+      l *= alpha;
+      o *= alpha;
+      m = m_new;
+#pragma unroll
+      for (int j = 0; j < BATCH; ++j) {
+        if (s0 + j >= wk.nsplit || ml[j].x == -INFINITY) continue;  // (a split that saw nothing wrote no values)
+        const float sw = __builtin_amdgcn_exp2f(ml[j].x - m);
+        l += ml[j].y * sw;
+        o += ob[j] * sw;
+      }
+    }
+    wk.finish(wk.first_row + mr, e0, o, m, l);
+  }
+}
+
+template <class K>
+static hipError_t allow_and_launch(K kernel, std::atomic<uint64_t>& allowed, size_t lds, int threads, const Kv4AttendCall& c, const Kv4Clients& cl,
+                                   hipStream_t st) {
+  if (lds > 64 * 1024) {
+    const hipError_t e = allow_lds(allowed, (const void*)kernel, lds);
     if (e != hipSuccess) return e;
   }
-  if (cl.items > 65535) return hipErrorInvalidValue;  // (a client has at most 2048 * group / 16 * 64 of them, and 32 share a launch)
-  kv4_attend_kernel<HD, T, TILES, WAVES, WIDE><<<dim3(c.view.n_kv_heads, cl.items), WAVES * 64, lds, st>>>(c, cl);
+  if (cl.items > 65535) return hipErrorInvalidValue;  // (the plan keeps them far below)
+  kernel<<<dim3(c.view.n_kv_heads, cl.items), threads, lds, st>>>(c, cl);
   return hipGetLastError();
+}
+template <int HD, typename T, int TILES>
+static hipError_t attend_few(const Kv4AttendCall& c, const Kv4Clients& cl, hipStream_t st) {
+  static std::atomic<uint64_t> allowed{0};
+  constexpr int WAVES = kv4_few_waves(TILES);
+  return allow_and_launch(kv4_attend_kernel<HD, T, TILES, WAVES>, allowed, few_lds_bytes<HD, T, TILES, WAVES>(), WAVES * 64, c, cl, st);
 }
 template <int HD, typename T>
 static hipError_t attend_of(const Kv4AttendCall& c, const Kv4Launch& l, hipStream_t st) {
-  if (l.wide) return attend_kernel<HD, T, kv4_wide_tiles(sizeof(T) == 4 ? PIPESD_F32 : PIPESD_BF16, HD), kKv4WideWaves, true>(c, l.c, st);
-  if (l.tiles == 1) return attend_kernel<HD, T, 1, kv4_few_waves(1), false>(c, l.c, st);
+  static std::atomic<uint64_t> allowed{0};
+  if (l.wide)
+    return allow_and_launch(kv4_attend_many_kernel<HD, T, kv4_wide_tiles(sizeof(T) == 4 ? PIPESD_F32 : PIPESD_BF16, HD) / 2>, allowed,
+                            many_lds_bytes<HD>(), kKv4WideWaves * 64, c, l.c, st);
+  if (l.tiles == 1) return attend_few<HD, T, 1>(c, l.c, st);
   if constexpr (sizeof(T) == 2)
-    if (l.tiles == 2) return attend_kernel<HD, T, 2, kv4_few_waves(2), false>(c, l.c, st);
+    if (l.tiles == 2) return attend_few<HD, T, 2>(c, l.c, st);
   return hipErrorInvalidValue;
 }
 hipError_t launch_kv4_attend(const Kv4AttendCall& c, const Kv4Launch& l, hipStream_t st) {
@@ -754,10 +984,10 @@ __global__ __launch_bounds__(256) void kv4_mass_kernel(Kv4AttendCall a, Kv4Clien
     if (q0 > 0) __syncthreads();  // the tiles before have been read
     {
       const TileRow tr = tile_row((q0 + w) * 16 + c, group, group_rinv, n_rows, row_off, kvh);
-      Queries<HD, NP> q;
-      load_queries<HD, NP>((const T*)a.q + tr.row * a.q_stride + tr.head * HD, tr.live, g, q);
+      k4u32x4 q[NP][NS];
+      load_queries<NP, NS>((const T*)a.q + tr.row * a.q_stride + tr.head * HD + g * (HD / 4), tr.live, q);
 #pragma unroll
-      for (int i = 0; i < NP * NS; ++i) q_lds[w][i][lane] = q.q[i / NS][i % NS];
+      for (int i = 0; i < NP * NS; ++i) q_lds[w][i][lane] = q[i / NS][i % NS];
       if (g == 0) {
         lse_lds[w][c] = tr.live ? a.lse[(size_t)tr.row * a.n_q_heads + tr.head] : INFINITY;
         lim_lds[w][c] = tr.live ? row_limit(a.limits, tr.row, row_off, n_rows, len) : 0;

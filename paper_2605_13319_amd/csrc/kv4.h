@@ -46,7 +46,7 @@ __device__ __forceinline__ int64_t kv4_record(const Kv4View& v, int layer, int b
 //   many tiles   each of four waves takes tiles of its own
 constexpr int kKv4ManyTiles = 16;  // (from here on)
 constexpr int kKv4WideWaves = 4;
-constexpr int kv4_wide_tiles(int dtype, int head_dim) { return dtype == PIPESD_BF16 && head_dim == 64 ? 3 : 2; }  // of a wave
+constexpr int kv4_wide_tiles(int dtype, int head_dim) { return dtype == PIPESD_BF16 && head_dim == 64 ? 4 : 2; }  // of a wave
 constexpr int kKv4MaxSplits = 64;
 constexpr int kv4_few_waves(int tiles) { return tiles == 1 ? 8 : 4; }
 
