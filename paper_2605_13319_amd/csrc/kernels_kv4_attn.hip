@@ -121,15 +121,25 @@ __device__ __forceinline__ void drop_values(Codes& v, unsigned& powers, int left
 
 // Wait states behind the last products of sums, tied to all of them: whoever reads them next may be in another basic block,
 // where the compiler pads too few.
-template <int N, int M, class V>
+template <bool ACC = false, int N, int M, class V>  // ACC: the sums are held in accumulation registers
 __device__ __forceinline__ void settle(V (&x)[N][M]) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  auto tie = [](V& v) {
+    if constexpr (ACC) asm volatile("" : "+a"(v));
+    else asm volatile("" : "+v"(v));
+  };
 #pragma unroll
-  for (int i = 0; i < N * M; ++i)
-    if (i > 0) asm volatile("" : "+v"(x[i / M][i % M]));
-  asm volatile("s_nop 15\n\ts_nop 1" : "+v"(x[0][0]));  // (in order: the products of all others come before)
+  for (int i = 1; i < N * M; ++i) tie(x[i / M][i % M]);
+  if constexpr (ACC) asm volatile("s_nop 15\n\ts_nop 1" : "+a"(x[0][0]));  // (in order: the products of all others come before)
+  else asm volatile("s_nop 15\n\ts_nop 1" : "+v"(x[0][0]));
 #pragma unroll
-  for (int i = 0; i < N * M; ++i)
-    if (i > 0) asm volatile("" : "+v"(x[i / M][i % M]));
+  for (int i = 1; i < N * M; ++i) tie(x[i / M][i % M]);
+#endif
+}
+
+__device__ __forceinline__ float plain(float x) {  // in an ordinary register
+  asm("" : "+v"(x));
+  return x;
 }
 
 // where lane (c, g) finds its part of a record
@@ -170,30 +180,17 @@ __device__ __forceinline__ float max3(float a, float b, float c) {  // (through 
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
   return d;
 }
-// p = hi + lo, each four pairs of bf16 numbers.  lo rounds p - hi, which is exact: a product with (-1, 0) or (0, -1) and a sum.
-// (Through the builtin the product accumulates in place, a copy each, and a factor that is a constant of the instruction sits
-// in the other half than the compiler takes it to.  Three wait states before anything reads such a product's result.)
+// p = hi + lo, each four pairs of bf16 numbers; p - hi is exact.  (Dot products with (-1, 0) and (0, -1) give it in half the
+// instructions, but wait for the matrix cores: two beside a 32 x 32 x 16 product take 53 cycles, where four of any others hide in its 32.)
+__device__ __forceinline__ unsigned lower_pair(float p0, float p1, unsigned hi) {
+  return pack2_bf16(p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xffff0000u));
+}
 __device__ __forceinline__ void split_weights(const float (&p)[8], unsigned (&hi)[4], unsigned (&lo)[4]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) hi[i] = pack2_bf16(p[2 * i], p[2 * i + 1]);
-#if defined(__HIP_DEVICE_COMPILE__)
-  float r[8];
-  asm("s_nop 0\n\t"
-      "v_dot2_f32_bf16 %0, %8, %20, %12\n\t"
-      "v_dot2_f32_bf16 %1, %8, %21, %13\n\t"
-      "v_dot2_f32_bf16 %2, %9, %20, %14\n\t"
-      "v_dot2_f32_bf16 %3, %9, %21, %15\n\t"
-      "v_dot2_f32_bf16 %4, %10, %20, %16\n\t"
-      "v_dot2_f32_bf16 %5, %10, %21, %17\n\t"
-      "v_dot2_f32_bf16 %6, %11, %20, %18\n\t"
-      "v_dot2_f32_bf16 %7, %11, %21, %19\n\t"
-      "s_nop 3"
-      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
-      : "v"(hi[0]), "v"(hi[1]), "v"(hi[2]), "v"(hi[3]), "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "v"(p[4]), "v"(p[5]), "v"(p[6]),
-        "v"(p[7]), "s"(0x0000bf80u), "s"(0xbf800000u));
-#pragma unroll
-  for (int i = 0; i < 4; ++i) lo[i] = pack2_bf16(r[2 * i], r[2 * i + 1]);
-#endif
+  for (int i = 0; i < 4; ++i) {
+    hi[i] = pack2_bf16(p[2 * i], p[2 * i + 1]);
+    lo[i] = lower_pair(p[2 * i], p[2 * i + 1], hi[i]);
+  }
 }
 
 // which client and split a workgroup is for
@@ -583,15 +580,19 @@ __global__ __launch_bounds__(WAVES * 64, TILES == 1 ? 4 : 2) void kv4_attend_ker
 // Layout of a 32 x 32 x 16 product: operand lane (r, h) holds row (column) r, k = 8 h .. + 7; the result's register 4 u + i holds
 // row 8 u + 4 h + i of column r.  Scores: k is channel h * HD / 2 + 8 s .. of step s.  Values: row r of product j is channel
 // r * HD / 32 + j, and k the tokens 4 h .. + 3 and 8 + 4 h .. + 3 of a block, which is how the weights lie.
-// LDS: keys [2 times 64 tokens][2 steps][HD / 16][lane], values [3 times 64 tokens][2 steps][HD / 32][block][lane]: at head
-// dim 128 half of a compute unit's, to the byte (before and behind the walk it holds a few words)
+// LDS: keys [2 times 64 tokens][2 steps][HD / 16][lane], values [2 times 64 tokens][2 steps][HD / 32][block][lane] (before and
+// behind the walk: a few words)
 template <int HD>
-constexpr size_t many_lds_bytes() { return (size_t)10 * (HD / 16) * 64 * 16; }
+constexpr size_t many_lds_bytes() { return (size_t)8 * (HD / 16) * 64 * 16; }
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
+// whether a wave takes a SIMD's registers alone, half of them accumulation registers: then O^T is there
 template <int HD, typename T, int TILES>
-__global__ __launch_bounds__(kKv4WideWaves * 64, 2) void kv4_attend_many_kernel(Kv4AttendCall a, Kv4Clients clients) {
+constexpr bool alone() { return HD * TILES * pieces<T>() > 128; }
+template <int HD, typename T, int TILES>
+__global__ __launch_bounds__(kKv4WideWaves * 64, (alone<HD, T, TILES>() ? 1 : 2)) void kv4_attend_many_kernel(Kv4AttendCall a, Kv4Clients clients) {
   constexpr int NP = pieces<T>(), KS = HD / 16, HT = HD / 32, ROW = HD + kKv4PartPad, WAVES = kKv4WideWaves, WG_ROWS = WAVES * TILES * 32;
+  constexpr bool ALONE = alone<HD, T, TILES>();
   typedef typename std::conditional<HD == 128, k4u32x4, k4u32x2>::type Codes;
   extern __shared__ float lds[];
   k4u32x4* key_lds = (k4u32x4*)lds;
@@ -599,7 +600,7 @@ __global__ __launch_bounds__(kKv4WideWaves * 64, 2) void kv4_attend_many_kernel(
   int* word = (int*)lds;
 
   const int kvh = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int c = lane & 15, g = lane >> 4, col = lane & 31, half = lane >> 5;
+  const int c = lane & 15, g = lane >> 4, gv = (g & 1) * 2 + (g >> 1), col = lane & 31, half = lane >> 5;
   const Kv4Item it = find_item(clients, blockIdx.y, lane);
   const Work<HD, T> wk(a, clients, it, kvh, WG_ROWS / 16);
   const int len = wk.len, span0 = it.split * clients.span;
@@ -634,7 +635,6 @@ __global__ __launch_bounds__(kKv4WideWaves * 64, 2) void kv4_attend_many_kernel(
     const int end = min(min(span0 + clients.span, len), seen);
     return end > span0 ? (end - span0 + 31) / 32 : 0;
   };
-  const int my_steps = steps_to(hi);
   if (lane == 0) word[w] = hi;  // all waves walk as far as one of them has to
   __syncthreads();
 #pragma unroll
@@ -652,172 +652,150 @@ __global__ __launch_bounds__(kKv4WideWaves * 64, 2) void kv4_attend_many_kernel(
 #pragma unroll
     for (int j = 0; j < HT; ++j) acc[t][j] = f32x16{};
   }
-  const LaneOffsets<HD> at(c, g);
+  const LaneOffsets<HD> at(c, g), at_v(c, gv);
   const float c1 = kv4_scale<HD>();
 
   // ---- this wave's block of a round ----
-  Codes k_raw, v_raw;
-  unsigned k_pow, v_pow;
-  auto request = [&](int i) {
+  Codes k_raw[2], v_raw[2];  // of even rounds, of odd ones
+  unsigned k_pow[2], v_pow[2];
+  auto record = [&](int i) {
+    const unsigned lo = __builtin_amdgcn_readlane((unsigned)my_rec, i & 63), hi = __builtin_amdgcn_readlane((unsigned)(my_rec >> 32), i & 63);
+    return head_base + (int64_t)(((uint64_t)hi << 32) | lo);
+  };
+  auto request_keys = [&](int i, int set) {
     if (i >= rounds) return;
     if (i > 0 && (i & 63) == 0) load_blocks(i);
-    const unsigned lo = __builtin_amdgcn_readlane((unsigned)my_rec, i & 63), hi = __builtin_amdgcn_readlane((unsigned)(my_rec >> 32), i & 63);
-    const uint8_t* rec = head_base + (int64_t)(((uint64_t)hi << 32) | lo);
-    k_raw = *(const Codes*)(rec + at.k);
-    v_raw = *(const Codes*)(rec + at.v);
-    k_pow = rec[at.kp];
-    v_pow = *(const unsigned*)(rec + at.vp);
+    const uint8_t* rec = record(i);
+    k_raw[set] = *(const Codes*)(rec + at.k);
+    k_pow[set] = rec[at.kp];
   };
-  auto convert = [&](int i, int value_buf) {
+  auto request_values = [&](int i, int set) {  // (after the keys')
     if (i >= rounds) return;
-    const int tt = w & 1, st0 = w >> 1;  // block of a step, step of the round
-    {  // lane (token c, quarter g): channels g * HD / 4 + 8 st .. + 7
-      k4u32x4* to = key_lds + (((i & 1) * 2 + st0) * KS + (g & 1) * (KS / 2)) * 64 + (g >> 1) * 32 + tt * 16 + c;
-      const float power = __uint_as_float(k_pow << 23);
-#pragma unroll
-      for (int st = 0; st < KS / 2; ++st) to[st * 64] = __builtin_bit_cast(k4u32x4, key_operand(k_raw[st], power));
-    }
-    {  // lane (unit c, quarter g): channels c * HD / 16 .. of tokens 4 g .. + 3
-      const int left = len - (span0 + i * 64 + w * 16);
-      if (left < 16) drop_values<HD>(v_raw, v_pow, left - g * 4);
-      k4u32x2* to = (k4u32x2*)(value_lds + ((value_buf * 2 + st0) * HT * 2 + tt) * 64 + (g & 1) * 32 + 2 * c) + (g >> 1);
-#pragma unroll
-      for (int b = 0; b < HD / 32; ++b) {  // channels 2 b and 2 b + 1 of the unit: of row 2 c, then of row 2 c + 1
-        k4u32x2 even, odd;
-        value_operands<HD>(v_raw, v_pow, b, even, odd);
-        const int ch = 2 * b;
-        to[((ch % HT) * 2 * 64 + ch / HT) * 2] = even;
-        to[(((ch + 1) % HT) * 2 * 64 + (ch + 1) / HT) * 2] = odd;
-      }
-    }
+    const uint8_t* rec = record(i);
+    v_raw[set] = *(const Codes*)(rec + at_v.v);
+    v_pow[set] = *(const unsigned*)(rec + at_v.vp);
+  };
+  // In pieces: an operand's registers of each go between two products.  (An LDS store of 16 bytes a lane takes 13 cycles of the
+  // compute unit, a load 4: a round's stores are spread over its two steps.)
+  k4u32x4* key_to;
+  k4u32x2* value_to;
+  auto open_keys = [&](int i) { key_to = key_lds + (((i & 1) * 2 + (w >> 1)) * KS + (g & 1) * (KS / 2)) * 64 + (g >> 1) * 32 + (w & 1) * 16 + c; };
+  auto convert_keys = [&](int piece, int set) {  // lane (token c, quarter g): channels g * HD / 4 + 8 piece .. + 7
+    key_to[piece * 64] = __builtin_bit_cast(k4u32x4, key_operand(k_raw[set][piece], __uint_as_float(k_pow[set] << 23)));
+  };
+  auto open_values = [&](int i, int set) {
+    value_to = (k4u32x2*)(value_lds + (((i & 1) * 2 + (w >> 1)) * HT * 2 + (w & 1)) * 64 + (gv & 1) * 32 + c) + (gv >> 1);
+    const int left = len - (span0 + i * 64 + w * 16);
+    if (left < 16) drop_values<HD>(v_raw[set], v_pow[set], left - gv * 4);
+  };
+  auto convert_values = [&](int piece, int set) {  // lane (unit c, quarter gv): two channels of the unit, of tokens 4 gv .. + 3
+    const int ch = 2 * piece;
+    k4u32x2 even, odd;
+    value_operands<HD>(v_raw[set], v_pow[set], piece, even, odd);
+    value_to[(ch % HT * 2 * 64 + ch / HT * 16) * 2] = even;
+    value_to[((ch + 1) % HT * 2 * 64 + (ch + 1) / HT * 16) * 2] = odd;
   };
 
-  bf16x8 ph[TILES][2], pl[TILES][2];  // the step before's weights, not yet multiplied
+  // A step's weights as two operands a block: upper and lower parts.  Two sets: the step's, and those of the step before, whose
+  // products are still to come.
+  unsigned up[2][TILES][2][4], low[2][TILES][2][4];
 #pragma unroll
   for (int t = 0; t < TILES; ++t)
 #pragma unroll
-    for (int tt = 0; tt < 2; ++tt) ph[t][tt] = pl[t][tt] = __builtin_bit_cast(bf16x8, k4u32x4{0u, 0u, 0u, 0u});
-  auto multiply = [&](int at_step) {  // (place of the step in the ring of values)
-    const k4u32x4* from = value_lds + at_step * HT * 2 * 64 + lane;
-#pragma unroll
     for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-      for (int j = 0; j < HT; ++j) {
-        const bf16x8 value = __builtin_bit_cast(bf16x8, from[(j * 2 + tt) * 64]);
-#pragma unroll
-        for (int t = 0; t < TILES; ++t) {
-          acc[t][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value, ph[t][tt], acc[t][j], 0, 0, 0);
-          acc[t][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value, pl[t][tt], acc[t][j], 0, 0, 0);
-        }
-      }
-  };
-  // a step's weights, as two sets of operands each, and the lane's sum of them
-  auto weights = [&](const float (&sc)[16], float neg, bf16x8 (&h)[2], bf16x8 (&l)[2]) {
-    float total = 0.f;
-#pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
-      float p[8];
-      unsigned hw[4], lw[4];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(sc[tt * 8 + i], c1, neg));
-      total += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-      split_weights(p, hw, lw);
-      h[tt] = __builtin_bit_cast(bf16x8, k4u32x4{hw[0], hw[1], hw[2], hw[3]});
-      l[tt] = __builtin_bit_cast(bf16x8, k4u32x4{lw[0], lw[1], lw[2], lw[3]});
-    }
-    return total;
-  };
-
-  request(0);
-  convert(0, 0);
-  request(1);
-  int place = 0;  // of step n in the ring of 6
-  auto step = [&](int n) {
-    const int last = n == 0 ? 0 : place == 0 ? 5 : place - 1;
-    if (n >= my_steps) {
-      if (n == my_steps && n > 0) {
-        multiply(last);
-        settle(acc);
-      }
-      return;
-    }
+      for (int i = 0; i < 4; ++i) up[1][t][tt][i] = low[1][t][tt][i] = 0u;
+  auto operand = [](const unsigned (&x)[4]) { return __builtin_bit_cast(bf16x8, k4u32x4{x[0], x[1], x[2], x[3]}); };
+  k4u32x4 key[KS];
+  auto step = [&](int n, auto second, auto odd) {
+    constexpr int NOW = decltype(second)::value, BEFORE = 1 - NOW, NEXT = 1 - decltype(odd)::value;  // of a round's two steps; the next round's set
     const int tok0 = span0 + n * 32;
     const bool masked = tok0 + 32 > lo;  // (of the wave) some row does not see all 32 tokens
+    const k4u32x4* from = value_lds + ((n == 0 ? 0 : n - 1) & 3) * HT * 2 * 64 + lane;  // (for the first step's weights of 0: its own)
+    k4u32x4 value[2][HT];
     f32x16 score[TILES][1];
-    const k4u32x4* keys = key_lds + (n & 3) * KS * 64 + lane;
 #pragma unroll
     for (int t = 0; t < TILES; ++t) score[t][0] = f32x16{};
-    // (all reads first: left to itself the compiler reads two operands at a time and waits for each pair)
-    k4u32x4 key[KS];
-#pragma unroll
-    for (int st = 0; st < KS; ++st) key[st] = keys[st * 64];
-    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (NOW == 0) open_keys(n / 2 + 1);
+    else open_values(n / 2 + 1, NEXT);
+    // Scores, and between them half of the next round's operands (behind the last round: nobody's).
 #pragma unroll
     for (int st = 0; st < KS; ++st) {
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int m = NP - 1; m >= 0; --m)
 #pragma unroll
         for (int t = 0; t < TILES; ++t)
           score[t][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, key[st]), __builtin_bit_cast(bf16x8, q[t][m][st]), score[t][0], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      if (st % 2 == 0) {
+        if constexpr (NOW == 0) convert_keys(st / 2, NEXT);
+        else convert_values(st / 2, NEXT);
+      }
+      if (st >= KS - HT) value[0][st - (KS - HT)] = from[(st - (KS - HT)) * 2 * 64];
     }
-    settle(score);
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (NOW == 0) request_keys(n / 2 + 3, NEXT);
+    else request_values(n / 2 + 3, NEXT);
+    settle<ALONE>(score);
     float sc[TILES][16];
 #pragma unroll
-    for (int t = 0; t < TILES; ++t) {
+    for (int t = 0; t < TILES; ++t)
 #pragma unroll
-      for (int j = 0; j < 16; ++j) sc[t][j] = score[t][0][j];
-      if (masked) {
+      for (int j = 0; j < 16; ++j) sc[t][j] = plain(score[t][0][j]);
+    if (masked) {
+#pragma unroll
+      for (int t = 0; t < TILES; ++t)
 #pragma unroll
         for (int j = 0; j < 16; ++j)
           if (tok0 + (j >> 2) * 8 + half * 4 + (j & 3) >= lim[t]) sc[t][j] = -INFINITY;
-      }
     }
-    // The step before's products with this step's weights in between: chunks that the compiler keeps in this order.
-    bf16x8 nh[TILES][2], nl[TILES][2];
-    float total[TILES], p[TILES][8];
-    bool move = false;
-    {
-      const k4u32x4* from = value_lds + last * HT * 2 * 64 + lane;
-      // (a product and the next are of different sums: one that adds to its predecessor's would wait for it, and the wave with it)
-      constexpr int CHUNKS = 4 * HT;  // (block, upper or lower weights, channels' tile)
-      k4u32x4 value[2][HT];
+    // The step before's products, and between them two weights of this step at a time (and the lower parts of the two before).
+    constexpr int PAIRS = 8 * TILES, EACH = HT / 2;  // products for each pair
+    float total[TILES], p[2];
 #pragma unroll
-      for (int j = 0; j < HT; ++j) value[0][j] = from[j * 2 * 64];
+    for (int t = 0; t < TILES; ++t) total[t] = 0.f;
+    auto pair = [&](int x) -> unsigned& { return up[NOW][x / 4 % TILES][x / (4 * TILES)][x % 4]; };
+    auto pair_low = [&](int x) -> unsigned& { return low[NOW][x / 4 % TILES][x / (4 * TILES)][x % 4]; };
+    auto score_of = [&](int x, int k) { return sc[x / 4 % TILES][x / (4 * TILES) * 8 + x % 4 * 2 + k]; };
+    auto raise = [&](int x) {  // the weights of pair x
+      const float neg = neg_m[x / 4 % TILES];
+      p[0] = __builtin_amdgcn_exp2f(fmaf(score_of(x, 0), c1, neg));
+      p[1] = __builtin_amdgcn_exp2f(fmaf(score_of(x, 1), c1, neg));
+    };
+    raise(0);
+    const k4u32x4* keys = key_lds + ((n + 1) & 3) * KS * 64 + lane;
+    unsigned long long move = 0;
 #pragma unroll
-      for (int t = 0; t < TILES; ++t) total[t] = 0.f;
+    for (int x = 0; x < PAIRS; ++x) {
 #pragma unroll
-      for (int m = 0; m < CHUNKS; ++m) {
-        const int block = m / (2 * HT), lower = m / HT % 2, j = m % HT;
+      for (int k = 0; k < EACH; ++k) {
+        const int y = x * EACH + k, block = y / (2 * HT * TILES), lower = y / (HT * TILES) % 2, j = y / TILES % HT, tile = y % TILES;
         __builtin_amdgcn_sched_barrier(0);
-        if (m < HT) value[1][j] = from[(j * 2 + 1) * 64];
-#pragma unroll
-        for (int t = 0; t < TILES; ++t)
-          acc[t][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, value[block][j]), lower ? pl[t][block] : ph[t][block], acc[t][j], 0, 0, 0);
+        acc[tile][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, value[block][j]),
+                                                              operand(lower ? low[BEFORE][tile][block] : up[BEFORE][tile][block]), acc[tile][j], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
+        if (k == 0) {
+          pair(x) = pack2_bf16(p[0], p[1]);
+          pair_low(x) = lower_pair(p[0], p[1], pair(x));
+          total[x / 4 % TILES] += p[0] + p[1];
+          if (x < HT) value[1][x] = from[(x * 2 + 1) * 64];
+          if (x >= PAIRS - KS) key[x - (PAIRS - KS)] = keys[(x - (PAIRS - KS)) * 64];
+          if (x == PAIRS - 1) {
+            bool far = false;
 #pragma unroll
-        for (int t = 0; t < TILES; ++t) {
-#pragma unroll
-          for (int k = m * 16 / CHUNKS; k < (m + 1) * 16 / CHUNKS; ++k) {
-            p[t][k % 8] = __builtin_amdgcn_exp2f(fmaf(sc[t][k], c1, neg_m[t]));
-            total[t] += p[t][k % 8];
-          }
-          if ((m + 1) * 16 / CHUNKS % 8 == 0) {
-            const int tt = m * 16 / CHUNKS / 8;
-            unsigned hw[4], lw[4];
-            split_weights(p[t], hw, lw);
-            nh[t][tt] = __builtin_bit_cast(bf16x8, k4u32x4{hw[0], hw[1], hw[2], hw[3]});
-            nl[t][tt] = __builtin_bit_cast(bf16x8, k4u32x4{lw[0], lw[1], lw[2], lw[3]});
+            for (int t = 0; t < TILES; ++t) far |= !(total[t] <= 4096.f);
+            move = __ballot(far);
           }
         }
+        if (k == EACH - 1 && x + 1 < PAIRS) raise(x + 1);
       }
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int t = 0; t < TILES; ++t) move |= !(total[t] <= 4096.f);
     }
-    settle(acc);
+    __builtin_amdgcn_sched_barrier(0);
     // A maximum moves only when the weights it leaves have grown to 2^12 (any scale will do for fp32 sums), or when a row sees
     // something for the first time: an infinite total, or none.
-    if (__ballot(move) != 0) {
+    if (move != 0) {
+      settle<ALONE>(acc);
 #pragma unroll
       for (int t = 0; t < TILES; ++t) {
         float top = max3(max3(sc[t][0], sc[t][1], sc[t][2]), max3(sc[t][3], sc[t][4], sc[t][5]), max3(sc[t][6], sc[t][7], sc[t][8]));
@@ -828,30 +806,66 @@ __global__ __launch_bounds__(kKv4WideWaves * 64, 2) void kv4_attend_many_kernel(
         sum[t] *= alpha;
 #pragma unroll
         for (int j = 0; j < HT; ++j) acc[t][j] *= alpha;
-        total[t] = weights(sc[t], m_new == -INFINITY ? 0.f : -m_new, nh[t], nl[t]);
+        const float neg = m_new == -INFINITY ? 0.f : -m_new;
+        total[t] = 0.f;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[t][2 * x], c1, neg)), p1 = __builtin_amdgcn_exp2f(fmaf(sc[t][2 * x + 1], c1, neg));
+          total[t] += p0 + p1;
+          up[NOW][t][x / 4][x % 4] = pack2_bf16(p0, p1);
+          low[NOW][t][x / 4][x % 4] = lower_pair(p0, p1, up[NOW][t][x / 4][x % 4]);
+        }
       }
     }
 #pragma unroll
-    for (int t = 0; t < TILES; ++t) {
-      sum[t] += total[t];
-#pragma unroll
-      for (int tt = 0; tt < 2; ++tt) ph[t][tt] = nh[t][tt], pl[t][tt] = nl[t][tt];
-    }
+    for (int t = 0; t < TILES; ++t) sum[t] += total[t];
   };
-  for (int i = 0; i <= rounds; ++i) {
-    // This round's operands are there; the keys of the round before have been read, and the values of the one before that.
+
+  if (rounds > 0) {
+    request_keys(0, 0);
+    request_values(0, 0);
+    request_keys(1, 1);
+    request_values(1, 1);
+    open_keys(0);
+    open_values(0, 0);
+#pragma unroll
+    for (int piece = 0; piece < KS / 2; ++piece) convert_keys(piece, 0), convert_values(piece, 0);
+    request_keys(2, 0);
+    request_values(2, 0);
     __syncthreads();
-    convert(i + 1, place == 4 ? 0 : place / 2 + 1);
-    request(i + 2);
+#pragma unroll
+    for (int st = 0; st < KS; ++st) key[st] = key_lds[st * 64 + lane];
+    // Between two barriers, the second step of round i - 1 and the first of round i: they read keys of round i, as operands of the
+    // steps to come, and values of round i - 1, and write values of round i and keys of round i + 1.
+    typedef std::integral_constant<int, 0> Zero;
+    typedef std::integral_constant<int, 1> One;
 #pragma unroll 1
-    for (int n = 2 * i; n < 2 * i + 2; ++n) {
-      step(n);
-      place = place == 5 ? 0 : place + 1;
+    for (int i = 0; i < rounds; i += 2) {
+      step(2 * i, Zero{}, Zero{});
+      __syncthreads();
+      step(2 * i + 1, One{}, Zero{});
+      if (i + 1 == rounds) break;
+      step(2 * i + 2, Zero{}, One{});
+      __syncthreads();
+      step(2 * i + 3, One{}, One{});
     }
+    const k4u32x4* from = value_lds + ((2 * rounds - 1) & 3) * HT * 2 * 64 + lane;
+#pragma unroll
+    for (int block = 0; block < 2; ++block)
+#pragma unroll
+      for (int j = 0; j < HT; ++j) {
+        const bf16x8 value = __builtin_bit_cast(bf16x8, from[(j * 2 + block) * 64]);
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) {
+          acc[t][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value, operand(up[1][t][block]), acc[t][j], 0, 0, 0);
+          acc[t][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value, operand(low[1][t][block]), acc[t][j], 0, 0, 0);
+        }
+      }
+    settle<ALONE>(acc);
   }
   __syncthreads();  // (the words go where operands were)
 
-  // ---- rows, or a split's partial rows (written through): lane (col, half) has channels (8 u + 4 half + i) * HT + j of row col ----
+  // ---- rows, or a split's partial rows (written through) ----
 #pragma unroll
   for (int t = 0; t < TILES; ++t) {
     if (row0 + t * 32 >= wk.group_rows) break;
@@ -859,16 +873,18 @@ __global__ __launch_bounds__(kKv4WideWaves * 64, 2) void kv4_attend_many_kernel(
     float* dst = wk.all + ((size_t)it.split * WG_ROWS + (w * TILES + t) * 32 + col) * ROW;
     const bool live = row0 + t * 32 + col < wk.group_rows;
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int i = 0; i < 4; i += 4 / HT) {
-        const int ch = (8 * u + 4 * half + i) * HT;
-        f32x4 o;
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o[j] = acc[t][j % HT][4 * u + i + j / HT];
-        if (wk.nsplit == 1) wk.finish(row0 + t * 32 + col, ch, o, m, l);
-        else if (my_steps > 0 && live) Xwg<true>::st4f(dst + ch, o);  // (nothing seen: nothing to read)
-      }
+        for (int e = 0; e < HD / 16; e += 4) {  // of unit 8 u + 4 half + i
+          const int ch = (8 * u + 4 * half + i) * (HD / 16) + e;
+          f32x4 o;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) o[k] = acc[t][(e + k) % HT][4 * (u + (e + k) / HT * 2) + i];
+          if (wk.nsplit == 1) wk.finish(row0 + t * 32 + col, ch, o, m, l);
+          else if (rounds > 0 && live) Xwg<true>::st4f(dst + ch, o);  // (nothing seen: nothing to read)
+        }
     if (wk.nsplit > 1 && half == 0 && live) Xwg<true>::st4f(dst + HD, f32x4{m, l, 0.f, 0.f});
   }
   if (wk.nsplit == 1 || !wk.arrives_last(word)) return;

@@ -110,11 +110,12 @@ inline Kv4PlanNeeds kv4_plan(const Kv4Client* cl, int n, int dtype, int head_dim
     for (int i = 0; i < n; ++i)
       if (mine(cl[i])) most_tiles = std::max(most_tiles, tiles_of(cl[i])), longest = std::max(longest, (int)cl[i].len);
     if (most_tiles == 0) continue;
-    int tiles, wg_tiles, step;
+    int tiles, wg_tiles, step, resident = 2;  // resident: workgroups that a compute unit holds at once
     if (wide) {
       tiles = kv4_wide_tiles(dtype, head_dim);
       wg_tiles = kKv4WideWaves * tiles;
       step = 512;
+      if (head_dim == 128 && dtype == PIPESD_F32) resident = 1;
     } else {
       tiles = kv4_few_tiles(dtype, head_dim, work(1), work(2), n_cu);
       wg_tiles = tiles;
@@ -123,7 +124,7 @@ inline Kv4PlanNeeds kv4_plan(const Kv4Client* cl, int n, int dtype, int head_dim
     // (a split costs what joins it, about the time of three steps: none below 768 tokens)
     int64_t span = std::max<int64_t>(step, longest <= 768 ? longest : 0);
     span = (span + step - 1) / step * step;
-    while (workgroups(wg_tiles, span) > 2L * n_cu && span < longest) span += span < 16 * step ? step : span / 16 / step * step;
+    while (workgroups(wg_tiles, span) > (int64_t)resident * n_cu && span < longest) span += span < 16 * step ? step : span / 16 / step * step;
     span = std::max<int64_t>(span, ((longest + kKv4MaxSplits - 1) / kKv4MaxSplits + step - 1) / step * step);
     Kv4Launch l{};
     auto flush = [&] {
