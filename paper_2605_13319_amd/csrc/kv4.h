@@ -94,22 +94,14 @@ inline Kv4PlanNeeds kv4_plan(const Kv4Client* cl, int n, int dtype, int head_dim
   for (int wide = 0; wide < 2; ++wide) {
     auto tiles_of = [&](const Kv4Client& c) { return attn_query_tiles(group, c.n_rows); };
     auto mine = [&](const Kv4Client& c) { return c.n_rows > 0 && (tiles_of(c) >= kKv4ManyTiles) == (wide != 0); };
-    auto workgroups = [&](int tiles, int64_t span) {
-      int64_t w = 0;
-      for (int i = 0; i < n; ++i)
-        if (mine(cl[i])) w += (int64_t)n_kv_heads * ((tiles_of(cl[i]) + tiles - 1) / tiles) * ((cl[i].len + span - 1) / span);
-      return w;
-    };
-    auto work = [&](int tiles) {  // steps of 32 tokens of all workgroups' sets of tiles
-      double w = 0;
-      for (int i = 0; i < n; ++i)
-        if (mine(cl[i])) w += (double)n_kv_heads * ((tiles_of(cl[i]) + tiles - 1) / tiles) * cl[i].len / 32;
-      return w;
-    };
-    int most_tiles = 0, longest = 0;
-    for (int i = 0; i < n; ++i)
-      if (mine(cl[i])) most_tiles = std::max(most_tiles, tiles_of(cl[i])), longest = std::max(longest, (int)cl[i].len);
-    if (most_tiles == 0) continue;
+    int longest = 0;
+    double work[3] = {0, 0, 0};  // [tiles]: steps of 32 tokens of all workgroups' sets of tiles
+    for (int i = 0; i < n; ++i) {
+      if (!mine(cl[i])) continue;
+      longest = std::max(longest, (int)cl[i].len);
+      for (int tiles = 1; tiles <= 2; ++tiles) work[tiles] += (double)n_kv_heads * ((tiles_of(cl[i]) + tiles - 1) / tiles) * cl[i].len / 32;
+    }
+    if (longest == 0) continue;
     int tiles, wg_tiles, step, resident = 2;  // resident: workgroups that a compute unit holds at once
     if (wide) {
       tiles = kv4_wide_tiles(dtype, head_dim);
@@ -117,14 +109,22 @@ inline Kv4PlanNeeds kv4_plan(const Kv4Client* cl, int n, int dtype, int head_dim
       step = 512;
       if (head_dim == 128 && dtype == PIPESD_F32) resident = 1;
     } else {
-      tiles = kv4_few_tiles(dtype, head_dim, work(1), work(2), n_cu);
+      tiles = kv4_few_tiles(dtype, head_dim, work[1], work[2], n_cu);
       wg_tiles = tiles;
       step = kv4_few_waves(tiles) * 32;
     }
+    auto workgroups = [&](int64_t span) {
+      int64_t w = 0;
+      for (int i = 0; i < n; ++i)
+        if (mine(cl[i])) w += (int64_t)n_kv_heads * ((tiles_of(cl[i]) + wg_tiles - 1) / wg_tiles) * ((cl[i].len + span - 1) / span);
+      return w;
+    };
     // (a split costs what joins it, about the time of three steps: none below 768 tokens)
+    const int64_t room = (int64_t)resident * n_cu;
     int64_t span = std::max<int64_t>(step, longest <= 768 ? longest : 0);
+    span = std::max<int64_t>(span, (int64_t)(workgroups(1) / room));  // (no shorter one would do)
     span = (span + step - 1) / step * step;
-    while (workgroups(wg_tiles, span) > (int64_t)resident * n_cu && span < longest) span += span < 16 * step ? step : span / 16 / step * step;
+    while (workgroups(span) > room && span < longest) span += span < 16 * step ? step : span / 16 / step * step;
     span = std::max<int64_t>(span, ((longest + kKv4MaxSplits - 1) / kKv4MaxSplits + step - 1) / step * step);
     Kv4Launch l{};
     auto flush = [&] {
