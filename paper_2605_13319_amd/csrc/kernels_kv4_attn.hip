@@ -573,26 +573,31 @@ __global__ __launch_bounds__(WAVES * 64, TILES == 1 ? 4 : 2) void kv4_attend_ker
   }
 }
 
-// ---- many rows: each of four waves has 32 or 64 of its own ----
-// Keys and values are converted once, a block by each wave, into operands in LDS that all read; one barrier for 64 tokens.  Products of 32 x 32: what a wave may issue is the bound, 8 cycles a product of either
-// size beside 4 to 5 an instruction of the vector unit.  The values of a step of 32 tokens are multiplied one step later, so
-// that those products, which depend on nothing of the step, travel with the weights' instructions.
-// Layout of a 32 x 32 x 16 product: operand lane (r, h) holds row (column) r, k = 8 h .. + 7; the result's register 4 u + i holds
-// row 8 u + 4 h + i of column r.  Scores: k is channel h * HD / 2 + 8 s .. of step s.  Values: row r of product j is channel
-// r * HD / 32 + j, and k the tokens 4 h .. + 3 and 8 + 4 h .. + 3 of a block, which is how the weights lie.
-// LDS: keys [2 times 64 tokens][2 steps][HD / 16][lane], values [2 times 64 tokens][2 steps][HD / 32][block][lane] (before and
-// behind the walk: a few words)
+// ---- many tiles: each of four waves has two of its own, 32 rows ----
+// Keys and values are converted once, a block by each wave, into operands in LDS that all read; a barrier for every 64 tokens.
+// Products of 32 x 32 x 16: 8 for a step's scores, 16 for its values, which are multiplied a step later: those products, which depend
+// on nothing of the step, travel with the weights' instructions, the score products with half of the next round's conversion.  (The
+// matrix cores leave a wave 28 of a product's 32 cycles for other instructions, and one after another, products and instructions
+// would take both times.)  Chunks that the compiler keeps in order do it: left to itself it puts the products side by side.
+//
+// Layout of a product: operand lane (r, h) holds row (column) r, k = 8 h .. + 7; the result's register 4 u + i holds row 8 u + 4 h + i
+// of column r.  Scores: k is channel h * HD / 2 + 8 s .. of step s.  Values: row r of product j is channel
+// r % 16 * HD / 16 + r / 16 * HD / 32 + j, so that what 32 lanes store lies side by side, and k the tokens 4 h .. + 3 and 8 + 4 h .. + 3
+// of a block, which is how the weights lie.
+// LDS: keys [2 times 64 tokens][2 steps][HD / 16][lane], values [2 times 64 tokens][2 steps][HD / 32][block][lane] (before the walk: a
+// few words)
 template <int HD>
 constexpr size_t many_lds_bytes() { return (size_t)8 * (HD / 16) * 64 * 16; }
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 // whether a wave takes a SIMD's registers alone, half of them accumulation registers: then O^T is there
-template <int HD, typename T, int TILES>
-constexpr bool alone() { return HD * TILES * pieces<T>() > 128; }
-template <int HD, typename T, int TILES>
-__global__ __launch_bounds__(kKv4WideWaves * 64, (alone<HD, T, TILES>() ? 1 : 2)) void kv4_attend_many_kernel(Kv4AttendCall a, Kv4Clients clients) {
-  constexpr int NP = pieces<T>(), KS = HD / 16, HT = HD / 32, ROW = HD + kKv4PartPad, WAVES = kKv4WideWaves, WG_ROWS = WAVES * TILES * 32;
-  constexpr bool ALONE = alone<HD, T, TILES>();
+template <int HD, typename T>
+constexpr bool alone() { return HD * pieces<T>() > 192; }
+
+template <int HD, typename T>
+__global__ __launch_bounds__(kKv4WideWaves * 64, (alone<HD, T>() ? 1 : 2)) void kv4_attend_many_kernel(Kv4AttendCall a, Kv4Clients clients) {
+  constexpr int NP = pieces<T>(), KS = HD / 16, HT = HD / 32, ROW = HD + kKv4PartPad, WAVES = kKv4WideWaves, WG_ROWS = WAVES * 32;
+  constexpr bool ALONE = alone<HD, T>();
   typedef typename std::conditional<HD == 128, k4u32x4, k4u32x2>::type Codes;
   extern __shared__ float lds[];
   k4u32x4* key_lds = (k4u32x4*)lds;
@@ -616,46 +621,34 @@ __global__ __launch_bounds__(kKv4WideWaves * 64, (alone<HD, T, TILES>() ? 1 : 2)
   load_blocks(0);
 
   // ---- queries, and how far each row sees ----
-  k4u32x4 q[TILES][NP][KS];
-  int lim[TILES];
-  int lo = len, hi = 0;
-  const int row0 = wk.first_row + w * TILES * 32;
-#pragma unroll
-  for (int t = 0; t < TILES; ++t) {
-    const TileRow tr = wk.row(row0 + t * 32 + col);
-    load_queries<NP, KS>((const T*)a.q + tr.row * a.q_stride + tr.head * HD + half * (HD / 2), tr.live, q[t]);
-    lim[t] = wk.limit(tr);
-    if (tr.live) lo = min(lo, lim[t]), hi = max(hi, lim[t]);
-  }
+  const int row0 = wk.first_row + w * 32;
+  const bool idle = row0 >= wk.group_rows;  // (the wave has no row, and only converts)
+  k4u32x4 q[NP][KS];
+  const TileRow tr = wk.row(row0 + col);
+  load_queries<NP, KS>((const T*)a.q + tr.row * a.q_stride + tr.head * HD + half * (HD / 2), tr.live, q);
+  const int lim = wk.limit(tr);
+  int lo = tr.live ? lim : len, hi = tr.live ? lim : 0;
 #pragma unroll
   for (int m = 1; m < 32; m *= 2) lo = min(lo, __shfl_xor(lo, m)), hi = max(hi, __shfl_xor(hi, m));
   lo = __builtin_amdgcn_readfirstlane(lo);
   hi = __builtin_amdgcn_readfirstlane(hi);
-  auto steps_to = [&](int seen) {
-    const int end = min(min(span0 + clients.span, len), seen);
-    return end > span0 ? (end - span0 + 31) / 32 : 0;
-  };
   if (lane == 0) word[w] = hi;  // all waves walk as far as one of them has to
   __syncthreads();
 #pragma unroll
   for (int ww = 0; ww < WAVES; ++ww) hi = max(hi, word[ww]);
-  const int rounds = (steps_to(__builtin_amdgcn_readfirstlane(hi)) + 1) / 2;  // of 64 tokens
+  const int end = min(min(span0 + clients.span, len), __builtin_amdgcn_readfirstlane(hi));
+  const int rounds = end > span0 ? (end - span0 + 63) / 64 : 0;
   __syncthreads();
 
-  // O^T; per row: -(running maximum) (infinity while nothing has been seen), the lane's own sum of weights
-  f32x16 acc[TILES][HT];
-  float neg_m[TILES], sum[TILES];
+  // O^T; the row's -(running maximum) (infinity while nothing has been seen), the lane's own sum of weights
+  f32x16 acc[1][HT];
+  float neg_m = INFINITY, sum = 0.f;
 #pragma unroll
-  for (int t = 0; t < TILES; ++t) {
-    neg_m[t] = INFINITY;
-    sum[t] = 0.f;
-#pragma unroll
-    for (int j = 0; j < HT; ++j) acc[t][j] = f32x16{};
-  }
+  for (int j = 0; j < HT; ++j) acc[0][j] = f32x16{};
   const LaneOffsets<HD> at(c, g), at_v(c, gv);
   const float c1 = kv4_scale<HD>();
 
-  // ---- this wave's block of a round ----
+  // ---- this wave's block of a round: requested two rounds before it is converted ----
   Codes k_raw[2], v_raw[2];  // of even rounds, of odd ones
   unsigned k_pow[2], v_pow[2];
   auto record = [&](int i) {
@@ -675,8 +668,8 @@ __global__ __launch_bounds__(kKv4WideWaves * 64, (alone<HD, T, TILES>() ? 1 : 2)
     v_raw[set] = *(const Codes*)(rec + at_v.v);
     v_pow[set] = *(const unsigned*)(rec + at_v.vp);
   };
-  // In pieces: an operand's registers of each go between two products.  (An LDS store of 16 bytes a lane takes 13 cycles of the
-  // compute unit, a load 4: a round's stores are spread over its two steps.)
+  // In pieces, so that little of each goes between two products.  (An LDS store of 16 bytes a lane takes 13 cycles of the compute unit,
+  // a load 4: a round's stores are spread over its two steps.)
   k4u32x4* key_to;
   k4u32x2* value_to;
   auto open_keys = [&](int i) { key_to = key_lds + (((i & 1) * 2 + (w >> 1)) * KS + (g & 1) * (KS / 2)) * 64 + (g >> 1) * 32 + (w & 1) * 16 + c; };
@@ -698,97 +691,92 @@ __global__ __launch_bounds__(kKv4WideWaves * 64, (alone<HD, T, TILES>() ? 1 : 2)
 
   // A step's weights as two operands a block: upper and lower parts.  Two sets: the step's, and those of the step before, whose
   // products are still to come.
-  unsigned up[2][TILES][2][4], low[2][TILES][2][4];
+  unsigned up[2][8], low[2][8];
 #pragma unroll
-  for (int t = 0; t < TILES; ++t)
-#pragma unroll
-    for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) up[1][t][tt][i] = low[1][t][tt][i] = 0u;
-  auto operand = [](const unsigned (&x)[4]) { return __builtin_bit_cast(bf16x8, k4u32x4{x[0], x[1], x[2], x[3]}); };
+  for (int x = 0; x < 8; ++x) up[1][x] = low[1][x] = 0u;
+  auto operand = [](const unsigned (&x)[8], int block) {
+    return __builtin_bit_cast(bf16x8, k4u32x4{x[4 * block], x[4 * block + 1], x[4 * block + 2], x[4 * block + 3]});
+  };
+
   k4u32x4 key[KS];
   auto step = [&](int n, auto second, auto odd) {
     constexpr int NOW = decltype(second)::value, BEFORE = 1 - NOW, NEXT = 1 - decltype(odd)::value;  // of a round's two steps; the next round's set
+    if constexpr (NOW == 0) open_keys(n / 2 + 1);
+    else open_values(n / 2 + 1, NEXT);
+    // Half of the next round's operands (behind the last round: nobody's).
+    auto convert = [&](int piece) {
+      if constexpr (NOW == 0) convert_keys(piece, NEXT);
+      else convert_values(piece, NEXT);
+    };
+    auto request = [&] {
+      if constexpr (NOW == 0) request_keys(n / 2 + 3, NEXT);
+      else request_values(n / 2 + 3, NEXT);
+    };
+    if (idle) {
+#pragma unroll
+      for (int piece = 0; piece < KS / 2; ++piece) convert(piece);
+      request();
+      return;
+    }
     const int tok0 = span0 + n * 32;
     const bool masked = tok0 + 32 > lo;  // (of the wave) some row does not see all 32 tokens
     const k4u32x4* from = value_lds + ((n == 0 ? 0 : n - 1) & 3) * HT * 2 * 64 + lane;  // (for the first step's weights of 0: its own)
     k4u32x4 value[2][HT];
-    f32x16 score[TILES][1];
-#pragma unroll
-    for (int t = 0; t < TILES; ++t) score[t][0] = f32x16{};
-    if constexpr (NOW == 0) open_keys(n / 2 + 1);
-    else open_values(n / 2 + 1, NEXT);
-    // Scores, and between them half of the next round's operands (behind the last round: nobody's).
+    f32x16 score[1][1];
+    score[0][0] = f32x16{};
 #pragma unroll
     for (int st = 0; st < KS; ++st) {
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int m = NP - 1; m >= 0; --m)
-#pragma unroll
-        for (int t = 0; t < TILES; ++t)
-          score[t][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, key[st]), __builtin_bit_cast(bf16x8, q[t][m][st]), score[t][0], 0, 0, 0);
+        score[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, key[st]), __builtin_bit_cast(bf16x8, q[m][st]), score[0][0], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
-      if (st % 2 == 0) {
-        if constexpr (NOW == 0) convert_keys(st / 2, NEXT);
-        else convert_values(st / 2, NEXT);
-      }
+      if (st % 2 == 0) convert(st / 2);
       if (st >= KS - HT) value[0][st - (KS - HT)] = from[(st - (KS - HT)) * 2 * 64];
     }
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (NOW == 0) request_keys(n / 2 + 3, NEXT);
-    else request_values(n / 2 + 3, NEXT);
+    request();
     settle<ALONE>(score);
-    float sc[TILES][16];
+    float sc[16];
 #pragma unroll
-    for (int t = 0; t < TILES; ++t)
-#pragma unroll
-      for (int j = 0; j < 16; ++j) sc[t][j] = plain(score[t][0][j]);
+    for (int j = 0; j < 16; ++j) sc[j] = plain(score[0][0][j]);
     if (masked) {
 #pragma unroll
-      for (int t = 0; t < TILES; ++t)
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-          if (tok0 + (j >> 2) * 8 + half * 4 + (j & 3) >= lim[t]) sc[t][j] = -INFINITY;
+      for (int j = 0; j < 16; ++j)
+        if (tok0 + (j >> 2) * 8 + half * 4 + (j & 3) >= lim) sc[j] = -INFINITY;
     }
-    // The step before's products, and between them two weights of this step at a time (and the lower parts of the two before).
-    constexpr int PAIRS = 8 * TILES, EACH = HT / 2;  // products for each pair
-    float total[TILES], p[2];
-#pragma unroll
-    for (int t = 0; t < TILES; ++t) total[t] = 0.f;
-    auto pair = [&](int x) -> unsigned& { return up[NOW][x / 4 % TILES][x / (4 * TILES)][x % 4]; };
-    auto pair_low = [&](int x) -> unsigned& { return low[NOW][x / 4 % TILES][x / (4 * TILES)][x % 4]; };
-    auto score_of = [&](int x, int k) { return sc[x / 4 % TILES][x / (4 * TILES) * 8 + x % 4 * 2 + k]; };
-    auto raise = [&](int x) {  // the weights of pair x
-      const float neg = neg_m[x / 4 % TILES];
-      p[0] = __builtin_amdgcn_exp2f(fmaf(score_of(x, 0), c1, neg));
-      p[1] = __builtin_amdgcn_exp2f(fmaf(score_of(x, 1), c1, neg));
+    // The step before's products, and between them two weights of this step at a time; a step's last keys are read for the next.
+    constexpr int EACH = HT / 2;  // products for each pair of weights
+    float total = 0.f, p[2];
+    auto weigh = [&](int x, float neg) {
+      p[0] = __builtin_amdgcn_exp2f(fmaf(sc[2 * x], c1, neg));
+      p[1] = __builtin_amdgcn_exp2f(fmaf(sc[2 * x + 1], c1, neg));
     };
-    raise(0);
+    auto keep = [&](int x) {
+      up[NOW][x] = pack2_bf16(p[0], p[1]);
+      low[NOW][x] = lower_pair(p[0], p[1], up[NOW][x]);
+      total += p[0] + p[1];
+    };
+    weigh(0, neg_m);
     const k4u32x4* keys = key_lds + ((n + 1) & 3) * KS * 64 + lane;
     unsigned long long move = 0;
 #pragma unroll
-    for (int x = 0; x < PAIRS; ++x) {
+    for (int x = 0; x < 8; ++x) {
 #pragma unroll
       for (int k = 0; k < EACH; ++k) {
-        const int y = x * EACH + k, block = y / (2 * HT * TILES), lower = y / (HT * TILES) % 2, j = y / TILES % HT, tile = y % TILES;
+        const int y = x * EACH + k, block = y / (2 * HT), lower = y / HT % 2, j = y % HT;
         __builtin_amdgcn_sched_barrier(0);
-        acc[tile][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, value[block][j]),
-                                                              operand(lower ? low[BEFORE][tile][block] : up[BEFORE][tile][block]), acc[tile][j], 0, 0, 0);
+        acc[0][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, value[block][j]), operand(lower ? low[BEFORE] : up[BEFORE], block),
+                                                           acc[0][j], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
         if (k == 0) {
-          pair(x) = pack2_bf16(p[0], p[1]);
-          pair_low(x) = lower_pair(p[0], p[1], pair(x));
-          total[x / 4 % TILES] += p[0] + p[1];
+          keep(x);
+          asm volatile("" ::"v"(low[NOW][x]));  // (here, not behind the branch below)
           if (x < HT) value[1][x] = from[(x * 2 + 1) * 64];
-          if (x >= PAIRS - KS) key[x - (PAIRS - KS)] = keys[(x - (PAIRS - KS)) * 64];
-          if (x == PAIRS - 1) {
-            bool far = false;
-#pragma unroll
-            for (int t = 0; t < TILES; ++t) far |= !(total[t] <= 4096.f);
-            move = __ballot(far);
-          }
+          if (x >= 8 - KS) key[x - (8 - KS)] = keys[(x - (8 - KS)) * 64];
+          if (x == 7) move = __ballot(!(total <= 4096.f));  // (before the last product: the branch need not wait for it)
         }
-        if (k == EACH - 1 && x + 1 < PAIRS) raise(x + 1);
+        if (k == EACH - 1 && x < 7) weigh(x + 1, neg_m);
       }
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -796,29 +784,22 @@ __global__ __launch_bounds__(kKv4WideWaves * 64, (alone<HD, T, TILES>() ? 1 : 2)
     // something for the first time: an infinite total, or none.
     if (move != 0) {
       settle<ALONE>(acc);
+      float top = max3(max3(sc[0], sc[1], sc[2]), max3(sc[3], sc[4], sc[5]), max3(sc[6], sc[7], sc[8]));
+      top = max3(top, max3(sc[9], sc[10], sc[11]), max3(sc[12], sc[13], max3(sc[14], sc[15], top)));
+      const float m_old = -neg_m, m_new = fmaxf(m_old, fold32(top, LaneMax{}) * c1);
+      const float alpha = m_new == m_old ? 1.f : __builtin_amdgcn_exp2f(m_old - m_new);
+      neg_m = -m_new;
+      sum *= alpha;
 #pragma unroll
-      for (int t = 0; t < TILES; ++t) {
-        float top = max3(max3(sc[t][0], sc[t][1], sc[t][2]), max3(sc[t][3], sc[t][4], sc[t][5]), max3(sc[t][6], sc[t][7], sc[t][8]));
-        top = max3(top, max3(sc[t][9], sc[t][10], sc[t][11]), max3(sc[t][12], sc[t][13], max3(sc[t][14], sc[t][15], top)));
-        const float m_old = -neg_m[t], m_new = fmaxf(m_old, fold32(top, LaneMax{}) * c1);
-        const float alpha = m_new == m_old ? 1.f : __builtin_amdgcn_exp2f(m_old - m_new);
-        neg_m[t] = -m_new;
-        sum[t] *= alpha;
+      for (int j = 0; j < HT; ++j) acc[0][j] *= alpha;
+      total = 0.f;
 #pragma unroll
-        for (int j = 0; j < HT; ++j) acc[t][j] *= alpha;
-        const float neg = m_new == -INFINITY ? 0.f : -m_new;
-        total[t] = 0.f;
-#pragma unroll
-        for (int x = 0; x < 8; ++x) {
-          const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[t][2 * x], c1, neg)), p1 = __builtin_amdgcn_exp2f(fmaf(sc[t][2 * x + 1], c1, neg));
-          total[t] += p0 + p1;
-          up[NOW][t][x / 4][x % 4] = pack2_bf16(p0, p1);
-          low[NOW][t][x / 4][x % 4] = lower_pair(p0, p1, up[NOW][t][x / 4][x % 4]);
-        }
+      for (int x = 0; x < 8; ++x) {
+        weigh(x, m_new == -INFINITY ? 0.f : -m_new);
+        keep(x);
       }
     }
-#pragma unroll
-    for (int t = 0; t < TILES; ++t) sum[t] += total[t];
+    sum += total;
   };
 
   if (rounds > 0) {
@@ -855,45 +836,45 @@ __global__ __launch_bounds__(kKv4WideWaves * 64, (alone<HD, T, TILES>() ? 1 : 2)
 #pragma unroll
       for (int j = 0; j < HT; ++j) {
         const bf16x8 value = __builtin_bit_cast(bf16x8, from[(j * 2 + block) * 64]);
-#pragma unroll
-        for (int t = 0; t < TILES; ++t) {
-          acc[t][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value, operand(up[1][t][block]), acc[t][j], 0, 0, 0);
-          acc[t][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value, operand(low[1][t][block]), acc[t][j], 0, 0, 0);
-        }
+        acc[0][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value, operand(up[1], block), acc[0][j], 0, 0, 0);
+        acc[0][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value, operand(low[1], block), acc[0][j], 0, 0, 0);
       }
     settle<ALONE>(acc);
   }
-  __syncthreads();  // (the words go where operands were)
+  if (idle) return;
 
-  // ---- rows, or a split's partial rows (written through) ----
+  // ---- rows, or a split's partial rows ----
+  const float m = -neg_m, l = fold32(sum, LaneAdd{});
+  float* dst = wk.all + ((size_t)it.split * WG_ROWS + w * 32 + col) * ROW;
 #pragma unroll
-  for (int t = 0; t < TILES; ++t) {
-    if (row0 + t * 32 >= wk.group_rows) break;
-    const float m = -neg_m[t], l = fold32(sum[t], LaneAdd{});
-    float* dst = wk.all + ((size_t)it.split * WG_ROWS + (w * TILES + t) * 32 + col) * ROW;
-    const bool live = row0 + t * 32 + col < wk.group_rows;
+  for (int u = 0; u < 2; ++u)
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int e = 0; e < HD / 16; e += 4) {  // of unit 8 u + 4 half + i
+        const int ch = (8 * u + 4 * half + i) * (HD / 16) + e;
+        f32x4 o;
 #pragma unroll
-        for (int e = 0; e < HD / 16; e += 4) {  // of unit 8 u + 4 half + i
-          const int ch = (8 * u + 4 * half + i) * (HD / 16) + e;
-          f32x4 o;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) o[k] = acc[t][(e + k) % HT][4 * (u + (e + k) / HT * 2) + i];
-          if (wk.nsplit == 1) wk.finish(row0 + t * 32 + col, ch, o, m, l);
-          else if (rounds > 0 && live) Xwg<true>::st4f(dst + ch, o);  // (nothing seen: nothing to read)
-        }
-    if (wk.nsplit > 1 && half == 0 && live) Xwg<true>::st4f(dst + HD, f32x4{m, l, 0.f, 0.f});
-  }
-  if (wk.nsplit == 1 || !wk.arrives_last(word)) return;
+        for (int k = 0; k < 4; ++k) o[k] = acc[0][(e + k) % HT][4 * (u + (e + k) / HT * 2) + i];
+        if (wk.nsplit == 1) wk.finish(row0 + col, ch, o, m, l);
+        else if (rounds > 0 && tr.live) *(f32x4*)(dst + ch) = o;  // (nothing seen: nothing to read)
+      }
+  if (wk.nsplit > 1 && half == 0 && tr.live) *(f32x2*)(dst + HD) = f32x2{m, l};
+}
 
-  // ---- the splits joined: a thread has 4 channels of a row at a time ----
-  constexpr int TPR = HD / 4, NT = WAVES * 64, BATCH = 8;
-  const int tasks = min(WG_ROWS, wk.group_rows - wk.first_row) * TPR;
+// The splits of many tiles joined: a group's splits have a workgroup each, as in the walk, for its share of the rows; a thread has 4
+// channels of a row at a time.  (By the walk's last workgroup alone, as with few tiles, 128 rows took 40 us.)
+template <int HD, typename T>
+__global__ __launch_bounds__(kKv4WideWaves * 64) void kv4_join_kernel(Kv4AttendCall a, Kv4Clients clients) {
+  constexpr int ROW = HD + kKv4PartPad, WG_ROWS = kKv4WideWaves * 32, TPR = HD / 4, NT = kKv4WideWaves * 64, BATCH = 8;
+  const int tid = threadIdx.x;
+  const Kv4Item it = find_item(clients, blockIdx.y, tid & 63);
+  const Work<HD, T> wk(a, clients, it, blockIdx.x, WG_ROWS / 16);
+  if (wk.nsplit == 1) return;
+  const int share = (WG_ROWS + wk.nsplit - 1) / wk.nsplit, from = it.split * share;
+  const int tasks = min(share, min(WG_ROWS, wk.group_rows - wk.first_row) - from) * TPR;
   for (int task = tid; task < tasks; task += NT) {
-    const int mr = task / TPR, e0 = (task % TPR) * 4;
+    const int mr = from + task / TPR, e0 = (task % TPR) * 4;
     const float* p0 = wk.all + (size_t)mr * ROW;
     float m = -INFINITY, l = 0.f;
     f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -947,9 +928,14 @@ static hipError_t attend_few(const Kv4AttendCall& c, const Kv4Clients& cl, hipSt
 template <int HD, typename T>
 static hipError_t attend_of(const Kv4AttendCall& c, const Kv4Launch& l, hipStream_t st) {
   static std::atomic<uint64_t> allowed{0};
-  if (l.wide)
-    return allow_and_launch(kv4_attend_many_kernel<HD, T, kv4_wide_tiles(sizeof(T) == 4 ? PIPESD_F32 : PIPESD_BF16, HD) / 2>, allowed,
-                            many_lds_bytes<HD>(), kKv4WideWaves * 64, c, l.c, st);
+  if (l.wide) {
+    const hipError_t e = allow_and_launch(kv4_attend_many_kernel<HD, T>, allowed, many_lds_bytes<HD>(), kKv4WideWaves * 64, c, l.c, st);
+    bool split = false;
+    for (int i = 0; i < l.c.n; ++i) split |= l.c.nsplit[i] > 1;
+    if (e != hipSuccess || !split) return e;
+    kv4_join_kernel<HD, T><<<dim3(c.view.n_kv_heads, l.c.items), kKv4WideWaves * 64, 0, st>>>(c, l.c);
+    return hipGetLastError();
+  }
   if (l.tiles == 1) return attend_few<HD, T, 1>(c, l.c, st);
   if constexpr (sizeof(T) == 2)
     if (l.tiles == 2) return attend_few<HD, T, 2>(c, l.c, st);

@@ -43,10 +43,9 @@ __device__ __forceinline__ int64_t kv4_record(const Kv4View& v, int layer, int b
 // group, head rr % group of the group; 16 of them make a tile.
 //   few tiles    the waves of a workgroup take every WAVES-th 32 tokens of a span for the same one or two tiles, and
 //                join their sums
-//   many tiles   each of four waves takes tiles of its own
-constexpr int kKv4ManyTiles = 16;  // (from here on)
+//   many tiles   each of four waves takes two tiles of its own, over tokens that they convert together
 constexpr int kKv4WideWaves = 4;
-constexpr int kv4_wide_tiles(int dtype, int head_dim) { return dtype == PIPESD_BF16 && head_dim == 64 ? 4 : 2; }  // of a wave
+constexpr int kKv4WideTiles = 2 * kKv4WideWaves;  // of a workgroup
 constexpr int kKv4MaxSplits = 64;
 constexpr int kv4_few_waves(int tiles) { return tiles == 1 ? 8 : 4; }
 
@@ -66,21 +65,30 @@ struct Kv4Client {
   int32_t seq, n_rows, row_off, len;
 };
 struct Kv4Launch {
-  int32_t wide, tiles;  // tiles: of a workgroup (few), of a wave (many)
+  int32_t wide, tiles;  // tiles: of a workgroup
   Kv4Clients c;
 };
 struct Kv4PlanNeeds {
   size_t part_tiles, counters;
 };
 
-// One tile a workgroup or two.  Two share the conversion of keys and values (a step of 32 tokens takes 1.5 times as long, not
-// twice), but leave registers for half the waves and twice the rows to join: measured on a device of 256 compute units, a
-// launch takes 8 us + 0.14 us per step and compute unit of one tile, 14 us + 0.215 us of two (head dim 64: 0.086 and 0.10).
-// Two in fp32 were never faster: 4 clients of 9 rows behind 4096 tokens 32.9 us, 21.9 with one.
-inline int kv4_few_tiles(int dtype, int head_dim, double work1, double work2, int n_cu) {
-  if (dtype == PIPESD_F32) return 1;
-  const double one = head_dim == 128 ? 0.14 : 0.086, two = head_dim == 128 ? 0.215 : 0.10;
-  return 8 + one * work1 / n_cu <= 14 + two * work2 / n_cu ? 1 : 2;
+// What a launch takes on a device of 256 compute units, in us: `start`, and `step` for each 32 tokens of a workgroup's tiles and
+// compute unit.  Two tiles in a workgroup share the conversion of keys and values, but leave registers for half the waves; eight share it
+// through LDS, four times as many rows to join.  Measured, query heads 4 to a cache head: 4 clients of 8 rows behind 2048 tokens 13.5 us
+// with one tile, 18.2 with two; 32 clients behind 4096 46.6 and 45.0; 32 rows behind 65536 tokens 67 with two, 71 with eight; 2048 rows behind 6144
+// of head dim 64 225 with two, 186 with eight, of head dim 128 349 and 265.  Two in fp32 were never faster: 4 clients of 9 rows behind 4096 tokens 32.9 us, 21.9 with one.
+struct Kv4Cost {
+  double start, step;
+};
+constexpr Kv4Cost kv4_cost(int tiles, int dtype, int head_dim) {
+  if (dtype == PIPESD_F32) {
+    if (tiles == 2) return Kv4Cost{1e30, 1e30};
+    if (tiles == 1) return head_dim == 128 ? Kv4Cost{12, 0.15} : Kv4Cost{10, 0.105};
+    return head_dim == 128 ? Kv4Cost{25, 1.1} : Kv4Cost{18, 0.7};
+  }
+  if (tiles == 1) return head_dim == 128 ? Kv4Cost{8, 0.14} : Kv4Cost{8, 0.086};
+  if (tiles == 2) return head_dim == 128 ? Kv4Cost{14, 0.185} : Kv4Cost{13, 0.12};
+  return head_dim == 128 ? Kv4Cost{24, 0.6} : Kv4Cost{18, 0.39};
 }
 
 // The launches of a pass: clients of few and of many tiles apart, at most kKv4ClientsPerLaunch in one.  All splits of a kind
@@ -91,32 +99,40 @@ inline Kv4PlanNeeds kv4_plan(const Kv4Client* cl, int n, int dtype, int head_dim
   out.clear();
   const int group = n_q_heads / n_kv_heads;
   Kv4PlanNeeds need{0, 0};
+  const Kv4Cost one = kv4_cost(1, dtype, head_dim), two = kv4_cost(2, dtype, head_dim), eight = kv4_cost(kKv4WideTiles, dtype, head_dim);
+  auto tiles_of = [&](const Kv4Client& c) { return attn_query_tiles(group, c.n_rows); };
+  auto sets = [&](const Kv4Client& c, int tiles) { return (tiles_of(c) + tiles - 1) / tiles; };
+  // Many tiles: clients whose steps are cheaper so, if together they save what the other launch costs.
+  auto gain = [&](const Kv4Client& c) { return std::min(one.step * sets(c, 1), two.step * sets(c, 2)) - eight.step * sets(c, kKv4WideTiles); };
+  double saved = 0;
+  bool few = false;
+  for (int i = 0; i < n; ++i) {
+    if (cl[i].n_rows > 0 && gain(cl[i]) > 0) saved += gain(cl[i]) * n_kv_heads * cl[i].len / 32 / n_cu;
+    else few |= cl[i].n_rows > 0;
+  }
+  const bool any_wide = saved > eight.start - (few ? 0 : one.start);
   for (int wide = 0; wide < 2; ++wide) {
-    auto tiles_of = [&](const Kv4Client& c) { return attn_query_tiles(group, c.n_rows); };
-    auto mine = [&](const Kv4Client& c) { return c.n_rows > 0 && (tiles_of(c) >= kKv4ManyTiles) == (wide != 0); };
+    auto mine = [&](const Kv4Client& c) { return c.n_rows > 0 && (any_wide && gain(c) > 0) == (wide != 0); };
     int longest = 0;
-    double work[3] = {0, 0, 0};  // [tiles]: steps of 32 tokens of all workgroups' sets of tiles
+    double work1 = 0, work2 = 0;  // steps of 32 tokens of all workgroups, of one tile and of two
     for (int i = 0; i < n; ++i) {
       if (!mine(cl[i])) continue;
       longest = std::max(longest, (int)cl[i].len);
-      for (int tiles = 1; tiles <= 2; ++tiles) work[tiles] += (double)n_kv_heads * ((tiles_of(cl[i]) + tiles - 1) / tiles) * cl[i].len / 32;
+      work1 += (double)n_kv_heads * sets(cl[i], 1) * cl[i].len / 32;
+      work2 += (double)n_kv_heads * sets(cl[i], 2) * cl[i].len / 32;
     }
     if (longest == 0) continue;
-    int tiles, wg_tiles, step, resident = 2;  // resident: workgroups that a compute unit holds at once
+    int wg_tiles = kKv4WideTiles, step = 256, resident = 2;  // resident: workgroups that a compute unit holds at once
     if (wide) {
-      tiles = kv4_wide_tiles(dtype, head_dim);
-      wg_tiles = kKv4WideWaves * tiles;
-      step = 512;
       if (head_dim == 128 && dtype == PIPESD_F32) resident = 1;
     } else {
-      tiles = kv4_few_tiles(dtype, head_dim, work[1], work[2], n_cu);
-      wg_tiles = tiles;
-      step = kv4_few_waves(tiles) * 32;
+      wg_tiles = one.start + one.step * work1 / n_cu <= two.start + two.step * work2 / n_cu ? 1 : 2;
+      step = kv4_few_waves(wg_tiles) * 32;
     }
     auto workgroups = [&](int64_t span) {
       int64_t w = 0;
       for (int i = 0; i < n; ++i)
-        if (mine(cl[i])) w += (int64_t)n_kv_heads * ((tiles_of(cl[i]) + wg_tiles - 1) / wg_tiles) * ((cl[i].len + span - 1) / span);
+        if (mine(cl[i])) w += (int64_t)n_kv_heads * sets(cl[i], wg_tiles) * ((cl[i].len + span - 1) / span);
       return w;
     };
     // (a split costs what joins it, about the time of three steps: none below 768 tokens)
@@ -138,14 +154,14 @@ inline Kv4PlanNeeds kv4_plan(const Kv4Client* cl, int n, int dtype, int head_dim
       if (l.c.n == kKv4ClientsPerLaunch) flush();
       const int j = l.c.n++;
       l.wide = wide;
-      l.tiles = tiles;
+      l.tiles = wg_tiles;
       l.c.span = (int)span;
       l.c.first[j] = l.c.items;
       l.c.seq[j] = cl[i].seq;
       l.c.len[j] = cl[i].len;
       l.c.n_rows[j] = cl[i].n_rows;
       l.c.row_off[j] = cl[i].row_off;
-      l.c.groups[j] = (tiles_of(cl[i]) + wg_tiles - 1) / wg_tiles;
+      l.c.groups[j] = sets(cl[i], wg_tiles);
       l.c.nsplit[j] = (int)((cl[i].len + span - 1) / span);
       l.c.items += l.c.groups[j] * l.c.nsplit[j];
       l.c.part_off[j] = (int)need.part_tiles;
