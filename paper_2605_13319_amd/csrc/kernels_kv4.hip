@@ -224,7 +224,7 @@ hipError_t launch_kv4_read(int dtype, int head_dim, const Kv4View& v, int layer0
 // Workgroup (cache head, layer, client).  Of the tokens before the newest `recent` the keep - recent heaviest stay, the
 // lower index first among equals: the weights as integers in their order, the (keep - recent)-th largest found 8 bits at
 // a time from the counts of each value of the 8 bits, then one walk in order that numbers the tokens that stay.
-constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64, kSelPer = 4;
+constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64, kSelPer = 4, kSelHold = 8;
 
 // order of floats as an order of integers; NaN counts as 0, as does -0
 __device__ __forceinline__ uint32_t weight_key(float x) {
@@ -250,12 +250,32 @@ __global__ __launch_bounds__(kSelThreads) void kv4_select_kernel(Kv4Cuts c, int 
   // threshold: keys above it stay, and the first `ties` of those equal to it
   uint32_t prefix = 0, mask = 0, left = (uint32_t)want;
   if (want > 0 && want < old) {
+    // (the first kSelHold a thread stay in registers; what is behind comes again for every digit, as many requested at once)
+    float held[kSelHold];
+    auto load = [&](int t0, float (&x)[kSelHold]) {
+#pragma unroll
+      for (int i = 0; i < kSelHold; ++i) {
+        const int t = t0 + i * kSelThreads + tid;
+        x[i] = src[min(t, old - 1)];
+      }
+    };
+    auto add = [&](int t0, const float (&x)[kSelHold], int shift) {
+#pragma unroll
+      for (int i = 0; i < kSelHold; ++i) {
+        if (t0 + i * kSelThreads >= old) break;
+        const uint32_t key = weight_key(x[i]);
+        if (t0 + i * kSelThreads + tid < old && (key & mask) == prefix) atomicAdd(&count[(key >> shift) & 255u], 1u);
+      }
+    };
+    load(0, held);
     for (int shift = 24; shift >= 0; shift -= 8) {
       if (tid < 256) count[tid] = 0;
       __syncthreads();
-      for (int t = tid; t < old; t += kSelThreads) {
-        const uint32_t key = weight_key(src[t]);
-        if ((key & mask) == prefix) atomicAdd(&count[(key >> shift) & 255u], 1u);
+      add(0, held, shift);
+      for (int t0 = kSelHold * kSelThreads; t0 < old; t0 += kSelHold * kSelThreads) {
+        float x[kSelHold];
+        load(t0, x);
+        add(t0, x, shift);
       }
       __syncthreads();
       if (tid < 64) {  // lane l: digits 255 - 4 l down to 252 - 4 l

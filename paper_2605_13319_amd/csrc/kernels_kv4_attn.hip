@@ -308,6 +308,10 @@ __device__ __forceinline__ void hide(float (&sc)[8], int tok, int lim) {  // tok
   for (int i = 0; i < 8; ++i)
     if (tok + (i >> 2) * 16 + (i & 3) >= lim) sc[i] = -INFINITY;
 }
+// What a split leaves as its row's maximum.  None means that it saw nothing and is passed over; a row of NaN, whose maximum never
+// moves, must not be.
+__device__ __forceinline__ float partial_maximum(float m, float l) { return l != l ? INFINITY : m; }
+
 template <int N, int HT>
 __device__ __forceinline__ void settle(Running<HT> (&x)[N]) {
   f32x4 acc[N][HT];
@@ -516,7 +520,7 @@ __global__ __launch_bounds__(WAVES * 64, TILES == 1 ? 4 : 2) void kv4_attend_ker
     } else {
       float* dst = wk.all + ((size_t)it.split * ROWS + mr) * ROW;
       Xwg<true>::st4f(dst + e0, o);
-      if (e0 == 0) Xwg<true>::st4f(dst + HD, f32x4{m, l, 0.f, 0.f});
+      if (e0 == 0) Xwg<true>::st4f(dst + HD, f32x4{partial_maximum(m, l), l, 0.f, 0.f});
     }
   }
   if (wk.nsplit == 1 || !wk.arrives_last(word)) return;
@@ -859,7 +863,7 @@ __global__ __launch_bounds__(kKv4WideWaves * 64, (alone<HD, T>() ? 1 : 2)) void 
         if (wk.nsplit == 1) wk.finish(row0 + col, ch, o, m, l);
         else if (rounds > 0 && tr.live) *(f32x4*)(dst + ch) = o;  // (nothing seen: nothing to read)
       }
-  if (wk.nsplit > 1 && half == 0 && tr.live) *(f32x2*)(dst + HD) = f32x2{m, l};
+  if (wk.nsplit > 1 && half == 0 && tr.live) *(f32x2*)(dst + HD) = f32x2{partial_maximum(m, l), l};
 }
 
 // The splits of many tiles joined: a group's splits have a workgroup each, as in the walk, for its share of the rows; a thread has 4

@@ -138,7 +138,7 @@ inline Kv4PlanNeeds kv4_plan(const Kv4Client* cl, int n, int dtype, int head_dim
     // (a split costs what joins it, about the time of three steps: none below 768 tokens)
     const int64_t room = (int64_t)resident * n_cu;
     int64_t span = std::max<int64_t>(step, longest <= 768 ? longest : 0);
-    span = std::max<int64_t>(span, (int64_t)(workgroups(1) / room));  // (no shorter one would do)
+    span = std::max<int64_t>(span, std::min<int64_t>(workgroups(1) / room, longest));  // (no shorter one would do)
     span = (span + step - 1) / step * step;
     while (workgroups(span) > room && span < longest) span += span < 16 * step ? step : span / 16 / step * step;
     span = std::max<int64_t>(span, ((longest + kKv4MaxSplits - 1) / kKv4MaxSplits + step - 1) / step * step);
