@@ -387,7 +387,8 @@ size_t pipesd_kv4_block_bytes(const pipesd_config *cfg, int32_t block_tokens);
 /* Cache of up to max_seqs clients over a caller-allocated device pool of floor(pool_bytes / block bytes) blocks (borrowed until
  * pipesd_kv4_destroy).  Of the config it takes n_layers, n_q_heads, n_kv_heads (at most 256
  * query heads each), head_dim (64 or 128) and dtype.  Beside the
- * pool it allocates the block tables and what passes of up to PIPESD_MAX_ROWS rows by 16 clients need.  pool == NULL: bookkeeping only.
+ * pool it allocates the block tables and what passes of up to PIPESD_MAX_ROWS rows by 16 clients take at the lengths that the
+ * pool allows.  pool == NULL: bookkeeping only.
  * EINVAL: an unsupported config, block_tokens != 16, max_seqs < 1, no room for one block, a pool that is not 256-byte
  * aligned or of 2^31 tokens or table entries (2 * max_seqs * blocks) and more; ENOMEM: an allocation failed. */
 int pipesd_kv4_create(const pipesd_config *cfg, int32_t max_seqs, int32_t block_tokens, void *pool, size_t pool_bytes,
@@ -413,7 +414,8 @@ int pipesd_kv4_append(pipesd_kv4 *kv, int32_t layer, const void *k, int64_t k_st
  *           each client of the pass, at this layer, mass[t] = decay * mass[t] + (sum of token t's weights over the client's rows
  *           and the query heads of the cache head), 0 <= decay <= 1; the pass's own tokens, and all with decay 0, start at 0
  *           whatever the buffer held.
- * A row's result depends on its client and, in which order sums are formed, on the most rows that a client of the pass has.
+ * A row's result depends on its own client's tokens and queries alone.  Into how many pieces a context is cut, and so the
+ * order of sums, goes by the lengths and numbers of rows of all clients of the pass; the same pass gives the same bits.
  * EINVAL: also a client longer than mass_stride, or a decay outside [0, 1]; ESTATE: no pass that can attend, no pool. */
 int pipesd_kv4_attend(pipesd_kv4 *kv, int32_t layer, const void *q, int64_t q_stride, const int32_t *limits, void *out,
                       int64_t out_stride, float *mass, int64_t mass_stride, float decay, void *stream);
