@@ -523,7 +523,7 @@ __global__ __launch_bounds__(WAVES * 64, TILES == 1 ? 4 : 2) void kv4_attend_ker
       if (e0 == 0) Xwg<true>::st4f(dst + HD, f32x4{partial_maximum(m, l), l, 0.f, 0.f});
     }
   }
-  if (wk.nsplit == 1 || !wk.arrives_last(word)) return;
+  if (wk.nsplit == 1 || clients.apart || !wk.arrives_last(word)) return;
 
   // ---- the splits joined ----
   // Their maxima and sums come to LDS at once; each thread then has a task, or several one after the other, and takes its
@@ -866,49 +866,74 @@ __global__ __launch_bounds__(kKv4WideWaves * 64, (alone<HD, T>() ? 1 : 2)) void 
   if (wk.nsplit > 1 && half == 0 && tr.live) *(f32x2*)(dst + HD) = f32x2{partial_maximum(m, l), l};
 }
 
-// The splits of many tiles joined: a group's splits have a workgroup each, as in the walk, for its share of the rows; a thread has 4
-// channels of a row at a time.  (By the walk's last workgroup alone, as with few tiles, 128 rows took 40 us.)
-template <int HD, typename T>
-__global__ __launch_bounds__(kKv4WideWaves * 64) void kv4_join_kernel(Kv4AttendCall a, Kv4Clients clients) {
-  constexpr int ROW = HD + kKv4PartPad, WG_ROWS = kKv4WideWaves * 32, TPR = HD / 4, NT = kKv4WideWaves * 64, BATCH = 8;
+// ---- the splits of a group of tiles joined by a kernel of its own: a group's splits have a workgroup each, as in the walk, for its share
+// of the rows.  What a join takes is the way to memory, 1.7 us for a thread's next 8 splits of its next 4 channels: by the walk's last
+// workgroup alone (which starts 2 us sooner) 16 splits of 32 rows took 13 us, 8 of 128 rows 40. ----
+// Partial sums of splits s0, s0 + step, .. added to a row's.
+template <int N>
+__device__ __forceinline__ void add_splits(const f32x4 (&ob)[N], const f32x2 (&ml)[N], int s0, int step, int nsplit, float& m, float& l, f32x4& o) {
+  float m_new = m;
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    if (s0 + j * step < nsplit) m_new = fmaxf(m_new, ml[j].x);
+  if (m_new == -INFINITY) return;
+  const float alpha = m_new == m ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+  l *= alpha;
+  o *= alpha;
+  m = m_new;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    if (s0 + j * step >= nsplit || ml[j].x == -INFINITY) continue;  // (a split that saw nothing may have written no values)
+    const float sw = __builtin_amdgcn_exp2f(ml[j].x - m);
+    l += ml[j].y * sw;
+    o += ob[j] * sw;
+  }
+}
+// A thread has 4 channels of a row (a task); threads that the tasks leave over share a task's splits: thread (share, task) takes splits
+// share, share + shares, .., 8 at a time, and the shares are joined through LDS in order.
+template <int HD, typename T, int WG_ROWS>
+__global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttendCall a, Kv4Clients clients) {
+  constexpr int ROW = HD + kKv4PartPad, TPR = HD / 4, NT = 256, BATCH = 8;
+  __shared__ float joined[NT * 6];
   const int tid = threadIdx.x;
   const Kv4Item it = find_item(clients, blockIdx.y, tid & 63);
   const Work<HD, T> wk(a, clients, it, blockIdx.x, WG_ROWS / 16);
   if (wk.nsplit == 1) return;
-  const int share = (WG_ROWS + wk.nsplit - 1) / wk.nsplit, from = it.split * share;
-  const int tasks = min(share, min(WG_ROWS, wk.group_rows - wk.first_row) - from) * TPR;
-  for (int task = tid; task < tasks; task += NT) {
-    const int mr = from + task / TPR, e0 = (task % TPR) * 4;
+  const int per = (WG_ROWS + wk.nsplit - 1) / wk.nsplit, from = it.split * per;
+  const int tasks = min(per, min(WG_ROWS, wk.group_rows - wk.first_row) - from) * TPR;
+  if (tasks <= 0) return;
+  int log_tasks = 31 - __builtin_clz(TPR);  // (their number made a power of two)
+  while ((1 << log_tasks) < tasks) ++log_tasks;
+  const int shares = max(1, NT >> log_tasks), share = shares > 1 ? tid >> log_tasks : 0;
+#pragma unroll 1
+  for (int k0 = 0; k0 < tasks; k0 += NT) {
+    const int task = k0 + (tid & ((1 << log_tasks) - 1)), mr = from + min(task, tasks - 1) / TPR, e0 = (task % TPR) * 4;
     const float* p0 = wk.all + (size_t)mr * ROW;
     float m = -INFINITY, l = 0.f;
     f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < wk.nsplit; s0 += BATCH) {
+    for (int s0 = share; s0 < wk.nsplit; s0 += BATCH * shares) {
       f32x4 ob[BATCH];
       f32x2 ml[BATCH];
 #pragma unroll
       for (int j = 0; j < BATCH; ++j) {
-        const float* ps = p0 + (size_t)min(s0 + j, wk.nsplit - 1) * (WG_ROWS * ROW);
+        const float* ps = p0 + (size_t)min(s0 + j * shares, wk.nsplit - 1) * (WG_ROWS * ROW);
         ml[j] = *(const f32x2*)(ps + HD);
         ob[j] = *(const f32x4*)(ps + e0);
       }
-      float m_new = m;
-#pragma unroll
-      for (int j = 0; j < BATCH; ++j)
-        if (s0 + j < wk.nsplit) m_new = fmaxf(m_new, ml[j].x);
-      if (m_new == -INFINITY) continue;
-      const float alpha = __builtin_amdgcn_exp2f(m - m_new);
-      l *= alpha;
-      o *= alpha;
-      m = m_new;
-#pragma unroll
-      for (int j = 0; j < BATCH; ++j) {
-        if (s0 + j >= wk.nsplit || ml[j].x == -INFINITY) continue;  // (a split that saw nothing wrote no values)
-        const float sw = __builtin_amdgcn_exp2f(ml[j].x - m);
-        l += ml[j].y * sw;
-        o += ob[j] * sw;
+      add_splits(ob, ml, s0, shares, wk.nsplit, m, l, o);
+    }
+    if (shares > 1) {  // (then this is the only turn)
+      float* x = joined + tid * 6;
+      x[0] = o[0], x[1] = o[1], x[2] = o[2], x[3] = o[3], x[4] = l, x[5] = m;
+      __syncthreads();
+      for (int sh = 1; share == 0 && sh < shares; ++sh) {
+        const float* y = joined + ((sh << log_tasks) + tid) * 6;
+        const f32x4 one_o[1] = {f32x4{y[0], y[1], y[2], y[3]}};
+        const f32x2 one_ml[1] = {f32x2{y[5], y[4]}};
+        add_splits(one_o, one_ml, 0, 1, 1, m, l, o);
       }
     }
-    wk.finish(wk.first_row + mr, e0, o, m, l);
+    if (share == 0 && task < tasks) wk.finish(wk.first_row + mr, e0, o, m, l);
   }
 }
 
@@ -923,23 +948,25 @@ static hipError_t allow_and_launch(K kernel, std::atomic<uint64_t>& allowed, siz
   kernel<<<dim3(c.view.n_kv_heads, cl.items), threads, lds, st>>>(c, cl);
   return hipGetLastError();
 }
+template <int HD, typename T, int WG_ROWS>
+static hipError_t join(hipError_t e, const Kv4AttendCall& c, const Kv4Clients& cl, hipStream_t st) {
+  if (e != hipSuccess || !cl.apart) return e;
+  kv4_join_kernel<HD, T, WG_ROWS><<<dim3(c.view.n_kv_heads, cl.items), 256, 0, st>>>(c, cl);
+  return hipGetLastError();
+}
 template <int HD, typename T, int TILES>
 static hipError_t attend_few(const Kv4AttendCall& c, const Kv4Clients& cl, hipStream_t st) {
   static std::atomic<uint64_t> allowed{0};
   constexpr int WAVES = kv4_few_waves(TILES);
-  return allow_and_launch(kv4_attend_kernel<HD, T, TILES, WAVES>, allowed, few_lds_bytes<HD, T, TILES, WAVES>(), WAVES * 64, c, cl, st);
+  return join<HD, T, TILES * 16>(
+      allow_and_launch(kv4_attend_kernel<HD, T, TILES, WAVES>, allowed, few_lds_bytes<HD, T, TILES, WAVES>(), WAVES * 64, c, cl, st), c, cl, st);
 }
 template <int HD, typename T>
 static hipError_t attend_of(const Kv4AttendCall& c, const Kv4Launch& l, hipStream_t st) {
   static std::atomic<uint64_t> allowed{0};
-  if (l.wide) {
-    const hipError_t e = allow_and_launch(kv4_attend_many_kernel<HD, T>, allowed, many_lds_bytes<HD>(), kKv4WideWaves * 64, c, l.c, st);
-    bool split = false;
-    for (int i = 0; i < l.c.n; ++i) split |= l.c.nsplit[i] > 1;
-    if (e != hipSuccess || !split) return e;
-    kv4_join_kernel<HD, T><<<dim3(c.view.n_kv_heads, l.c.items), kKv4WideWaves * 64, 0, st>>>(c, l.c);
-    return hipGetLastError();
-  }
+  if (l.wide)
+    return join<HD, T, kKv4WideTiles * 16>(
+        allow_and_launch(kv4_attend_many_kernel<HD, T>, allowed, many_lds_bytes<HD>(), kKv4WideWaves * 64, c, l.c, st), c, l.c, st);
   if (l.tiles == 1) return attend_few<HD, T, 1>(c, l.c, st);
   if constexpr (sizeof(T) == 2)
     if (l.tiles == 2) return attend_few<HD, T, 2>(c, l.c, st);

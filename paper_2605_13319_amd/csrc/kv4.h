@@ -54,6 +54,7 @@ constexpr int kv4_few_waves(int tiles) { return tiles == 1 ? 8 : 4; }
 constexpr int kKv4ClientsPerLaunch = 32;
 struct Kv4Clients {
   int32_t n, items, span;  // span: tokens of a split
+  int32_t apart;           // splits are joined by a kernel of their own, not by their last workgroup
   int32_t first[kKv4ClientsPerLaunch];  // item (beyond the last client: the number of items)
   int32_t seq[kKv4ClientsPerLaunch], table_off[kKv4ClientsPerLaunch], len[kKv4ClientsPerLaunch];  // len: with the pass's own rows
   int32_t n_rows[kKv4ClientsPerLaunch], row_off[kKv4ClientsPerLaunch];
@@ -146,6 +147,14 @@ inline Kv4PlanNeeds kv4_plan(const Kv4Client* cl, int n, int dtype, int head_dim
     auto flush = [&] {
       if (l.c.n == 0) return;
       for (int i = l.c.n; i < kKv4ClientsPerLaunch; ++i) l.c.first[i] = l.c.items;
+      for (int i = 0; i < l.c.n; ++i) {  // (few tiles: where the last workgroup would go to memory 4 times and more.  4 rows
+        // behind 20000 tokens: 15.3 us apart, 17.2 not; 4 such clients, 2 times: 26.3 and 24.9)
+        const int threads = kv4_few_waves(wg_tiles) * 64, tasks = std::min(group * l.c.n_rows[i], wg_tiles * 16) * (head_dim / 4);
+        int shares = 1;
+        while (2 * shares * tasks <= threads) shares *= 2;
+        const int turns = (tasks + threads - 1) / threads * ((l.c.nsplit[i] + 8 * shares - 1) / (8 * shares));
+        if (l.c.nsplit[i] > 1 && (wide || turns > 3)) l.c.apart = 1;
+      }
       out.push_back(l);
       l = Kv4Launch{};
     };
