@@ -385,7 +385,7 @@ __global__ __launch_bounds__(WAVES * 64, TILES == 1 ? 4 : 2) void kv4_attend_ker
   for (int m = 1; m < 16; m *= 2) lo = min(lo, __shfl_xor(lo, m)), hi = max(hi, __shfl_xor(hi, m));
   lo = __builtin_amdgcn_readfirstlane(lo);
   hi = __builtin_amdgcn_readfirstlane(hi);
-  const int end = min(min(span0 + clients.span, len), hi);
+  const int end = min(it.split + 1 < wk.nsplit ? span0 + clients.span : len, hi);
   const int nsteps = end > first ? (end - first + STEP - 1) / STEP : 0;
   auto query = [&](int t, int piece, int st) {
     if constexpr (Q_LDS) return __builtin_bit_cast(bf16x8, q_lds[((t * NP + piece) * NS + st) * 64]);
@@ -640,7 +640,7 @@ __global__ __launch_bounds__(kKv4WideWaves * 64, (alone<HD, T>() ? 1 : 2)) void 
   __syncthreads();
 #pragma unroll
   for (int ww = 0; ww < WAVES; ++ww) hi = max(hi, word[ww]);
-  const int end = min(min(span0 + clients.span, len), __builtin_amdgcn_readfirstlane(hi));
+  const int end = min(it.split + 1 < wk.nsplit ? span0 + clients.span : len, __builtin_amdgcn_readfirstlane(hi));
   const int rounds = end > span0 ? (end - span0 + 63) / 64 : 0;
   __syncthreads();
 

@@ -47,6 +47,10 @@ __device__ __forceinline__ int64_t kv4_record(const Kv4View& v, int layer, int b
 constexpr int kKv4WideWaves = 4;
 constexpr int kKv4WideTiles = 2 * kKv4WideWaves;  // of a workgroup
 constexpr int kKv4MaxSplits = 64;
+// A client's last split takes up to so many tokens more than the others: a context of some power of two and a few new rows is not cut
+// once more for the rows.
+constexpr int kKv4SplitSlack = 64;
+inline int kv4_splits(int64_t len, int64_t span) { return (int)std::max<int64_t>(1, (len - kKv4SplitSlack + span - 1) / span); }
 constexpr int kv4_few_waves(int tiles) { return tiles == 1 ? 8 : 4; }
 
 // Clients of a launch, by value.  Workgroups: (cache head, item); a client's items are its splits, the groups of tiles of a
@@ -133,7 +137,7 @@ inline Kv4PlanNeeds kv4_plan(const Kv4Client* cl, int n, int dtype, int head_dim
     auto workgroups = [&](int64_t span) {
       int64_t w = 0;
       for (int i = 0; i < n; ++i)
-        if (mine(cl[i])) w += (int64_t)n_kv_heads * sets(cl[i], wg_tiles) * ((cl[i].len + span - 1) / span);
+        if (mine(cl[i])) w += (int64_t)n_kv_heads * sets(cl[i], wg_tiles) * kv4_splits(cl[i].len, span);
       return w;
     };
     // (a split costs what joins it, about the time of three steps: none below 768 tokens)
@@ -171,7 +175,7 @@ inline Kv4PlanNeeds kv4_plan(const Kv4Client* cl, int n, int dtype, int head_dim
       l.c.n_rows[j] = cl[i].n_rows;
       l.c.row_off[j] = cl[i].row_off;
       l.c.groups[j] = sets(cl[i], wg_tiles);
-      l.c.nsplit[j] = (int)((cl[i].len + span - 1) / span);
+      l.c.nsplit[j] = kv4_splits(cl[i].len, span);
       l.c.items += l.c.groups[j] * l.c.nsplit[j];
       l.c.part_off[j] = (int)need.part_tiles;
       l.c.count_off[j] = (int)need.counters;

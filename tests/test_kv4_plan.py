@@ -46,7 +46,7 @@ static int check(int nq, int nkv, int hd, int dtype, int n_cu, const std::vector
       if (l.c.len[j] != c.len || l.c.n_rows[j] != c.n_rows || l.c.row_off[j] != c.row_off) return fail("numbers", nq, nkv, hd, dtype, cl);
       if ((long)l.c.groups[j] * l.tiles < tiles || (long)(l.c.groups[j] - 1) * l.tiles >= tiles) return fail("groups", nq, nkv, hd, dtype, cl);
       const long n = l.c.nsplit[j], span = l.c.span;
-      if (n < 1 || n > kKv4MaxSplits || n * span < c.len || (n - 1) * span >= c.len) return fail("splits", nq, nkv, hd, dtype, cl);
+      if (n < 1 || n > kKv4MaxSplits || n * span + kKv4SplitSlack < c.len || (n - 1) * span >= c.len) return fail("splits", nq, nkv, hd, dtype, cl);
       if (n > 1) {
         if ((size_t)l.c.part_off[j] != part) return fail("partials", nq, nkv, hd, dtype, cl);
         part += (size_t)nkv * l.c.groups[j] * n * l.tiles;
