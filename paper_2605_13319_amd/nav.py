@@ -546,6 +546,12 @@ class KV4Cache:
                "pipesd_kv4_create")
         self._rows = 0
 
+    def _stream(self):
+        """The current stream of the pool's device."""
+        if self.pool is None:
+            return None
+        return _stream() if _raw_stream is None else _raw_stream(self.device.index)
+
     def close(self) -> None:
         if self.handle:
             _lib.pipesd_kv4_destroy(self.handle)
@@ -579,7 +585,7 @@ class KV4Cache:
         (s, n, _held), (c, m, new) = _numbers(seqs), _numbers(n_new)
         if n != m:
             raise ValueError(f"{n} clients, {m} numbers of tokens")
-        _check(_lib.pipesd_kv4_extend(self.handle, n, s, c, _stream() if self.pool is not None else None), "pipesd_kv4_extend")
+        _check(_lib.pipesd_kv4_extend(self.handle, n, s, c, self._stream()), "pipesd_kv4_extend")
         self._rows = int(sum(new))
 
     def append(self, layer: int, k, v) -> None:
@@ -587,7 +593,7 @@ class KV4Cache:
         heads = self.shape.n_kv_heads
         kp, ks = self._tensor(k, heads, "k")
         vp, vs = self._tensor(v, heads, "v")
-        _check(_lib.pipesd_kv4_append(self.handle, layer, kp, ks, vp, vs, _stream()), "pipesd_kv4_append")
+        _check(_lib.pipesd_kv4_append(self.handle, layer, kp, ks, vp, vs, self._stream()), "pipesd_kv4_append")
 
     def attend(self, layer: int, q, out=None, limits=None, mass=None, decay: float = 1.0):
         """Attention of the pass's queries over a layer of the cache; returns `out` (a new tensor like q if None).
@@ -606,7 +612,7 @@ class KV4Cache:
             lp = limits.data_ptr()
         if mass is not None:
             mp, tokens = self._mass(mass)
-        _check(_lib.pipesd_kv4_attend(self.handle, layer, qp, qs, lp, op, os_, mp, tokens, decay, _stream()), "pipesd_kv4_attend")
+        _check(_lib.pipesd_kv4_attend(self.handle, layer, qp, qs, lp, op, os_, mp, tokens, decay, self._stream()), "pipesd_kv4_attend")
         return out
 
     def _mass(self, mass):
@@ -627,7 +633,7 @@ class KV4Cache:
         k, v = torch.empty(size, dtype=self.dtype, device=self.device).unbind(0)
         # (a tensor of no elements has no address)
         _check(_lib.pipesd_kv4_read(self.handle, n, ids, f, c, layer0, n_layers, k.data_ptr() or self.pool.data_ptr(),
-                                    v.data_ptr() or self.pool.data_ptr(), _stream()), "pipesd_kv4_read")
+                                    v.data_ptr() or self.pool.data_ptr(), self._stream()), "pipesd_kv4_read")
         return k, v
 
     def evict(self, seqs: Sequence[int], into: Sequence[int], keep: int, recent: int, mass, kept=None):
@@ -645,7 +651,7 @@ class KV4Cache:
             kept = torch.empty(size, dtype=torch.int32, device=self.device)
         elif kept.dtype is not torch.int32 or kept.device != self.device or kept.shape != size or not kept.is_contiguous():
             raise ValueError(f"kept: a contiguous int32 tensor {size} on {self.device}")
-        _check(_lib.pipesd_kv4_evict(self.handle, n, ids, to, keep, recent, mp, tokens, kept.data_ptr(), _stream()), "pipesd_kv4_evict")
+        _check(_lib.pipesd_kv4_evict(self.handle, n, ids, to, keep, recent, mp, tokens, kept.data_ptr(), self._stream()), "pipesd_kv4_evict")
         return kept
 
     def truncate(self, seqs: Sequence[int], lengths: Sequence[int]) -> None:
