@@ -535,12 +535,13 @@ class KV4Cache:
             raise PipesdError(EINVAL, "pipesd_kv4_block_bytes")
         self.block_bytes = bb
         self.dtype = torch.float32 if shape.dtype == 0 else torch.bfloat16
-        self.pool = None
+        self.pool = self.device = self._device_index = None
         pool_ptr = None
         if on_device:
             torch.cuda.set_device(device)
             self.pool = torch.empty(n_blocks * bb, dtype=torch.uint8, device=device)
             self.device = self.pool.device
+            self._device_index = self.device.index
             pool_ptr = self.pool.data_ptr()
         _check(_lib.pipesd_kv4_create(C.byref(cfg), max_seqs, block_tokens, pool_ptr, n_blocks * bb, C.byref(self.handle)),
                "pipesd_kv4_create")
@@ -550,7 +551,7 @@ class KV4Cache:
         """The current stream of the pool's device."""
         if self.pool is None:
             return None
-        return _stream() if _raw_stream is None else _raw_stream(self.device.index)
+        return _stream() if _raw_stream is None else _raw_stream(self._device_index)
 
     def close(self) -> None:
         if self.handle:
@@ -568,7 +569,7 @@ class KV4Cache:
         """(address, elements between rows) of a tensor [rows][heads][head_dim] or [rows][heads * head_dim], the heads of a
         row side by side."""
         hd = self.shape.head_dim
-        if t.dtype is not self.dtype or not t.is_cuda or t.device != self.device:
+        if t.dtype is not self.dtype or t.get_device() != self._device_index:  # (-1: the host's memory)
             raise TypeError(f"{name}: a {self.dtype} tensor on {self.device}, not {t.dtype} on {t.device}")
         size, stride = t.shape, t.stride()
         if len(size) == 3:
