@@ -25,20 +25,18 @@ template <int HD>
 __device__ __forceinline__ float kv4_scale() { return (HD == 128 ? 0.08838834764831845f : 0.125f) * 1.44269504088896341f; }  // log2(e) / sqrt(HD)
 
 // Queries as operand B.  A lane holds 8 channels of its row in each step of a product; in step s these are 8 s .. + 7 of the
-// lane's own part of the row, so that what it needs of a key in all steps is one load.
+// lane's own part of the row, so that what it needs of a key in all steps is one load.  (Columns beyond the last row have the last
+// row's once more: nothing reads theirs.)
 template <int NP, int NS, typename T>
-__device__ __forceinline__ void load_queries(const T* part, bool live, k4u32x4 (&out)[NP][NS]) {
+__device__ __forceinline__ void load_queries(const T* part, k4u32x4 (&out)[NP][NS]) {
 #pragma unroll
   for (int s = 0; s < NS; ++s) {
     const T* p = part + s * 8;
     if constexpr (sizeof(T) == 2) {
-      const k4u32x4 x = *(const k4u32x4*)p;
-      out[0][s] = live ? x : k4u32x4{0u, 0u, 0u, 0u};
+      out[0][s] = *(const k4u32x4*)p;
     } else {
       const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
       float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = live ? x[i] : 0.f;
 #pragma unroll
       for (int m = 0; m < NP; ++m) {  // the upper half of each float is a bf16 number; what it leaves goes on
         unsigned w[4];
@@ -373,7 +371,7 @@ __global__ __launch_bounds__(WAVES * 64, TILES == 1 ? 4 : 2) void kv4_attend_ker
 #pragma unroll
   for (int t = 0; t < TILES; ++t) {
     const TileRow tr = wk.row(wk.first_row + t * 16 + c);
-    load_queries<NP, NS>((const T*)a.q + tr.row * a.q_stride + tr.head * HD + g * (HD / 4), tr.live, q[Q_LDS ? 0 : t]);
+    load_queries<NP, NS>((const T*)a.q + tr.row * a.q_stride + tr.head * HD + g * (HD / 4), q[Q_LDS ? 0 : t]);
     if constexpr (Q_LDS) {  // (the waves write the same)
 #pragma unroll
       for (int i = 0; i < NP * NS; ++i) q_lds[(t * NP * NS + i) * 64] = q[0][i / NS][i % NS];
@@ -381,8 +379,15 @@ __global__ __launch_bounds__(WAVES * 64, TILES == 1 ? 4 : 2) void kv4_attend_ker
     lim[t] = wk.limit(tr);
     if (tr.live) lo = min(lo, lim[t]), hi = max(hi, lim[t]);
   }
-#pragma unroll
-  for (int m = 1; m < 16; m *= 2) lo = min(lo, __shfl_xor(lo, m)), hi = max(hi, __shfl_xor(hi, m));
+  auto fold = [&](auto n) {
+    constexpr int N = decltype(n)::value;
+    lo = min(lo, (int)lanes_ror<N>((unsigned)lo));
+    hi = max(hi, (int)lanes_ror<N>((unsigned)hi));
+  };
+  fold(std::integral_constant<int, 8>{});
+  fold(std::integral_constant<int, 4>{});
+  fold(std::integral_constant<int, 2>{});
+  fold(std::integral_constant<int, 1>{});
   lo = __builtin_amdgcn_readfirstlane(lo);
   hi = __builtin_amdgcn_readfirstlane(hi);
   const int end = min(it.split + 1 < wk.nsplit ? span0 + clients.span : len, hi);
@@ -629,7 +634,7 @@ __global__ __launch_bounds__(kKv4WideWaves * 64, (alone<HD, T>() ? 1 : 2)) void 
   const bool idle = row0 >= wk.group_rows;  // (the wave has no row, and only converts)
   k4u32x4 q[NP][KS];
   const TileRow tr = wk.row(row0 + col);
-  load_queries<NP, KS>((const T*)a.q + tr.row * a.q_stride + tr.head * HD + half * (HD / 2), tr.live, q);
+  load_queries<NP, KS>((const T*)a.q + tr.row * a.q_stride + tr.head * HD + half * (HD / 2), q);
   const int lim = wk.limit(tr);
   int lo = tr.live ? lim : len, hi = tr.live ? lim : 0;
 #pragma unroll
@@ -1018,7 +1023,7 @@ __global__ __launch_bounds__(256) void kv4_mass_kernel(Kv4AttendCall a, Kv4Clien
     {
       const TileRow tr = tile_row((q0 + w) * 16 + c, group, group_rinv, n_rows, row_off, kvh);
       k4u32x4 q[NP][NS];
-      load_queries<NP, NS>((const T*)a.q + tr.row * a.q_stride + tr.head * HD + g * (HD / 4), tr.live, q);
+      load_queries<NP, NS>((const T*)a.q + tr.row * a.q_stride + tr.head * HD + g * (HD / 4), q);
 #pragma unroll
       for (int i = 0; i < NP * NS; ++i) q_lds[w][i][lane] = q[i / NS][i % NS];
       if (g == 0) {
