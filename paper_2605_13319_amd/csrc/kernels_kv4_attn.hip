@@ -987,9 +987,9 @@ hipError_t launch_kv4_attend(const Kv4AttendCall& c, const Kv4Launch& l, hipStre
 // ------------------------------------------------------------------------------------------------
 // Workgroup (cache head, tokens, client): each wave has TT * 16 tokens' keys in registers and meets all query rows, whose
 // tiles the four waves bring through LDS four at a time.  One writer per token, sums in a fixed order.
-template <int HD, typename T, int TT>
+template <int HD, typename T>
 __global__ __launch_bounds__(256) void kv4_mass_kernel(Kv4AttendCall a, Kv4Clients cl) {
-  constexpr int NP = pieces<T>(), NS = HD / 32;
+  constexpr int NP = pieces<T>(), NS = HD / 32, TT = 2;
   typedef typename std::conditional<HD == 128, k4u32x4, k4u32x2>::type Codes;
   __shared__ k4u32x4 q_lds[4][NP * NS][64];
   __shared__ float lse_lds[4][16];
@@ -1047,13 +1047,22 @@ __global__ __launch_bounds__(256) void kv4_mass_kernel(Kv4AttendCall a, Kv4Clien
         for (int tt = 0; tt < TT; ++tt) score[0][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[tt][i % NS], q, score[0][tt], 0, 0, 0);
       }
       settle(score);
+      float p[2][4];
 #pragma unroll
-      for (int tt = 0; tt < TT; ++tt)
+      for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(score[0][tt][i], c1, -lse));
-          sum[tt][i] += tok0 + tt * 16 + g * 4 + i < lim ? p : 0.f;
-        }
+        for (int i = 0; i < 4; ++i) p[tt][i] = __builtin_amdgcn_exp2f(fmaf(score[0][tt][i], c1, -lse));
+      if (__ballot(lim < tok0 + 32) != 0) {  // some row does not see all of the wave's tokens
+        asm volatile("");                    // (a branch: eight selections for every tile would be a third of its time)
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p[tt][i] = tok0 + tt * 16 + g * 4 + i < lim ? p[tt][i] : 0.f;
+      }
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[tt][i] += p[tt][i];
     }
   }
   float* out = a.mass + (((int64_t)cl.seq[ci] * a.view.n_layers + a.layer) * a.view.n_kv_heads + kvh) * a.mass_stride;
@@ -1075,13 +1084,7 @@ template <int HD, typename T>
 static hipError_t mass_of(const Kv4AttendCall& a, const Kv4Clients& cl, hipStream_t st) {
   int most = 0;
   for (int i = 0; i < cl.n; ++i) most = std::max(most, (int)cl.len[i]);
-  auto go = [&](auto tt) {
-    constexpr int TT = decltype(tt)::value;
-    const dim3 grid(a.view.n_kv_heads, (most + 64 * TT - 1) / (64 * TT), cl.n);
-    kv4_mass_kernel<HD, T, TT><<<grid, 256, 0, st>>>(a, cl);
-  };
-  if (most <= 32768) go(std::integral_constant<int, 2>{});
-  else go(std::integral_constant<int, 4>{});
+  kv4_mass_kernel<HD, T><<<dim3(a.view.n_kv_heads, (most + 127) / 128, cl.n), 256, 0, st>>>(a, cl);
   return hipGetLastError();
 }
 hipError_t launch_kv4_mass(const Kv4AttendCall& c, const Kv4Clients& cl, hipStream_t st) {
