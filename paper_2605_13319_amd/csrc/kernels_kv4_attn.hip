@@ -325,6 +325,12 @@ __device__ __forceinline__ void settle(Running<HT> (&x)[N]) {
 }
 
 // ---- few tiles: the waves share them, take every WAVES-th 32 tokens of the span and join their states through LDS at the end ----
+// One pass over the cache: keys and values go from memory into registers, become operands there and are not kept.  Eight waves with
+// one tile have 128 registers each and are four to a SIMD, which hides the way to memory; four with two tiles convert once for
+// both.  Bound by memory for a row or a few over a long context (1 row behind 131071 tokens, 32 query heads on 8 of 128: 34 us, 4.2 TB/s; 32
+// clients of 4 rows behind 8192: 60 us, 4.8 TB/s), by the conversion and the products for more rows (0.14 us for each 32 tokens of a
+// tile and compute unit), and by latency where there is little (9 rows behind 2048 tokens 8.9 us: 1.2 until the first keys are
+// asked for, 1.5 for them and their products, 1.2 for the waves' states, 3.5 to join the splits).
 // LDS: states [tile][wave][row], later what joins the splits; then the queries that registers do not hold; words
 template <int HD, int TILES, int WAVES>
 constexpr size_t state_floats() { return (size_t)TILES * WAVES * 16 * (HD + kKv4PartPad); }
@@ -588,6 +594,9 @@ __global__ __launch_bounds__(WAVES * 64, TILES == 1 ? 4 : 2) void kv4_attend_ker
 // on nothing of the step, travel with the weights' instructions, the score products with half of the next round's conversion.  (The
 // matrix cores leave a wave 28 of a product's 32 cycles for other instructions, and one after another, products and instructions
 // would take both times.)  Chunks that the compiler keeps in order do it: left to itself it puts the products side by side.
+// Bound by the matrix cores' power: 2048 rows behind 6144 tokens, 32 query heads on 8 of 128, 300 to 320 us and 750 to 800
+// TFLOP/s (two weights for each, so 1.5 times that in products); on zeros, which draw less, 250 us.  With two tiles more a
+// wave and its SIMD's registers to itself, half the LDS reads: 337 us where this took 326, and the longest rows end alone.
 //
 // Layout of a product: operand lane (r, h) holds row (column) r, k = 8 h .. + 7; the result's register 4 u + i holds row 8 u + 4 h + i
 // of column r.  Scores: k is channel h * HD / 2 + 8 s .. of step s.  Values: row r of product j is channel
@@ -986,7 +995,10 @@ hipError_t launch_kv4_attend(const Kv4AttendCall& c, const Kv4Launch& l, hipStre
 // weights given to the cached tokens, once the rows' sums are known
 // ------------------------------------------------------------------------------------------------
 // Workgroup (cache head, tokens, client): each wave has TT * 16 tokens' keys in registers and meets all query rows, whose
-// tiles the four waves bring through LDS four at a time.  One writer per token, sums in a fixed order.
+// tiles the four waves bring through LDS four at a time.  One writer per token, sums in a fixed order.  The scores are formed again: kept,
+// they would be 30 times the keys' bytes at 32 rows of 4 heads.  Bound by the way from block table to keys to products that each
+// short workgroup goes: 32 rows behind 12001 tokens of 8 heads of 64 8.0 us, 38 behind 65536 of 128 (64 tokens a wave in place of
+// 32: 10.9 and 39.9).
 template <int HD, typename T>
 __global__ __launch_bounds__(256) void kv4_mass_kernel(Kv4AttendCall a, Kv4Clients cl) {
   constexpr int NP = pieces<T>(), NS = HD / 32, TT = 2;

@@ -1,15 +1,15 @@
 // The 4-bit cache: its layout, the plan of a pass, and the launchers.
 //
 // A value is one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 or their negatives (e2m1: the magnitudes are the codes 0..7, 8 is the
-// sign) times a power of two that 32 neighbouring channels of a token and head share; a power is a byte e + 127.  That is
-// what the matrix cores multiply as it is.  All values are finite.
+// sign) times a power of two that 32 neighbouring channels of a token and head share; a power is a byte e + 127.  All values are
+// finite, and exact as bf16 numbers.
 //
 // Per (layer, block of 16 tokens, head of the cache) the pool holds one record: the codes of the keys, of the values, the
 // powers of the keys, of the values.
-//   keys          [token][head_dim / 2 bytes], the even channel in the low half.  Operand A of S^T = K Q^T (16 tokens x 128
-//                 channels): lane (token, quarter) holds 32 channels, which share one power.
-//   values        [token / 4][unit 0..15][token % 4][head_dim / 32 bytes]; unit r holds channels r * head_dim / 16 and on.
-//                 Operand A of O^T = V^T P^T: lane (r, quarter g) holds its unit of the tokens 4g .. 4g + 3, side by side.
+//   keys          [token][head_dim / 2 bytes], the even channel in the low half: a wave reads a block with one load, lane (token,
+//                 quarter) its quarter of the channels, which at head_dim 128 share one power
+//   values        [token / 4][unit 0..15][token % 4][head_dim / 32 bytes]; unit r holds channels r * head_dim / 16 and on.  Lane (r,
+//                 quarter g) reads its unit of the tokens 4g .. 4g + 3, side by side: what pairs of tokens are made of
 //   key powers    [token][head_dim / 32]
 //   value powers  [token / 4][head_dim / 32][token % 4]: those of a lane's four tokens are one word
 #pragma once
