@@ -455,8 +455,8 @@ __global__ __launch_bounds__(WAVES * 64, TILES == 1 ? 4 : 2) void kv4_attend_ker
           for (int t = 0; t < TILES; ++t) score[t][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, query(t, m, st), score[t][tt], 0, 0, 0);
       }
     }
-    settle(score);
     request_keys(i + 1);
+    settle(score);
     bf16x8 ph[TILES], pl[TILES];
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
@@ -487,8 +487,8 @@ __global__ __launch_bounds__(WAVES * 64, TILES == 1 ? 4 : 2) void kv4_attend_ker
         y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, pl[t], y, 0, 0, 0);
       }
     }
-    settle(run);
     request_values(i + 1);
+    settle(run);
   }
 
   // ---- the waves' states joined: rows, or a split's partial rows (written through) ----
