@@ -328,7 +328,7 @@ __device__ __forceinline__ void settle(Running<HT> (&x)[N]) {
 // One pass over the cache: keys and values go from memory into registers, become operands there and are not kept.  Eight waves with
 // one tile have 128 registers each and are four to a SIMD, which hides the way to memory; four with two tiles convert once for
 // both.  Bound by memory for a row or a few over a long context (1 row behind 131071 tokens, 32 query heads on 8 of 128: 34 us, 4.2 TB/s; 32
-// clients of 4 rows behind 8192: 60 us, 4.8 TB/s), by the conversion and the products for more rows (0.14 us for each 32 tokens of a
+// clients of 4 rows behind 8192: 57 us, 5.0 TB/s), by the conversion and the products for more rows (0.14 us for each 32 tokens of a
 // tile and compute unit), and by latency where there is little (9 rows behind 2048 tokens 8.9 us: 1.2 until the first keys are
 // asked for, 1.5 for them and their products, 1.2 for the waves' states, 3.5 to join the splits).
 // LDS: states [tile][wave][row], later what joins the splits; then the queries that registers do not hold; words
