@@ -44,8 +44,9 @@ struct pipesd_kv4 {
   float* lse = nullptr;
   size_t lse_cap = 0;
   // the pass
-  std::vector<Kv4Client> pass;
-  std::vector<Kv4Launch> launches;
+  std::vector<Kv4Client> pass, next_pass;  // (next_..: where the next pass is made)
+  std::vector<Kv4Launch> launches, next_launches;
+  std::vector<int32_t> had;
   bool pass_open = false, attends = false;
 
   int32_t table_off(int32_t seq) const { return (2 * seq + seqs[seq].which) * n_blocks; }
@@ -56,11 +57,14 @@ static int32_t kv4_blocks(int32_t tokens) { return tokens / kBlockTokens + (toke
 static bool kv4_seq_ok(const pipesd_kv4* kv, int32_t seq) { return kv && seq >= 0 && seq < kv->max_seqs; }
 // every id in range, none twice
 static bool kv4_seqs_ok(const pipesd_kv4* kv, int32_t n, const int32_t* ids) {
+  for (int32_t i = 0; i < n; ++i)
+    if (!kv4_seq_ok(kv, ids[i])) return false;
+  bool rising = true;  // (as ids mostly are)
+  for (int32_t i = 1; i < n; ++i) rising = rising && ids[i] > ids[i - 1];
+  if (rising) return true;
   std::vector<char> seen(kv->max_seqs, 0);
-  for (int32_t i = 0; i < n; ++i) {
-    if (!kv4_seq_ok(kv, ids[i]) || seen[ids[i]]) return false;
-    seen[ids[i]] = 1;
-  }
+  for (int32_t i = 0; i < n; ++i)
+    if (seen[ids[i]]++) return false;
   return true;
 }
 static void kv4_release(pipesd_kv4* kv, Kv4Seq& s, int32_t tokens) {
@@ -196,7 +200,7 @@ extern "C" int pipesd_kv4_truncate(pipesd_kv4* kv, int32_t n_seqs, const int32_t
     for (int32_t i = 0; i < n_seqs; ++i)
       if (new_len[i] < 0 || new_len[i] > kv->seqs[seq_ids[i]].len) return PIPESD_ESTATE;
     bool touched = false;
-    for (int32_t i = 0; i < n_seqs; ++i) {
+    for (int32_t i = n_seqs - 1; i >= 0; --i) {  // (backwards: who asks for as much again, in the same order, gets the same blocks)
       Kv4Seq& s = kv->seqs[seq_ids[i]];
       touched |= s.in_pass && new_len[i] < s.len;
       kv4_release(kv, s, new_len[i]);
@@ -250,9 +254,12 @@ extern "C" int pipesd_kv4_extend(pipesd_kv4* kv, int32_t n_seqs, const int32_t* 
     if (total < 1 || total > INT32_MAX) return PIPESD_EINVAL;
     if (blocks > (int64_t)kv->free_list.size()) return PIPESD_ENOMEM;
 
-    std::vector<Kv4Client> plan;
-    std::vector<Kv4Launch> launches;
-    std::vector<int32_t> had(n_seqs);
+    std::vector<Kv4Client>& plan = kv->next_pass;
+    std::vector<Kv4Launch>& launches = kv->next_launches;
+    std::vector<int32_t>& had = kv->had;
+    plan.clear();
+    launches.clear();
+    had.resize(n_seqs);
     plan.reserve(n_seqs);
     int32_t row = 0;
     for (int32_t i = 0; i < n_seqs; ++i) {
