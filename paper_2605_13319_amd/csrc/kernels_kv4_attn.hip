@@ -602,9 +602,10 @@ __global__ __launch_bounds__(WAVES * 64, TILES == 1 ? 4 : 2) void kv4_attend_ker
 // on nothing of the step, travel with the weights' instructions, the score products with half of the next round's conversion.  (The
 // matrix cores leave a wave 28 of a product's 32 cycles for other instructions, and one after another, products and instructions
 // would take both times.)  Chunks that the compiler keeps in order do it: left to itself it puts the products side by side.
-// Bound by the matrix cores' power: 2048 rows behind 6144 tokens, 32 query heads on 8 of 128, 300 to 320 us and 750 to 800
-// TFLOP/s (two weights for each, so 1.5 times that in products); on zeros, which draw less, 250 us.  With two tiles more a
-// wave and its SIMD's registers to itself, half the LDS reads: 337 us where this took 326, and the longest rows end alone.
+// Bound by the matrix cores' power: 2048 rows behind 6144 tokens, 32 query heads on 8 of 128, 300 to 320 us, 750 to 800
+// TFLOP/s and, with two weights for each, 1.13 to 1.19 PFLOP/s of products, where a large matrix product of random numbers reaches
+// 1.24; on zeros, which draw less, 250 us.  With two tiles more a wave and its SIMD's registers to itself, half the LDS reads:
+// 337 us where this took 326, and the longest rows end alone.
 //
 // Layout of a product: operand lane (r, h) holds row (column) r, k = 8 h .. + 7; the result's register 4 u + i holds row 8 u + 4 h + i
 // of column r.  Scores: k is channel h * HD / 2 + 8 s .. of step s.  Values: row r of product j is channel
@@ -755,10 +756,10 @@ __global__ __launch_bounds__(kKv4WideWaves * 64, (alone<HD, T>() ? 1 : 2)) void 
         score[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, key[st]), __builtin_bit_cast(bf16x8, q[m][st]), score[0][0], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
       if (st % 2 == 0) convert(st / 2);
+      if (st == KS - 2) request();
       if (st >= KS - HT) value[0][st - (KS - HT)] = from[(st - (KS - HT)) * 2 * 64];
     }
     __builtin_amdgcn_sched_barrier(0);
-    request();
     settle<ALONE>(score);
     float sc[16];
 #pragma unroll
@@ -780,7 +781,6 @@ __global__ __launch_bounds__(kKv4WideWaves * 64, (alone<HD, T>() ? 1 : 2)) void 
       low[NOW][x] = lower_pair(p[0], p[1], up[NOW][x]);
       total += p[0] + p[1];
     };
-    weigh(0, neg_m);
     const k4u32x4* keys = key_lds + ((n + 1) & 3) * KS * 64 + lane;
     unsigned long long move = 0;
 #pragma unroll
@@ -793,6 +793,7 @@ __global__ __launch_bounds__(kKv4WideWaves * 64, (alone<HD, T>() ? 1 : 2)) void 
                                                            acc[0][j], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
         if (k == 0) {
+          if (x == 0) weigh(0, neg_m);
           keep(x);
           asm volatile("" ::"v"(low[NOW][x]));  // (here, not behind the branch below)
           if (x < HT) value[1][x] = from[(x * 2 + 1) * 64];

@@ -149,16 +149,17 @@ def _ints(a):
 
 
 def _numbers(a):
-    """(address, number, what holds them) of int32 values, taken as _ints takes them (0.4 us for one)."""
+    """(address, number, what holds them, their sum) of int32 values, taken as _ints takes them (0.3 us for one)."""
     if type(a) is list and a:
         try:
-            if type(sum(a)) is int:
+            total = sum(a)
+            if type(total) is int:
                 buf = array("i", a)
-                return (*buf.buffer_info(), buf)
+                return (*buf.buffer_info(), buf, total)
         except Exception:  # (numpy says what is wrong, or takes it)
             pass
     v = _i32(a)
-    return v.ctypes.data, len(v), v
+    return v.ctypes.data, len(v), v, int(v.sum(dtype=np.int64))
 
 
 def _floats(a):
@@ -583,11 +584,11 @@ class KV4Cache:
 
     def extend(self, seqs: Sequence[int], n_new: Sequence[int]) -> None:
         """Begin a pass: n_new[i] more tokens for client seqs[i]."""
-        (s, n, _held), (c, m, new) = _numbers(seqs), _numbers(n_new)
+        (s, n, _ids, _), (c, m, _new, total) = _numbers(seqs), _numbers(n_new)
         if n != m:
             raise ValueError(f"{n} clients, {m} numbers of tokens")
         _check(_lib.pipesd_kv4_extend(self.handle, n, s, c, self._stream()), "pipesd_kv4_extend")
-        self._rows = int(sum(new))
+        self._rows = total
 
     def append(self, layer: int, k, v) -> None:
         """Round the pass's keys and values of a layer into the cache."""
@@ -627,10 +628,10 @@ class KV4Cache:
         """(keys, values) [n_layers][sum of count][n_kv_heads][head_dim] that ranges of the clients' tokens are held as."""
         s = self.shape
         n_layers = s.n_layers - layer0 if n_layers is None else n_layers
-        (ids, n, _held), (f, nf, _first), (c, nc, rows) = _numbers(seqs), _numbers(first), _numbers(count)
+        (ids, n, _ids, _), (f, nf, _first, _), (c, nc, _count, rows) = _numbers(seqs), _numbers(first), _numbers(count)
         if n != nf or n != nc:
             raise ValueError(f"{n} clients, {nf} and {nc} ends of ranges")
-        size = (2, max(n_layers, 0), max(int(sum(rows)), 0), s.n_kv_heads, s.head_dim)
+        size = (2, max(n_layers, 0), max(rows, 0), s.n_kv_heads, s.head_dim)
         k, v = torch.empty(size, dtype=self.dtype, device=self.device).unbind(0)
         # (a tensor of no elements has no address)
         _check(_lib.pipesd_kv4_read(self.handle, n, ids, f, c, layer0, n_layers, k.data_ptr() or self.pool.data_ptr(),
@@ -641,7 +642,7 @@ class KV4Cache:
         """Cut clients to `keep` tokens, the newest `recent` and the heaviest others per layer and head, into clients `into`.
         Returns the kept indices, int32 [clients][n_layers][n_kv_heads][keep]."""
         s = self.shape
-        (ids, n, _held), (to, m, _into) = _numbers(seqs), _numbers(into)
+        (ids, n, _ids, _), (to, m, _into, _) = _numbers(seqs), _numbers(into)
         if n != m:
             raise ValueError(f"{n} clients into {m}")
         mp, tokens = self._mass(mass)
@@ -657,7 +658,7 @@ class KV4Cache:
 
     def truncate(self, seqs: Sequence[int], lengths: Sequence[int]) -> None:
         """Forget the clients' tokens from lengths[i] on."""
-        (s, n, _held), (c, m, _new) = _numbers(seqs), _numbers(lengths)
+        (s, n, _ids, _), (c, m, _new, _) = _numbers(seqs), _numbers(lengths)
         if n != m:
             raise ValueError(f"{n} clients, {m} lengths")
         _check(_lib.pipesd_kv4_truncate(self.handle, n, s, c), "pipesd_kv4_truncate")
