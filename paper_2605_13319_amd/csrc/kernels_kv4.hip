@@ -366,11 +366,11 @@ hipError_t launch_kv4_select(const Kv4View& v, const Kv4Cuts& c, float* mass, in
 // read and 71 written.
 // ------------------------------------------------------------------------------------------------
 template <int HD>
-__global__ __launch_bounds__(256) void kv4_move_kernel(Kv4View v, Kv4Cuts c, const int32_t* kept) {
+__global__ __launch_bounds__(256) void kv4_move_kernel(Kv4View v, Kv4Cuts c, const int32_t* kept, int first) {
   constexpr int U = Kv4Record<HD>::kUnit;
   const int lane = threadIdx.x & 63;
   const int kvh = blockIdx.x % v.n_kv_heads, layer = blockIdx.x / v.n_kv_heads, ci = blockIdx.z;
-  const int b = blockIdx.y * 4 + (threadIdx.x >> 6);
+  const int b = (first + (int)blockIdx.y) * 4 + (int)(threadIdx.x >> 6);
   if (b * kBlockTokens >= c.keep) return;
   const int32_t* idx = kept + (((int64_t)ci * v.n_layers + layer) * v.n_kv_heads + kvh) * c.keep + b * kBlockTokens;
   const int n = min(kBlockTokens, c.keep - b * kBlockTokens);
@@ -416,9 +416,12 @@ __global__ __launch_bounds__(256) void kv4_move_kernel(Kv4View v, Kv4Cuts c, con
 }
 
 hipError_t launch_kv4_move(int head_dim, const Kv4View& v, const Kv4Cuts& c, const int32_t* kept, hipStream_t st) {
-  const dim3 grid(v.n_kv_heads * v.n_layers, ((c.keep + kBlockTokens - 1) / kBlockTokens + 3) / 4, c.n);
-  if (head_dim == 128) kv4_move_kernel<128><<<grid, 256, 0, st>>>(v, c, kept);
-  else kv4_move_kernel<64><<<grid, 256, 0, st>>>(v, c, kept);
+  const int n = c.keep / (4 * kBlockTokens) + 1;
+  for (int first = 0; first < n; first += kKv4MaxItems) {
+    const dim3 grid(v.n_kv_heads * v.n_layers, std::min(n - first, kKv4MaxItems), c.n);
+    if (head_dim == 128) kv4_move_kernel<128><<<grid, 256, 0, st>>>(v, c, kept, first);
+    else kv4_move_kernel<64><<<grid, 256, 0, st>>>(v, c, kept, first);
+  }
   return hipGetLastError();
 }
 

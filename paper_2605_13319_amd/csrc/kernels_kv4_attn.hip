@@ -964,7 +964,7 @@ static hipError_t allow_and_launch(K kernel, std::atomic<uint64_t>& allowed, siz
     const hipError_t e = allow_lds(allowed, (const void*)kernel, lds);
     if (e != hipSuccess) return e;
   }
-  if (cl.items > 65535) return hipErrorInvalidValue;  // (the plan keeps them far below)
+  if (cl.items > kKv4MaxItems) return hipErrorInvalidValue;  // (the plan's launches have no more)
   kernel<<<dim3(c.view.n_kv_heads, cl.items), threads, lds, st>>>(c, cl);
   return hipGetLastError();
 }
@@ -1006,7 +1006,7 @@ hipError_t launch_kv4_attend(const Kv4AttendCall& c, const Kv4Launch& l, hipStre
 // short workgroup goes: 32 rows behind 12001 tokens of 8 heads of 64 8.0 us, 38 behind 65536 of 128 (64 tokens a wave in place of
 // 32: 10.9 and 39.9).
 template <int HD, typename T>
-__global__ __launch_bounds__(256) void kv4_mass_kernel(Kv4AttendCall a, Kv4Clients cl) {
+__global__ __launch_bounds__(256) void kv4_mass_kernel(Kv4AttendCall a, Kv4Clients cl, int first_piece) {
   constexpr int NP = pieces<T>(), NS = HD / 32, TT = 2;
   typedef typename std::conditional<HD == 128, k4u32x4, k4u32x2>::type Codes;
   __shared__ k4u32x4 q_lds[4][NP * NS][64];
@@ -1015,8 +1015,8 @@ __global__ __launch_bounds__(256) void kv4_mass_kernel(Kv4AttendCall a, Kv4Clien
   const int kvh = blockIdx.x, ci = blockIdx.z, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int c = lane & 15, g = lane >> 4;
   const int len = cl.len[ci], n_rows = cl.n_rows[ci], row_off = cl.row_off[ci];
-  const int tok0 = ((int)blockIdx.y * 4 + w) * TT * 16;
-  if ((int)blockIdx.y * 4 * TT * 16 >= len) return;  // (whole workgroup)
+  const int piece = first_piece + (int)blockIdx.y, tok0 = (piece * 4 + w) * TT * 16;
+  if (piece * 4 * TT * 16 >= len) return;  // (whole workgroup)
   const int group = a.group;
   const float group_rinv = __builtin_amdgcn_rcpf((float)group);
   const int nqt = (n_rows * group + 15) / 16;
@@ -1102,7 +1102,9 @@ template <int HD, typename T>
 static hipError_t mass_of(const Kv4AttendCall& a, const Kv4Clients& cl, hipStream_t st) {
   int most = 0;
   for (int i = 0; i < cl.n; ++i) most = std::max(most, (int)cl.len[i]);
-  kv4_mass_kernel<HD, T><<<dim3(a.view.n_kv_heads, (most + 127) / 128, cl.n), 256, 0, st>>>(a, cl);
+  const int pieces = most / 128 + (most % 128 != 0);
+  for (int first = 0; first < pieces; first += kKv4MaxItems)
+    kv4_mass_kernel<HD, T><<<dim3(a.view.n_kv_heads, std::min(pieces - first, kKv4MaxItems), cl.n), 256, 0, st>>>(a, cl, first);
   return hipGetLastError();
 }
 hipError_t launch_kv4_mass(const Kv4AttendCall& c, const Kv4Clients& cl, hipStream_t st) {

@@ -56,6 +56,7 @@ constexpr int kv4_few_waves(int tiles) { return tiles == 1 ? 8 : 4; }
 // Clients of a launch, by value.  Workgroups: (cache head, item); a client's items are its splits, the groups of tiles of a
 // split side by side, for they read the same tokens.
 constexpr int kKv4ClientsPerLaunch = 32;
+constexpr int kKv4MaxItems = 65535;  // workgroups of a grid in y
 struct Kv4Clients {
   int32_t n, items, span;  // span: tokens of a split
   int32_t apart;           // splits are joined by a kernel of their own, not by their last workgroup
@@ -164,7 +165,8 @@ inline Kv4PlanNeeds kv4_plan(const Kv4Client* cl, int n, int dtype, int head_dim
     };
     for (int i = 0; i < n; ++i) {
       if (!mine(cl[i])) continue;
-      if (l.c.n == kKv4ClientsPerLaunch) flush();
+      const int groups = sets(cl[i], wg_tiles), nsplit = kv4_splits(cl[i].len, span);
+      if (l.c.n == kKv4ClientsPerLaunch || l.c.items + groups * nsplit > kKv4MaxItems) flush();
       const int j = l.c.n++;
       l.wide = wide;
       l.tiles = wg_tiles;
@@ -174,8 +176,8 @@ inline Kv4PlanNeeds kv4_plan(const Kv4Client* cl, int n, int dtype, int head_dim
       l.c.len[j] = cl[i].len;
       l.c.n_rows[j] = cl[i].n_rows;
       l.c.row_off[j] = cl[i].row_off;
-      l.c.groups[j] = sets(cl[i], wg_tiles);
-      l.c.nsplit[j] = kv4_splits(cl[i].len, span);
+      l.c.groups[j] = groups;
+      l.c.nsplit[j] = nsplit;
       l.c.items += l.c.groups[j] * l.c.nsplit[j];
       l.c.part_off[j] = (int)need.part_tiles;
       l.c.count_off[j] = (int)need.counters;

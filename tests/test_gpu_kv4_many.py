@@ -8,6 +8,7 @@ import math
 import pytest
 import torch
 
+from paper_2605_13319_amd import nav
 from tests.test_gpu_kv4 import check_rows, make_cache, shape_of
 
 gpu = pytest.mark.gpu
@@ -157,3 +158,69 @@ def test_a_recorded_pass(name):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want) and torch.equal(mass, other)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_clients_than_a_launch_takes(dtype):
+    """40 clients: rows kept, attention and weights of each, 35 of them cut at once."""
+    n, nq, nkv, dim = 40, 8, 2, 64
+    before, rows = [(37 * c) % 211 for c in range(n)], [(c * 5) % 9 for c in range(n)]
+    kv = make_cache(shape_of(nq, nkv, dim, dtype), n, 240)
+    held = [b > 0 for b in before]
+    ids = [c for c in range(n) if held[c]]
+    kv.extend(ids, [before[c] for c in ids])
+    kv.append(0, rows_of(sum(before), nkv, dim, dtype, 1), rows_of(sum(before), nkv, dim, dtype, 2))
+    kv.extend(list(range(n)), rows)
+    total = sum(rows)
+    kv.append(0, rows_of(total, nkv, dim, dtype, 3), rows_of(total, nkv, dim, dtype, 4))
+    q = rows_of(total, nq, dim, dtype, 5)
+    mass = torch.full((n, 1, nkv, 240), torch.nan, device="cuda")
+    out = kv.attend(0, q, mass=mass, decay=0.0)
+    r = 0
+    for c, (b, m) in enumerate(zip(before, rows)):
+        if m:
+            k, v = kv.read([c], [0], [b + m])
+            o, s, a, w, big = definition(q[r:r + m], k[0], v[0], torch.arange(b + 1, b + m + 1, device="cuda"))
+            check_rows(out[r:r + m], o.cpu(), s.cpu(), a.cpu(), dtype)
+            assert bool(((mass[c, 0, :, :b + m].double() - w).abs() <= 2.0 ** -18 * (1 + big[:, None]) * w + 1e-30).all())
+        r += m
+    cut = [c for c in range(n) if before[c] + rows[c] >= 20][:35]
+    mass.nan_to_num_(0.0)
+    old = [kv.read([c], [0], [before[c] + rows[c]]) for c in cut]
+    weights = mass[cut, 0].cpu()
+    kept = kv.evict(cut, cut, 20, 5, mass).cpu().long()
+    k, v = kv.read(cut, [0] * len(cut), [20] * len(cut))
+    assert len(cut) > 32
+    for i, c in enumerate(cut):
+        length = before[c] + rows[c]
+        heavy = torch.argsort(-weights[i, :, :length - 5], dim=-1, stable=True)[:, :15].sort(-1).values
+        want = torch.cat([heavy, torch.arange(length - 5, length).expand(nkv, 5)], -1)
+        assert torch.equal(kept[i, 0], want)
+        at = want.T[..., None].expand(-1, -1, dim).cuda()
+        for new, was in ((k, old[i][0]), (v, old[i][1])):
+            assert torch.equal(new[0, 20 * i:20 * i + 20], was[0].gather(0, at))
+
+
+@gpu
+def test_a_context_beyond_the_workgroups_of_a_grid():
+    """8.5 million tokens whose keys are 0: the weights are all alike, and a cut keeps the first and the newest."""
+    length, keep, recent = 8500000, 4300000, 100
+    kv = nav.KV4Cache(shape_of(2, 1, 64), 1, -(-(length + 2) // 16) + -(-keep // 16))
+    kv.pool.zero_()
+    kv.extend([0], [length])
+    kv.extend([0], [2])
+    zero = torch.zeros(2, 1, 64, dtype=torch.bfloat16, device="cuda")
+    kv.append(0, zero, rows_of(2, 1, 64, "bf16", 1))
+    mass = torch.full((1, 1, 1, length + 2), torch.nan, device="cuda")
+    out = kv.attend(0, rows_of(2, 2, 64, "bf16", 2), mass=mass, decay=0.0)
+    assert float(out.abs().max()) < 1e-5
+    want = torch.full((length + 2,), 2 / (length + 1) + 2 / (length + 2), dtype=torch.float64, device="cuda")
+    want[-1] = 2 / (length + 2)
+    assert bool(((mass[0, 0, 0].double() - want).abs() <= 2.0 ** -18 * want).all())
+    mass.fill_(1.0)
+    kept = kv.evict([0], [0], keep, recent, mass)[0, 0, 0]
+    assert torch.equal(kept[:keep - recent], torch.arange(keep - recent, dtype=torch.int32, device="cuda"))
+    assert torch.equal(kept[keep - recent:], torch.arange(length + 2 - recent, length + 2, dtype=torch.int32, device="cuda"))
+    _, v = kv.read([0], [keep - 3], [3])
+    assert int((v[0, 0] != 0).sum()) == 0 and int((v[0, 1:] != 0).sum()) > 100

@@ -98,6 +98,13 @@ int main(int argc, char** argv) {
     if (check(h[0], h[1], hd, dtype, n_cu, cl)) return 1;
     for (const Kv4Launch& l : out) kinds[l.wide ? 2 : l.tiles - 1]++;
   }
+  for (int dtype : {PIPESD_F32, PIPESD_BF16}) {  // more workgroups than a grid has in y
+    std::vector<Kv4Client> cl;
+    for (int i = 0; i < 256; ++i) cl.push_back(Kv4Client{i, kKv4MaxRows, i * kKv4MaxRows, kKv4MaxRows + 1000 * i});
+    if (check(256, 1, 64, dtype, 256, cl)) return 1;
+    for (Kv4Client& c : cl) c.n_rows = 130, c.len = 700;
+    if (check(256, 1, 128, dtype, 256, cl)) return 1;
+  }
   printf("%ld %ld %ld\n", kinds[0], kinds[1], kinds[2]);
   return 0;
 }
