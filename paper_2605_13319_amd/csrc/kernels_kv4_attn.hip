@@ -326,8 +326,8 @@ __device__ __forceinline__ void settle(Running<HT> (&x)[N]) {
 
 // ---- few tiles: the waves share them, take every WAVES-th 32 tokens of the span and join their states through LDS at the end ----
 // One pass over the cache: keys and values go from memory into registers, become operands there and are not kept.  Eight waves with
-// one tile have 128 registers each and are four to a SIMD, which hides the way to memory; four with two tiles convert once for
-// both.  Bound by memory for a row or a few over a long context (1 row behind 131071 tokens, 32 query heads on 8 of 128: 34 us, 4.2 TB/s; 32
+// one tile have 128 registers each and are four to a SIMD, which hides the way to memory; with two tiles they convert once for
+// both and are two to a SIMD.  Bound by memory for a row or a few over a long context (1 row behind 131071 tokens, 32 query heads on 8 of 128: 34 us, 4.2 TB/s; 32
 // clients of 4 rows behind 8192: 57 us, 5.0 TB/s), by the conversion and the products for more rows (0.14 us for each 32 tokens of a
 // tile and compute unit), and by latency where there is little (9 rows behind 2048 tokens 8.9 us: 1.2 until the first keys are
 // asked for, 1.5 for them and their products, 1.2 for the waves' states, 3.5 to join the splits).
@@ -977,7 +977,7 @@ static hipError_t join(hipError_t e, const Kv4AttendCall& c, const Kv4Clients& c
 template <int HD, typename T, int TILES>
 static hipError_t attend_few(const Kv4AttendCall& c, const Kv4Clients& cl, hipStream_t st) {
   static std::atomic<uint64_t> allowed{0};
-  constexpr int WAVES = kv4_few_waves(TILES);
+  constexpr int WAVES = kKv4FewWaves;
   return join<HD, T, TILES * 16>(
       allow_and_launch(kv4_attend_kernel<HD, T, TILES, WAVES>, allowed, few_lds_bytes<HD, T, TILES, WAVES>(), WAVES * 64, c, cl, st), c, cl, st);
 }

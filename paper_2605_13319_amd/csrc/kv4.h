@@ -41,7 +41,7 @@ __device__ __forceinline__ int64_t kv4_record(const Kv4View& v, int layer, int b
 // ---- the plan of a pass ------------------------------------------------------------------------
 // A client's query rows are taken with the heads that share a head of the cache: row rr of a cache head is pass row rr /
 // group, head rr % group of the group; 16 of them make a tile.
-//   few tiles    the waves of a workgroup take every WAVES-th 32 tokens of a span for the same one or two tiles, and
+//   few tiles    the eight waves of a workgroup take every eighth 32 tokens of a span for the same one or two tiles, and
 //                join their sums
 //   many tiles   each of four waves takes two tiles of its own, over tokens that they convert together
 constexpr int kKv4WideWaves = 4;
@@ -51,7 +51,7 @@ constexpr int kKv4MaxSplits = 64;
 // once more for the rows.
 constexpr int kKv4SplitSlack = 64;
 inline int kv4_splits(int64_t len, int64_t span) { return (int)std::max<int64_t>(1, (len - kKv4SplitSlack + span - 1) / span); }
-constexpr int kv4_few_waves(int tiles) { return tiles == 1 ? 8 : 4; }
+constexpr int kKv4FewWaves = 8;
 
 // Clients of a launch, by value.  Workgroups: (cache head, item); a client's items are its splits, the groups of tiles of a
 // split side by side, for they read the same tokens.
@@ -78,28 +78,28 @@ struct Kv4PlanNeeds {
   size_t part_tiles, counters;
 };
 
-// What a launch takes on a device of 256 compute units, in us: `start`, and `step` for each 32 tokens of a workgroup's tiles and
-// compute unit.  Two tiles in a workgroup share the conversion of keys and values, but leave registers for half the waves; eight share it
-// through LDS, four times as many rows to join.  Measured, query heads 4 to a cache head: 4 clients of 8 rows behind 2048 tokens 13.5 us
-// with one tile, 18.2 with two; 32 clients behind 4096 46.6 and 45.0; 32 rows behind 65536 tokens 67 with two, 71 with eight; 2048 rows behind 6144
-// of head dim 64 225 with two, 186 with eight, of head dim 128 349 and 265.  Two in fp32 were never faster: 4 clients of 9 rows behind 4096 tokens 32.9 us, 21.9 with one.
+// What workgroups of one, two or eight tiles take, in us: a launch (with what joins eight tiles' splits), a workgroup to begin and end, 32 tokens
+// of it by compute unit with all `resident` workgroups that a compute unit holds, how much longer one takes alone, and a join.  Two
+// tiles share the conversion of keys and values, but leave registers for half the workgroups; eight share it through LDS, four times as
+// many rows to join.  Measured, 4 query heads on each of 8 cache heads of 128: 16 clients of 8 rows behind 4096 tokens 28.0 us with one
+// tile, 24.8 with two; 4 of 4 rows behind 20000 23.6 and 28; 32 rows behind 65536 63.5 with two, 68 with eight; 64 rows 115 and 98; 2048
+// rows behind 6144 349 and 265, of head dim 64 225 and 182.  Two in fp32 were never faster: 4 clients of 9 rows behind 4096 tokens
+// 32.9 us, 21.9 with one.  (40 cache heads, 4 clients of 17 rows behind 8192: 57.8; two tiles in four waves, two such workgroups to a
+// compute unit, 52.9, but 10 to 15 % longer wherever the rounds fit.)
 struct Kv4Cost {
-  double start, step;
+  double start, begin, step, alone, join;
+  int resident;
 };
 constexpr Kv4Cost kv4_cost(int tiles, int dtype, int head_dim) {
-  if (dtype == PIPESD_F32) {
-    if (tiles == 2) return Kv4Cost{1e30, 1e30};
-    if (tiles == 1) return head_dim == 128 ? Kv4Cost{12, 0.15} : Kv4Cost{10, 0.105};
-    return head_dim == 128 ? Kv4Cost{25, 1.1} : Kv4Cost{18, 0.7};
-  }
-  if (tiles == 1) return head_dim == 128 ? Kv4Cost{8, 0.14} : Kv4Cost{8, 0.086};
-  if (tiles == 2) return head_dim == 128 ? Kv4Cost{14, 0.185} : Kv4Cost{13, 0.12};
-  return head_dim == 128 ? Kv4Cost{24, 0.6} : Kv4Cost{18, 0.39};
+  const bool f32 = dtype == PIPESD_F32, wide = head_dim == 128;
+  if (tiles == 1) return Kv4Cost{2, 2.5, f32 ? (wide ? 0.15 : 0.105) : (wide ? 0.14 : 0.08), 1.15, 3, 2};
+  if (tiles == 2) return Kv4Cost{1, 7, f32 ? 1e30 : (wide ? 0.195 : 0.125), 1, 4, 1};
+  return Kv4Cost{10, 5, f32 ? (wide ? 1. : 0.65) : (wide ? 0.6 : 0.39), f32 && wide ? 1. : 1.8, 5, f32 && wide ? 1 : 2};
 }
 
-// The launches of a pass: clients of few and of many tiles apart, at most kKv4ClientsPerLaunch in one.  All splits of a kind
-// are as long: as short as leaves the workgroups of the pass one round on the device, and no shorter than a step of the
-// workgroup.  So what a row's sums are cut into depends on the pass, not on timing.
+// The launches of a pass: clients of few and of many tiles apart, at most kKv4ClientsPerLaunch in one.  All splits of a kind are as
+// long, some part of the longest context: as short as pays for what begins and joins them, in rounds of workgroups that fill the
+// device.  So what a row's sums are cut into depends on the pass, not on timing.
 template <class Out>  // std::vector<Kv4Launch>
 inline Kv4PlanNeeds kv4_plan(const Kv4Client* cl, int n, int dtype, int head_dim, int n_q_heads, int n_kv_heads, int n_cu, Out& out) {
   out.clear();
@@ -108,53 +108,59 @@ inline Kv4PlanNeeds kv4_plan(const Kv4Client* cl, int n, int dtype, int head_dim
   const Kv4Cost one = kv4_cost(1, dtype, head_dim), two = kv4_cost(2, dtype, head_dim), eight = kv4_cost(kKv4WideTiles, dtype, head_dim);
   auto tiles_of = [&](const Kv4Client& c) { return attn_query_tiles(group, c.n_rows); };
   auto sets = [&](const Kv4Client& c, int tiles) { return (tiles_of(c) + tiles - 1) / tiles; };
-  // Many tiles: clients whose steps are cheaper so, if together they save what the other launch costs.
-  auto gain = [&](const Kv4Client& c) { return std::min(one.step * sets(c, 1), two.step * sets(c, 2)) - eight.step * sets(c, kKv4WideTiles); };
-  double saved = 0;
-  bool few = false;
-  for (int i = 0; i < n; ++i) {
-    if (cl[i].n_rows > 0 && gain(cl[i]) > 0) saved += gain(cl[i]) * n_kv_heads * cl[i].len / 32 / n_cu;
-    else few |= cl[i].n_rows > 0;
-  }
-  const bool any_wide = saved > eight.start - (few ? 0 : one.start);
-  for (int wide = 0; wide < 2; ++wide) {
-    auto mine = [&](const Kv4Client& c) { return c.n_rows > 0 && (any_wide && gain(c) > 0) == (wide != 0); };
+  // The best span for workgroups of `tiles`, and the time that it takes, of the clients that `mine` picks.
+  auto best = [&](int tiles, const Kv4Cost& cost, auto mine, int64_t* span) {
+    const int64_t step = 32 * kKv4FewWaves, room = (int64_t)cost.resident * n_cu;
     int longest = 0;
-    double work1 = 0, work2 = 0;  // steps of 32 tokens of all workgroups, of one tile and of two
-    for (int i = 0; i < n; ++i) {
-      if (!mine(cl[i])) continue;
-      longest = std::max(longest, (int)cl[i].len);
-      work1 += (double)n_kv_heads * sets(cl[i], 1) * cl[i].len / 32;
-      work2 += (double)n_kv_heads * sets(cl[i], 2) * cl[i].len / 32;
-    }
-    if (longest == 0) continue;
-    int wg_tiles = kKv4WideTiles, step = 256, resident = 2;  // resident: workgroups that a compute unit holds at once
-    if (wide) {
-      if (head_dim == 128 && dtype == PIPESD_F32) resident = 1;
-    } else {
-      wg_tiles = one.start + one.step * work1 / n_cu <= two.start + two.step * work2 / n_cu ? 1 : 2;
-      step = kv4_few_waves(wg_tiles) * 32;
-    }
-    auto workgroups = [&](int64_t span) {
-      int64_t w = 0;
+    for (int i = 0; i < n; ++i)
+      if (mine(cl[i])) longest = std::max(longest, (int)cl[i].len);
+    double time = 1e300;
+    int64_t last = 0;
+    const int64_t cut = std::max<int64_t>(1, longest - kKv4SplitSlack);
+    for (int halves = 2; halves <= 2 * kKv4MaxSplits; halves += halves < 16 ? 1 : 2) {  // half parts of the longest context
+      const int64_t s = ((2 * cut + halves - 1) / halves + step - 1) / step * step;
+      if (s == last) continue;
+      last = s;
+      int64_t groups = 0;
       for (int i = 0; i < n; ++i)
-        if (mine(cl[i])) w += (int64_t)n_kv_heads * sets(cl[i], wg_tiles) * kv4_splits(cl[i].len, span);
-      return w;
-    };
-    // (a split costs what joins it, about the time of three steps: none below 768 tokens)
-    const int64_t room = (int64_t)resident * n_cu;
-    int64_t span = std::max<int64_t>(step, longest <= 768 ? longest : 0);
-    span = std::max<int64_t>(span, std::min<int64_t>(workgroups(1) / room, longest));  // (no shorter one would do)
-    span = (span + step - 1) / step * step;
-    while (workgroups(span) > room && span < longest) span += span < 16 * step ? step : span / 16 / step * step;
-    span = std::max<int64_t>(span, ((longest + kKv4MaxSplits - 1) / kKv4MaxSplits + step - 1) / step * step);
+        if (mine(cl[i])) groups += (int64_t)n_kv_heads * sets(cl[i], tiles) * kv4_splits(cl[i].len, s);
+      const double walk = std::min<double>(s, longest) / 32 * cost.step;
+      const int64_t rounds = groups / room, left = groups % room;  // whole rounds, and what the last has
+      const double t = cost.start + rounds * (walk * cost.resident + cost.begin) +
+                       (left ? walk * (left <= n_cu ? cost.alone : cost.resident) + cost.begin : 0) + (s < cut ? cost.join : 0);
+      if (t < time) time = t, *span = s;
+      if (rounds > 3) break;
+    }
+    return time;
+  };
+  // Many tiles: clients whose steps are cheaper so, if that pays for the other launch.
+  auto all = [&](const Kv4Client& c) { return c.n_rows > 0; };
+  auto many = [&](const Kv4Client& c) { return c.n_rows > 0 && eight.step * sets(c, kKv4WideTiles) < std::min(one.step * sets(c, 1), two.step * sets(c, 2)); };
+  auto others = [&](const Kv4Client& c) { return c.n_rows > 0 && !many(c); };
+  bool any = false, any_many = false, any_others = false;
+  for (int i = 0; i < n; ++i) any |= all(cl[i]), any_many |= many(cl[i]), any_others |= others(cl[i]);
+  if (!any) return need;
+  int64_t span1 = 0, span2 = 0, span8 = 0;
+  double time1 = best(1, one, all, &span1), time2 = best(2, two, all, &span2);
+  bool any_wide = false;
+  if (any_many) {
+    int64_t s1 = 0, s2 = 0;
+    const double t1 = any_others ? best(1, one, others, &s1) : 0, t2 = any_others ? best(2, two, others, &s2) : 0;
+    any_wide = std::min(t1, t2) + best(kKv4WideTiles, eight, many, &span8) < std::min(time1, time2);
+    if (any_wide) time1 = t1, time2 = t2, span1 = s1, span2 = s2;
+  }
+  for (int wide = 0; wide < 2; ++wide) {
+    if (wide ? !any_wide : any_wide && !any_others) continue;
+    auto mine = [&](const Kv4Client& c) { return c.n_rows > 0 && (any_wide && many(c)) == (wide != 0); };
+    const int wg_tiles = wide ? kKv4WideTiles : time1 <= time2 ? 1 : 2;
+    const int64_t span = wide ? span8 : wg_tiles == 1 ? span1 : span2;
     Kv4Launch l{};
     auto flush = [&] {
       if (l.c.n == 0) return;
       for (int i = l.c.n; i < kKv4ClientsPerLaunch; ++i) l.c.first[i] = l.c.items;
       for (int i = 0; i < l.c.n; ++i) {  // (few tiles: where the last workgroup would go to memory 4 times and more.  4 rows
         // behind 20000 tokens: 15.3 us apart, 17.2 not; 4 such clients, 2 times: 26.3 and 24.9)
-        const int threads = kv4_few_waves(wg_tiles) * 64, tasks = std::min(group * l.c.n_rows[i], wg_tiles * 16) * (head_dim / 4);
+        const int threads = kKv4FewWaves * 64, tasks = std::min(group * l.c.n_rows[i], wg_tiles * 16) * (head_dim / 4);
         int shares = 1;
         while (2 * shares * tasks <= threads) shares *= 2;
         const int turns = (tasks + threads - 1) / threads * ((l.c.nsplit[i] + 8 * shares - 1) / (8 * shares));

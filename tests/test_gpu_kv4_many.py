@@ -17,8 +17,8 @@ gpu = pytest.mark.gpu
 CASES = {
     "128": ((64, 8, 128), "bf16", [7936], [256]),
     "64": ((32, 8, 64), "bf16", [3100], [1024]),
-    "64_f32": ((32, 32, 64), "f32", [15000], [128]),
-    "128_f32": ((32, 4, 128), "f32", [9000], [512]),
+    "64_f32": ((32, 32, 64), "f32", [15000], [512]),
+    "128_f32": ((32, 4, 128), "f32", [9000], [1024]),
     "group_of_7": ((7, 1, 128), "bf16", [7003], [2045]),
     "long": ((32, 8, 128), "bf16", [118001], [32]),
     "beside_few": ((32, 8, 64), "bf16", [5000, 3971, 100], [1, 1536, 3]),

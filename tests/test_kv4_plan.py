@@ -140,18 +140,18 @@ def test_the_cases_of_many_tiles_are_that(plan, name):
     if name == "long":
         assert got[0][1] > 32
     if name == "prompt":
-        assert got[1][1] == 1
+        assert got[0][1] == 1
 
 
 def test_what_passes_are_given_to(plan):
     """(tiles of a workgroup, splits) where both sides have been measured: the faster one."""
-    assert kinds(plan, (32, 8, 128), "bf16", [2040] * 4, [8] * 4) == [(1, 8)] * 4  # 13.5 us; 18.2 with two
-    assert {t for t, _ in kinds(plan, (32, 8, 128), "bf16", [4096] * 32, [8] * 32)} == {2}  # 45.0; 46.6 with one
-    assert {t for t, _ in kinds(plan, (32, 8, 128), "bf16", [8192] * 32, [4] * 32)} == {1}  # 60; 73 with two
-    assert kinds(plan, (32, 8, 128), "bf16", [4096], [64])[0][0] == 1  # 19; 26 with eight
-    assert kinds(plan, (32, 8, 128), "bf16", [65536], [64])[0][0] == 8  # 101; 115 with two
+    assert kinds(plan, (32, 8, 128), "bf16", [2040] * 4, [8] * 4) == [(1, 8)] * 4  # 11.7 us
+    assert {t for t, _ in kinds(plan, (32, 8, 128), "bf16", [4096] * 32, [8] * 32)} == {2}  # 41; 48 with one
+    assert {t for t, _ in kinds(plan, (32, 8, 128), "bf16", [8192] * 32, [4] * 32)} == {1}  # 57; 73 with two
+    assert kinds(plan, (32, 8, 128), "bf16", [4096], [64])[0][0] == 1  # 16; 26 with eight
+    assert kinds(plan, (32, 8, 128), "bf16", [65536], [64])[0][0] == 8  # 98; 115 with two
     assert kinds(plan, (32, 8, 128), "bf16", [6144], [2048]) == [(8, 1)]  # 265; 349 with two
-    assert kinds(plan, (32, 8, 64), "bf16", [6144], [2048]) == [(8, 1)]  # 186; 225 with two
+    assert kinds(plan, (32, 8, 64), "bf16", [6144], [2048]) == [(8, 1)]  # 182; 225 with two
     assert kinds(plan, (32, 8, 128), "f32", [2048], [2048])[0][0] == 8  # 210; 248 with one
     assert kinds(plan, (32, 8, 128), "bf16", [600], [1]) == [(1, 1)]  # (no split below 768 tokens)
 
