@@ -413,7 +413,7 @@ int pipesd_kv4_append(pipesd_kv4 *kv, int32_t layer, const void *k, int64_t k_st
  *   mass    device fp32 [max_seqs][n_layers][n_kv_heads][mass_stride], or NULL: what weight the cached tokens were given.  For
  *           each client of the pass, at this layer, mass[t] = decay * mass[t] + (sum of token t's weights over the client's rows
  *           and the query heads of the cache head), 0 <= decay <= 1; the pass's own tokens, and all with decay 0, start at 0
- *           whatever the buffer held.
+ *           whatever the buffer held.  A client without new rows only has its weights decayed.
  * A row's result depends on its own client's tokens and queries alone.  Into how many pieces a context is cut, and so the
  * order of sums, goes by the lengths and numbers of rows of all clients of the pass; the same pass gives the same bits.
  * EINVAL: also a client longer than mass_stride, or a decay outside [0, 1]; ESTATE: no pass that can attend, no pool. */

@@ -46,6 +46,7 @@ struct pipesd_kv4 {
   // the pass
   std::vector<Kv4Client> pass, next_pass;  // (next_..: where the next pass is made)
   std::vector<Kv4Launch> launches, next_launches;
+  std::vector<int32_t> idle, next_idle;    // its clients without new rows
   std::vector<int32_t> had;
   bool pass_open = false, attends = false;
 
@@ -259,12 +260,15 @@ extern "C" int pipesd_kv4_extend(pipesd_kv4* kv, int32_t n_seqs, const int32_t* 
     std::vector<int32_t>& had = kv->had;
     plan.clear();
     launches.clear();
+    std::vector<int32_t>& idle = kv->next_idle;
     had.resize(n_seqs);
     plan.reserve(n_seqs);
+    idle.clear();
     int32_t row = 0;
     for (int32_t i = 0; i < n_seqs; ++i) {
       had[i] = (int32_t)kv->seqs[seq_ids[i]].blocks.size();
       if (n_new[i]) plan.push_back(Kv4Client{seq_ids[i], n_new[i], row, kv->seqs[seq_ids[i]].len + n_new[i]});
+      else idle.push_back(seq_ids[i]);
       row += n_new[i];
     }
     if (kv->pool && attends) {
@@ -306,6 +310,7 @@ extern "C" int pipesd_kv4_extend(pipesd_kv4* kv, int32_t n_seqs, const int32_t* 
     for (int32_t i = 0; i < n_seqs; ++i) kv->seqs[seq_ids[i]].in_pass = true;
     kv->pass.swap(plan);
     kv->launches.swap(launches);
+    kv->idle.swap(idle);
     kv->attends = attends;
     kv->pass_open = true;
     return PIPESD_OK;
@@ -353,6 +358,8 @@ extern "C" int pipesd_kv4_attend(pipesd_kv4* kv, int32_t layer, const void* q, i
     if (!(decay >= 0.f) || !(decay <= 1.f)) return PIPESD_EINVAL;
     for (const Kv4Client& c : kv->pass)
       if (c.len > mass_stride) return PIPESD_EINVAL;
+    for (int32_t seq : kv->idle)
+      if (kv->seqs[seq].len > mass_stride) return PIPESD_EINVAL;
   }
   hipStream_t st = (hipStream_t)stream;
   Kv4AttendCall a{};
@@ -376,6 +383,19 @@ extern "C" int pipesd_kv4_attend(pipesd_kv4* kv, int32_t layer, const void* q, i
   for (const Kv4Launch& l : kv->launches) {
     HIP_TRY(launch_kv4_attend(a, l, st));
     if (mass) HIP_TRY(launch_kv4_mass(a, l.c, st));
+  }
+  if (mass && decay != 1.f) {
+    Kv4Idle idle;
+    idle.n = idle.most = 0;
+    for (size_t i = 0; i < kv->idle.size(); ++i) {
+      idle.seq[idle.n] = kv->idle[i];
+      idle.len[idle.n] = kv->seqs[kv->idle[i]].len;
+      idle.most = std::max(idle.most, idle.len[idle.n++]);
+      if (idle.n == kKv4ClientsPerLaunch || i + 1 == kv->idle.size()) {
+        HIP_TRY(launch_kv4_decay(a, idle, st));
+        idle.n = idle.most = 0;
+      }
+    }
   }
   return PIPESD_OK;
 }

@@ -1112,4 +1112,24 @@ hipError_t launch_kv4_mass(const Kv4AttendCall& c, const Kv4Clients& cl, hipStre
   return c.dtype == PIPESD_F32 ? mass_of<64, float>(c, cl, st) : mass_of<64, uint16_t>(c, cl, st);
 }
 
+// Of a client without rows nothing is added.  Workgroup (cache head, 1024 tokens, client); what it reads and writes bounds it.
+constexpr int kDecayPer = 4;
+__global__ __launch_bounds__(256) void kv4_decay_kernel(Kv4AttendCall a, Kv4Idle cl, int first_piece) {
+  const int ci = blockIdx.z, len = cl.len[ci];
+  float* out = a.mass + (((int64_t)cl.seq[ci] * a.view.n_layers + a.layer) * a.view.n_kv_heads + blockIdx.x) * a.mass_stride;
+  const int t0 = (first_piece + (int)blockIdx.y) * (256 * kDecayPer) + (int)threadIdx.x;
+#pragma unroll
+  for (int i = 0; i < kDecayPer; ++i) {
+    const int t = t0 + i * 256;
+    if (t < len) out[t] = a.decay != 0.f ? a.decay * out[t] : 0.f;  // (0: whatever was there)
+  }
+}
+hipError_t launch_kv4_decay(const Kv4AttendCall& c, const Kv4Idle& cl, hipStream_t st) {
+  constexpr int kPiece = 256 * kDecayPer;
+  const int pieces = cl.most / kPiece + (cl.most % kPiece != 0);
+  for (int first = 0; first < pieces; first += kKv4MaxItems)
+    kv4_decay_kernel<<<dim3(c.view.n_kv_heads, std::min(pieces - first, kKv4MaxItems), cl.n), 256, 0, st>>>(c, cl, first);
+  return hipGetLastError();
+}
+
 }  // namespace pipesd

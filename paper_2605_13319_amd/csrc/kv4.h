@@ -232,6 +232,11 @@ struct Kv4AttendCall {
 constexpr int kKv4PartPad = 4;  // a partial row is [head_dim values, max, sum, 2 unused]
 hipError_t launch_kv4_attend(const Kv4AttendCall& c, const Kv4Launch& l, hipStream_t st);
 hipError_t launch_kv4_mass(const Kv4AttendCall& c, const Kv4Clients& clients, hipStream_t st);
+struct Kv4Idle {  // clients of a pass without rows: their weights are decayed, no more
+  int32_t n, most;  // most: largest length
+  int32_t seq[kKv4ClientsPerLaunch], len[kKv4ClientsPerLaunch];
+};
+hipError_t launch_kv4_decay(const Kv4AttendCall& c, const Kv4Idle& clients, hipStream_t st);
 
 struct Kv4Cuts {
   int32_t n, keep, recent;

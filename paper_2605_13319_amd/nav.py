@@ -600,7 +600,7 @@ class KV4Cache:
     def attend(self, layer: int, q, out=None, limits=None, mass=None, decay: float = 1.0):
         """Attention of the pass's queries over a layer of the cache; returns `out` (a new tensor like q if None).
         limits: int32 [rows], tokens that each row sees.  mass: float32 [max_seqs][n_layers][n_kv_heads][tokens], the weight
-        that cached tokens were given, accumulated."""
+        that cached tokens were given, accumulated (of a client of the pass without new rows only decayed)."""
         heads = self.shape.n_q_heads
         qp, qs = self._tensor(q, heads, "q")
         if out is None:
