@@ -407,7 +407,8 @@ int pipesd_kv4_append(pipesd_kv4 *kv, int32_t layer, const void *k, int64_t k_st
                       void *stream);
 
 /* Attention of the pass's queries over one layer of the cache: q, out device [rows][n_q_heads * head_dim], softmax of
- * q . k / sqrt(head_dim), query head g reads head g / (n_q_heads / n_kv_heads) of the cache.
+ * q . k / sqrt(head_dim), query head g reads head g / (n_q_heads / n_kv_heads) of the cache.  Without mass, out may be q itself (the
+ * same address and stride); otherwise no row of out shares memory with one of q (columns of one wider matrix do not).
  *   limits  device int32 [rows]: how many of its client's tokens (from the first) a row sees, cut to 0 .. its length; NULL:
  *           all up to the row's own.  A row that sees nothing gets zeros.
  *   mass    device fp32 [max_seqs][n_layers][n_kv_heads][mass_stride], or NULL: what weight the cached tokens were given.  For
@@ -416,7 +417,8 @@ int pipesd_kv4_append(pipesd_kv4 *kv, int32_t layer, const void *k, int64_t k_st
  *           whatever the buffer held.  A client without new rows only has its weights decayed.
  * A row's result depends on its own client's tokens and queries alone.  Into how many pieces a context is cut, and so the
  * order of sums, goes by the lengths and numbers of rows of all clients of the pass; the same pass gives the same bits.
- * EINVAL: also a client longer than mass_stride, or a decay outside [0, 1]; ESTATE: no pass that can attend, no pool. */
+ * EINVAL: also a client longer than mass_stride, a decay outside [0, 1], or out over q where that is not allowed; ESTATE: no
+ * pass that can attend, no pool. */
 int pipesd_kv4_attend(pipesd_kv4 *kv, int32_t layer, const void *q, int64_t q_stride, const int32_t *limits, void *out,
                       int64_t out_stride, float *mass, int64_t mass_stride, float decay, void *stream);
 

@@ -322,6 +322,20 @@ static bool kv4_rows_ok(const pipesd_config& c, const void* p, int64_t stride, i
   return p && ((uintptr_t)p & 15) == 0 && stride >= (int64_t)heads * c.head_dim && (stride * e) % 16 == 0;
 }
 
+// Whether a row of a and a row of b share bytes: `rows` of `width` bytes each, strides of at least that.
+static bool kv4_rows_overlap(const void* a, int64_t a_stride, const void* b, int64_t b_stride, int64_t rows, int64_t width) {
+  const uintptr_t pa = (uintptr_t)a, pb = (uintptr_t)b;
+  const uintptr_t reach = (uintptr_t)((rows - 1) * (pa < pb ? a_stride : b_stride) + width);  // of the one that begins first
+  if ((pa < pb ? pb - pa : pa - pb) >= reach) return false;
+  int64_t at = (int64_t)(pb - pa);  // of b's row j, from a's row i
+  for (int64_t i = 0, j = 0; i < rows && j < rows;) {
+    if (at >= width) ++i, at -= a_stride;
+    else if (at <= -width) ++j, at += b_stride;
+    else return true;
+  }
+  return false;
+}
+
 static void kv4_add_range(Kv4Ranges& r, int32_t table_off, int32_t first, int32_t count, int32_t row_off) {
   r.table_off[r.n] = table_off;
   r.first[r.n] = first;
@@ -353,6 +367,12 @@ extern "C" int pipesd_kv4_attend(pipesd_kv4* kv, int32_t layer, const void* q, i
   if (!kv || layer < 0 || layer >= kv->cfg.n_layers) return PIPESD_EINVAL;
   if (!kv4_rows_ok(kv->cfg, q, q_stride, kv->cfg.n_q_heads) || !kv4_rows_ok(kv->cfg, out, out_stride, kv->cfg.n_q_heads)) return PIPESD_EINVAL;
   if (((uintptr_t)limits & 3) || ((uintptr_t)mass & 3)) return PIPESD_EINVAL;
+  // Results where the queries are: every workgroup reads its rows' queries before it, or who joins its splits, writes these rows.
+  // The weights are formed from the queries again, when all results have been written.
+  if (kv->pass_open && (mass || q != out || q_stride != out_stride)) {
+    const int64_t e = kv->cfg.dtype == PIPESD_F32 ? 4 : 2, rows = kv->pass.back().row_off + kv->pass.back().n_rows;
+    if (kv4_rows_overlap(q, q_stride * e, out, out_stride * e, rows, (int64_t)kv->cfg.n_q_heads * kv->cfg.head_dim * e)) return PIPESD_EINVAL;
+  }
   if (!kv->pool || !kv->pass_open || !kv->attends) return PIPESD_ESTATE;
   if (mass) {
     if (!(decay >= 0.f) || !(decay <= 1.f)) return PIPESD_EINVAL;

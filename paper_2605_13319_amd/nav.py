@@ -598,9 +598,10 @@ class KV4Cache:
         _check(_lib.pipesd_kv4_append(self.handle, layer, kp, ks, vp, vs, self._stream()), "pipesd_kv4_append")
 
     def attend(self, layer: int, q, out=None, limits=None, mass=None, decay: float = 1.0):
-        """Attention of the pass's queries over a layer of the cache; returns `out` (a new tensor like q if None).
-        limits: int32 [rows], tokens that each row sees.  mass: float32 [max_seqs][n_layers][n_kv_heads][tokens], the weight
-        that cached tokens were given, accumulated (of a client of the pass without new rows only decayed)."""
+        """Attention of the pass's queries over a layer of the cache; returns `out` (a new tensor like q if None;
+        may be q itself where no weights are asked for).  limits: int32 [rows], tokens that each row sees.  mass: float32
+        [max_seqs][n_layers][n_kv_heads][tokens], the weight that cached tokens were given, accumulated (of a client of the pass
+        without new rows only decayed)."""
         heads = self.shape.n_q_heads
         qp, qs = self._tensor(q, heads, "q")
         if out is None:
