@@ -373,7 +373,8 @@ int pipesd_bo_suggest(const double *x, const double *y, int32_t n, double length
  * model rotates them), of the config's dtype (PIPESD_F32 or PIPESD_BF16).  A forward over new rows of some clients is a
  * PASS: pipesd_kv4_extend makes room for the rows, then, layer by layer, pipesd_kv4_append rounds that layer's keys and
  * values into the cache and pipesd_kv4_attend lets its queries read it.  Rows of a pass lie one client after the other, in
- * the order of pipesd_kv4_extend.  A pass ends when the next begins, or when one of its clients is cut.
+ * the order of pipesd_kv4_extend.  A pass ends when the next begins, or when one of its clients loses tokens: when it is
+ * shortened, cut in place, or becomes what another is cut into.
  *
  * All device work of a handle has to be ordered by its caller: one stream, or events between streams.  Nothing in here
  * waits for the device but creation, destruction and where stated; pointers to device memory need 16-byte alignment

@@ -485,7 +485,9 @@ extern "C" int pipesd_kv4_evict(pipesd_kv4* kv, int32_t n_seqs, const int32_t* s
       len[i] = kv->seqs[seq_ids[i]].len;
     }
     // what was in the targets is gone from here on, also if a launch fails: then they are empty, and clients cut in place whole
-    kv4_close_pass(kv);
+    bool touched = false;
+    for (int32_t i = 0; i < n_seqs; ++i) touched |= kv->seqs[into[i]].in_pass;  // (a client copied into another stays as it is)
+    if (touched) kv4_close_pass(kv);
     for (int32_t i = 0; i < n_seqs; ++i)
       if (into[i] != seq_ids[i]) kv4_release(kv, kv->seqs[into[i]], 0);
     std::vector<std::vector<int32_t>> old(n_seqs);
