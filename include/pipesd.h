@@ -378,7 +378,12 @@ int pipesd_bo_suggest(const double *x, const double *y, int32_t n, double length
  *
  * All device work of a handle has to be ordered by its caller: one stream, or events between streams.  Nothing in here
  * waits for the device but creation, destruction and where stated; pointers to device memory need 16-byte alignment
- * (4-byte for float and int32 arrays), strides are in elements and whole multiples of 16 bytes. */
+ * (4-byte for float and int32 arrays), strides are in elements and whole multiples of 16 bytes.
+ *
+ * Recorded into a graph, pipesd_kv4_append, pipesd_kv4_attend and pipesd_kv4_read do at every replay what they did for the lengths
+ * and block tables of the recording: replay while the clients hold the blocks that they held then (at least as many tokens, nothing
+ * cut since).  On a stream that is being recorded pipesd_kv4_extend returns ESTATE and changes nothing if it would have to write
+ * block tables or grow scratch (it has not where rows that were taken back come again), and so does pipesd_kv4_evict. */
 typedef struct pipesd_kv4 pipesd_kv4;
 enum { PIPESD_KV4_MAX_PASS_SEQS = 256, PIPESD_KV4_MAX_ROWS = 2048 };
 
@@ -399,7 +404,7 @@ int pipesd_kv4_destroy(pipesd_kv4 *kv);
 /* Begin a pass: client seq_ids[i] (pairwise distinct, 1 <= n_seqs <= 256) gets n_new[i] >= 0 more tokens, at least one in all.
  * A pass in which no client gets more than PIPESD_KV4_MAX_ROWS can attend; others only append.  Larger passes than
  * pipesd_kv4_create provided for grow the handle's scratch, which waits for the device.
- * ENOMEM: the pool has too few free blocks, or the scratch cannot grow. */
+ * ENOMEM: the pool has too few free blocks, or the scratch cannot grow; ESTATE: see above, of streams being recorded. */
 int pipesd_kv4_extend(pipesd_kv4 *kv, int32_t n_seqs, const int32_t *seq_ids, const int32_t *n_new, void *stream);
 
 /* Round the pass's keys and values of one layer into the cache: k, v device [rows][n_kv_heads * head_dim], rows k_stride and
@@ -436,7 +441,7 @@ int pipesd_kv4_read(const pipesd_kv4 *kv, int32_t n_seqs, const int32_t *seq_ids
  * old blocks count, a client's own that is cut in place do not).  The kept weights go to the target's `mass`, and the kept
  * indices to device int32 kept [n_seqs][n_layers][n_kv_heads][keep].
  * EINVAL: also into[i] that is another client being cut, or a client longer than mass_stride; ESTATE: a client of fewer than
- * `keep` tokens, no pool; ENOMEM: too few free blocks. */
+ * `keep` tokens, no pool, a stream being recorded; ENOMEM: too few free blocks. */
 int pipesd_kv4_evict(pipesd_kv4 *kv, int32_t n_seqs, const int32_t *seq_ids, const int32_t *into, int32_t keep, int32_t recent,
                      float *mass, int64_t mass_stride, int32_t *kept, void *stream);
 

@@ -211,12 +211,22 @@ extern "C" int pipesd_kv4_truncate(pipesd_kv4* kv, int32_t n_seqs, const int32_t
   });
 }
 
+// What writes block tables is not recorded: a replay would write them again, when the blocks may be another client's, and until the
+// first replay the device has not what the host takes it to have.
+static int kv4_not_recorded(hipStream_t st) {
+  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+  HIP_TRY(hipStreamIsCapturing(st, &status));
+  return status == hipStreamCaptureStatusNone ? PIPESD_OK : PIPESD_ESTATE;
+}
+
 // sends what is new of the block tables, some per launch.  (A block that a client gave back and got again is there already.)
 static int kv4_send(pipesd_kv4* kv, int32_t n, const int32_t* seq_ids, const int32_t* from, hipStream_t st) {
   Kv4TableUpdate u;
   u.n = 0;
   auto flush = [&]() -> int {
-    if (u.n) HIP_TRY(launch_kv4_table(u, kv->table, st));
+    if (u.n == 0) return PIPESD_OK;
+    if (int rc = kv4_not_recorded(st)) return rc;
+    HIP_TRY(launch_kv4_table(u, kv->table, st));
     u.n = 0;
     return PIPESD_OK;
   };
@@ -276,10 +286,13 @@ extern "C" int pipesd_kv4_extend(pipesd_kv4* kv, int32_t n_seqs, const int32_t* 
       if (need.part_tiles > (size_t)INT32_MAX || need.counters > (size_t)INT32_MAX) return PIPESD_ENOMEM;
       for (Kv4Launch& l : launches)
         for (int32_t j = 0; j < l.c.n; ++j) l.c.table_off[j] = kv->table_off(l.c.seq[j]);
+      const size_t parts = need.part_tiles * 16 * (cfg.head_dim + kKv4PartPad), sums = (size_t)total * cfg.n_q_heads;
       int e;
-      if ((e = kv4_grow(&kv->part, &kv->part_cap, need.part_tiles * 16 * (cfg.head_dim + kKv4PartPad), false))) return e;
+      if (parts > kv->part_cap || need.counters > kv->counters_cap || sums > kv->lse_cap)
+        if ((e = kv4_not_recorded(st))) return e;
+      if ((e = kv4_grow(&kv->part, &kv->part_cap, parts, false))) return e;
       if ((e = kv4_grow(&kv->counters, &kv->counters_cap, need.counters, true))) return e;
-      if ((e = kv4_grow(&kv->lse, &kv->lse_cap, (size_t)total * cfg.n_q_heads, false))) return e;
+      if ((e = kv4_grow(&kv->lse, &kv->lse_cap, sums, false))) return e;
     }
     for (int32_t i = 0; i < n_seqs; ++i) {
       Kv4Seq& s = kv->seqs[seq_ids[i]];
@@ -296,10 +309,9 @@ extern "C" int pipesd_kv4_extend(pipesd_kv4* kv, int32_t n_seqs, const int32_t* 
         kv->free_list.pop_back();
       }
     }
-    kv4_close_pass(kv);
     if (kv->pool) {
       if (int rc = kv4_send(kv, n_seqs, seq_ids, had.data(), st)) {
-        for (int32_t i = 0; i < n_seqs; ++i) {
+        for (int32_t i = n_seqs - 1; i >= 0; --i) {  // (backwards: the free blocks' order too is as it was)
           Kv4Seq& s = kv->seqs[seq_ids[i]];
           std::fill(s.sent[s.which].begin() + had[i], s.sent[s.which].end(), -1);
           kv4_release(kv, s, s.len - n_new[i]);
@@ -307,6 +319,7 @@ extern "C" int pipesd_kv4_extend(pipesd_kv4* kv, int32_t n_seqs, const int32_t* 
         return rc;
       }
     }
+    kv4_close_pass(kv);
     for (int32_t i = 0; i < n_seqs; ++i) kv->seqs[seq_ids[i]].in_pass = true;
     kv->pass.swap(plan);
     kv->launches.swap(launches);
@@ -470,6 +483,7 @@ extern "C" int pipesd_kv4_evict(pipesd_kv4* kv, int32_t n_seqs, const int32_t* s
       if (into[i] != seq_ids[i]) have += (int64_t)kv->seqs[into[i]].blocks.size();  // what the target holds is given up first
     }
     if (!kv->pool) return PIPESD_ESTATE;
+    if (int rc = kv4_not_recorded(st)) return rc;
     const int32_t nb = kv4_blocks(keep);
     if ((int64_t)nb * n_seqs > have) return PIPESD_ENOMEM;
 
