@@ -403,7 +403,8 @@ int pipesd_kv4_destroy(pipesd_kv4 *kv);
 
 /* Begin a pass: client seq_ids[i] (pairwise distinct, 1 <= n_seqs <= 256) gets n_new[i] >= 0 more tokens, at least one in all.
  * A pass in which no client gets more than PIPESD_KV4_MAX_ROWS can attend; others only append.  Larger passes than
- * pipesd_kv4_create provided for grow the handle's scratch, which waits for the device.
+ * pipesd_kv4_create provided for grow the handle's scratch, which waits for the device; what it was before stays, for calls
+ * recorded with it, until pipesd_kv4_destroy.
  * ENOMEM: the pool has too few free blocks, or the scratch cannot grow; ESTATE: see above, of streams being recorded. */
 int pipesd_kv4_extend(pipesd_kv4 *kv, int32_t n_seqs, const int32_t *seq_ids, const int32_t *n_new, void *stream);
 

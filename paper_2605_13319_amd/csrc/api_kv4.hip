@@ -43,6 +43,7 @@ struct pipesd_kv4 {
   size_t counters_cap = 0;
   float* lse = nullptr;
   size_t lse_cap = 0;
+  std::vector<void*> old;  // buffers that have grown since
   // the pass
   std::vector<Kv4Client> pass, next_pass;  // (next_..: where the next pass is made)
   std::vector<Kv4Launch> launches, next_launches;
@@ -92,11 +93,13 @@ extern "C" size_t pipesd_kv4_block_bytes(const pipesd_config* cfg, int32_t block
   return (size_t)cfg->n_layers * cfg->n_kv_heads * kv4_record_bytes(cfg->head_dim);
 }
 
-// grows a buffer of the pass; the device may still be using the old one
+// Grows a buffer of the pass.  The old one stays until the handle ends: the device may still be using it, and recorded calls hold its
+// address (half as much again each time: all old ones together are less than twice the last).
 template <class T>
-static int kv4_grow(T** p, size_t* cap, size_t want, bool zero) {
+static int kv4_grow(pipesd_kv4* kv, T** p, size_t* cap, size_t want, bool zero) {
   if (want <= *cap) return PIPESD_OK;
   want += want / 2;
+  kv->old.reserve(kv->old.size() + 1);
   T* fresh = nullptr;
   if (hipMalloc((void**)&fresh, want * sizeof(T)) != hipSuccess) {
     (void)hipGetLastError();
@@ -108,7 +111,7 @@ static int kv4_grow(T** p, size_t* cap, size_t want, bool zero) {
     (void)hipFree(fresh);
     return hip_fail(e, "growing a buffer of the 4-bit cache");
   }
-  if (*p) (void)hipFree(*p);
+  if (*p) kv->old.push_back(*p);
   *p = fresh;
   *cap = want;
   return PIPESD_OK;
@@ -120,6 +123,7 @@ extern "C" int pipesd_kv4_destroy(pipesd_kv4* kv) {
     (void)hipDeviceSynchronize();
     for (void* p : {(void*)kv->table, (void*)kv->part, (void*)kv->counters, (void*)kv->lse})
       if (p) (void)hipFree(p);
+    for (void* p : kv->old) (void)hipFree(p);
   }
   delete kv;
   return PIPESD_OK;
@@ -166,9 +170,9 @@ extern "C" int pipesd_kv4_create(const pipesd_config* cfg, int32_t max_seqs, int
         counts = std::max(counts, need.counters);
       }
     int e;
-    if ((e = kv4_grow(&kv->part, &kv->part_cap, tiles * 16 * (cfg->head_dim + kKv4PartPad), false))) return e;
-    if ((e = kv4_grow(&kv->counters, &kv->counters_cap, counts, true))) return e;
-    return kv4_grow(&kv->lse, &kv->lse_cap, (size_t)clients * kMaxRows * cfg->n_q_heads, false);
+    if ((e = kv4_grow(kv, &kv->part, &kv->part_cap, tiles * 16 * (cfg->head_dim + kKv4PartPad), false))) return e;
+    if ((e = kv4_grow(kv, &kv->counters, &kv->counters_cap, counts, true))) return e;
+    return kv4_grow(kv, &kv->lse, &kv->lse_cap, (size_t)clients * kMaxRows * cfg->n_q_heads, false);
   });
   if (rc) {
     pipesd_kv4_destroy(kv);
@@ -290,9 +294,9 @@ extern "C" int pipesd_kv4_extend(pipesd_kv4* kv, int32_t n_seqs, const int32_t* 
       int e;
       if (parts > kv->part_cap || need.counters > kv->counters_cap || sums > kv->lse_cap)
         if ((e = kv4_not_recorded(st))) return e;
-      if ((e = kv4_grow(&kv->part, &kv->part_cap, parts, false))) return e;
-      if ((e = kv4_grow(&kv->counters, &kv->counters_cap, need.counters, true))) return e;
-      if ((e = kv4_grow(&kv->lse, &kv->lse_cap, sums, false))) return e;
+      if ((e = kv4_grow(kv, &kv->part, &kv->part_cap, parts, false))) return e;
+      if ((e = kv4_grow(kv, &kv->counters, &kv->counters_cap, need.counters, true))) return e;
+      if ((e = kv4_grow(kv, &kv->lse, &kv->lse_cap, sums, false))) return e;
     }
     for (int32_t i = 0; i < n_seqs; ++i) {
       Kv4Seq& s = kv->seqs[seq_ids[i]];
