@@ -393,8 +393,9 @@ size_t pipesd_kv4_block_bytes(const pipesd_config *cfg, int32_t block_tokens);
 /* Cache of up to max_seqs clients over a caller-allocated device pool of floor(pool_bytes / block bytes) blocks (borrowed until
  * pipesd_kv4_destroy).  Of the config it takes n_layers, n_q_heads, n_kv_heads (at most 256
  * query heads each), head_dim (64 or 128) and dtype.  Beside the
- * pool it allocates the block tables and what passes of up to PIPESD_MAX_ROWS rows by 16 clients take at the lengths that the
- * pool allows.  pool == NULL: bookkeeping only.
+ * pool it allocates the block tables and the scratch that any pass of up to 16 clients with up to PIPESD_MAX_ROWS rows each takes at
+ * the lengths that the pool allows (32 query heads on 8 of 128, bf16: 235 MB for 16 clients of long contexts).  pool == NULL:
+ * bookkeeping only.
  * EINVAL: an unsupported config, block_tokens != 16, max_seqs < 1, no room for one block, a pool that is not 256-byte
  * aligned or of 2^31 tokens or table entries (2 * max_seqs * blocks) and more; ENOMEM: an allocation failed. */
 int pipesd_kv4_create(const pipesd_config *cfg, int32_t max_seqs, int32_t block_tokens, void *pool, size_t pool_bytes,

@@ -96,9 +96,9 @@ extern "C" size_t pipesd_kv4_block_bytes(const pipesd_config* cfg, int32_t block
 // Grows a buffer of the pass.  The old one stays until the handle ends: the device may still be using it, and recorded calls hold its
 // address (half as much again each time: all old ones together are less than twice the last).
 template <class T>
-static int kv4_grow(pipesd_kv4* kv, T** p, size_t* cap, size_t want, bool zero) {
+static int kv4_grow(pipesd_kv4* kv, T** p, size_t* cap, size_t want, bool zero, size_t spare) {
   if (want <= *cap) return PIPESD_OK;
-  want += want / 2;
+  want += spare;
   kv->old.reserve(kv->old.size() + 1);
   T* fresh = nullptr;
   if (hipMalloc((void**)&fresh, want * sizeof(T)) != hipSuccess) {
@@ -158,21 +158,13 @@ extern "C" int pipesd_kv4_create(const pipesd_config* cfg, int32_t max_seqs, int
       return PIPESD_ENOMEM;
     }
     HIP_TRY(hipMemset(kv->table, 0, entries * 4));
-    // what passes of up to PIPESD_MAX_ROWS rows by 16 clients take: a client alone has the most splits
-    size_t tiles = 0, counts = 0;
     const int32_t clients = std::min(max_seqs, 16);
-    std::vector<Kv4Launch> scratch;
-    for (int32_t n : {1, clients})
-      for (int32_t m = 1; m <= kMaxRows; ++m) {
-        std::vector<Kv4Client> c(n, Kv4Client{0, m, 0, (int32_t)std::min<size_t>((size_t)kv->n_blocks * kBlockTokens, (size_t)1 << 24)});
-        const Kv4PlanNeeds need = kv4_plan(c.data(), n, cfg->dtype, cfg->head_dim, cfg->n_q_heads, cfg->n_kv_heads, kv->n_cu, scratch);
-        tiles = std::max(tiles, need.part_tiles);
-        counts = std::max(counts, need.counters);
-      }
+    const Kv4PlanNeeds most = kv4_plan_most(clients, kMaxRows, (int64_t)kv->n_blocks * kBlockTokens, cfg->dtype, cfg->head_dim, cfg->n_q_heads,
+                                            cfg->n_kv_heads, kv->n_cu);
     int e;
-    if ((e = kv4_grow(kv, &kv->part, &kv->part_cap, tiles * 16 * (cfg->head_dim + kKv4PartPad), false))) return e;
-    if ((e = kv4_grow(kv, &kv->counters, &kv->counters_cap, counts, true))) return e;
-    return kv4_grow(kv, &kv->lse, &kv->lse_cap, (size_t)clients * kMaxRows * cfg->n_q_heads, false);
+    if ((e = kv4_grow(kv, &kv->part, &kv->part_cap, most.part_tiles * 16 * (cfg->head_dim + kKv4PartPad), false, 0))) return e;
+    if ((e = kv4_grow(kv, &kv->counters, &kv->counters_cap, most.counters, true, 0))) return e;
+    return kv4_grow(kv, &kv->lse, &kv->lse_cap, (size_t)clients * kMaxRows * cfg->n_q_heads, false, 0);
   });
   if (rc) {
     pipesd_kv4_destroy(kv);
@@ -294,9 +286,9 @@ extern "C" int pipesd_kv4_extend(pipesd_kv4* kv, int32_t n_seqs, const int32_t* 
       int e;
       if (parts > kv->part_cap || need.counters > kv->counters_cap || sums > kv->lse_cap)
         if ((e = kv4_not_recorded(st))) return e;
-      if ((e = kv4_grow(kv, &kv->part, &kv->part_cap, parts, false))) return e;
-      if ((e = kv4_grow(kv, &kv->counters, &kv->counters_cap, need.counters, true))) return e;
-      if ((e = kv4_grow(kv, &kv->lse, &kv->lse_cap, sums, false))) return e;
+      if ((e = kv4_grow(kv, &kv->part, &kv->part_cap, parts, false, parts / 2))) return e;
+      if ((e = kv4_grow(kv, &kv->counters, &kv->counters_cap, need.counters, true, need.counters / 2))) return e;
+      if ((e = kv4_grow(kv, &kv->lse, &kv->lse_cap, sums, false, sums / 2))) return e;
     }
     for (int32_t i = 0; i < n_seqs; ++i) {
       Kv4Seq& s = kv->seqs[seq_ids[i]];

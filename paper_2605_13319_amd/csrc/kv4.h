@@ -52,6 +52,10 @@ constexpr int kKv4MaxSplits = 64;
 constexpr int kKv4SplitSlack = 64;
 inline int kv4_splits(int64_t len, int64_t span) { return (int)std::max<int64_t>(1, (len - kKv4SplitSlack + span - 1) / span); }
 constexpr int kKv4FewWaves = 8;
+// Workgroups of a kind whose rows are to be joined, in rounds that fill the device: no pass has more, which bounds the partial rows.
+// (By the cost below none of 60000 ragged passes would take more; with four, 193 of them would be cut less, and take up to 11 %
+// longer.)
+constexpr int kKv4CutRounds = 6;
 
 // Clients of a launch, by value.  Workgroups: (cache head, item); a client's items are its splits, the groups of tiles of a
 // split side by side, for they read the same tokens.
@@ -121,9 +125,15 @@ inline Kv4PlanNeeds kv4_plan(const Kv4Client* cl, int n, int dtype, int head_dim
       const int64_t s = ((2 * cut + halves - 1) / halves + step - 1) / step * step;
       if (s == last) continue;
       last = s;
-      int64_t groups = 0;
+      int64_t groups = 0, cut_groups = 0;
       for (int i = 0; i < n; ++i)
-        if (mine(cl[i])) groups += (int64_t)n_kv_heads * sets(cl[i], tiles) * kv4_splits(cl[i].len, s);
+        if (mine(cl[i])) {
+          const int nsplit = kv4_splits(cl[i].len, s);
+          const int64_t g = (int64_t)n_kv_heads * sets(cl[i], tiles) * nsplit;
+          groups += g;
+          if (nsplit > 1) cut_groups += g;
+        }
+      if (cut_groups > kKv4CutRounds * room) break;  // (more still with shorter ones)
       const double walk = std::min<double>(s, longest) / 32 * cost.step;
       const int64_t rounds = groups / room, left = groups % room;  // whole rounds, and what the last has
       const double t = cost.start + rounds * (walk * cost.resident + cost.begin) +
@@ -193,6 +203,20 @@ inline Kv4PlanNeeds kv4_plan(const Kv4Client* cl, int n, int dtype, int head_dim
     flush();
   }
   return need;
+}
+
+// At least what kv4_plan needs for any pass of up to `clients` clients of up to `rows` rows and `len` tokens each.
+inline Kv4PlanNeeds kv4_plan_most(int clients, int rows, int64_t len, int dtype, int head_dim, int n_q_heads, int n_kv_heads, int n_cu) {
+  const int all = attn_query_tiles(n_q_heads / n_kv_heads, rows);
+  const int64_t splits = std::min<int64_t>(kKv4MaxSplits, kv4_splits(len, 32 * kKv4FewWaves));
+  auto tiles = [&](int wg_tiles) {
+    const int64_t sets = (all + wg_tiles - 1) / wg_tiles;
+    const int64_t cut = std::min<int64_t>((int64_t)clients * n_kv_heads * sets * splits, (int64_t)kKv4CutRounds * kv4_cost(wg_tiles, dtype, head_dim).resident * n_cu);
+    return splits > 1 ? (size_t)(cut * wg_tiles) : 0;
+  };
+  const double one = kv4_cost(1, dtype, head_dim).step, two = kv4_cost(2, dtype, head_dim).step, eight = kv4_cost(kKv4WideTiles, dtype, head_dim).step;
+  const bool wide = eight < std::min(one * all, two * ((all + 1) / 2));  // (some client may have many tiles)
+  return Kv4PlanNeeds{std::max(tiles(1), tiles(2)) + (wide ? tiles(kKv4WideTiles) : 0), (size_t)clients * n_kv_heads * all};
 }
 
 // block-table entries that changed, by value: no copy that the host would have to keep
