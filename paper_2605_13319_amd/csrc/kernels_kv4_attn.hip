@@ -5,8 +5,8 @@
 //
 // Keys and values become bf16 on their way to the matrix cores, exactly (two bits and a power of two).  The queries of a bf16
 // model are operands as they are, those of an fp32 model are cut into three bf16 numbers (24 bits, so exactly): scores are as
-// good as fp32 ones.  Weights are cut into two bf16 numbers (16 bits), as everywhere in this library: only the cache itself
-// is coarse.  Maxima and sums are fp32.
+// good as fp32 ones.  So are an fp32 model's weights, cut into three bf16 numbers too.  Those of a bf16 model are cut into two, 16
+// bits where its results have 8, as in the attention over its bf16 cache: only the cache itself is coarse.  Maxima and sums are fp32.
 //
 // (The products that take 4-bit codes with their powers as operands need no conversion of the keys, but cut the addends of a
 // sum about 2^15 below the largest: with the queries in two e4m3 pieces scores were off by 2^-20 to 2^-16 of sum |q k|, where
@@ -178,16 +178,16 @@ __device__ __forceinline__ float max3(float a, float b, float c) {  // (through 
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
   return d;
 }
-// p = hi + lo, each four pairs of bf16 numbers; p - hi is exact.  (Dot products with (-1, 0) and (0, -1) give it in half the
-// instructions, but wait for the matrix cores: two beside a 32 x 32 x 16 product take 53 cycles, where four of any others hide in its 32.)
-__device__ __forceinline__ unsigned lower_pair(float p0, float p1, unsigned hi) {
-  return pack2_bf16(p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xffff0000u));
-}
-__device__ __forceinline__ void split_weights(const float (&p)[8], unsigned (&hi)[4], unsigned (&lo)[4]) {
+// Two weights as NW pairs of bf16 numbers, each what the ones before leave (exactly).  (Dot products with (-1, 0) and (0, -1) give what is
+// left in half the instructions, but wait for the matrix cores: two beside a 32 x 32 x 16 product take 53 cycles, where four of any others
+// hide in its 32.)
+template <int NW>
+__device__ __forceinline__ void split_weights(float p0, float p1, unsigned (&out)[NW]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    hi[i] = pack2_bf16(p[2 * i], p[2 * i + 1]);
-    lo[i] = lower_pair(p[2 * i], p[2 * i + 1], hi[i]);
+  for (int m = 0; m < NW; ++m) {
+    out[m] = pack2_bf16(p0, p1);
+    p0 -= __uint_as_float(out[m] << 16);
+    p1 -= __uint_as_float(out[m] & 0xffff0000u);
   }
 }
 
@@ -205,7 +205,9 @@ __device__ __forceinline__ Kv4Item find_item(const Kv4Clients& cl, int item, int
 
 // A wave walks tokens 32 at a time (a step): scores of the step, weights, products with the values.
 template <typename T>
-constexpr int pieces() { return sizeof(T) == 4 ? 3 : 1; }
+constexpr int pieces() { return sizeof(T) == 4 ? 3 : 1; }  // of a query
+template <typename T>
+constexpr int weight_pieces() { return sizeof(T) == 4 ? 3 : 2; }
 
 // What a workgroup knows of its client, and how rows leave it.
 template <int HD, typename T>
@@ -287,15 +289,17 @@ struct Running {
 #pragma unroll
     for (int j = 0; j < HT; ++j) acc[j] *= alpha;
   }
-  __device__ __forceinline__ void weights(const float (&sc)[8], float c1, bf16x8& hi, bf16x8& lo) {
+  template <int NW>
+  __device__ __forceinline__ void weights(const float (&sc)[8], float c1, bf16x8 (&out)[NW]) {
     float p[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c1, neg_m));
     l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-    unsigned h[4], r[4];
-    split_weights(p, h, r);
-    hi = __builtin_bit_cast(bf16x8, k4u32x4{h[0], h[1], h[2], h[3]});
-    lo = __builtin_bit_cast(bf16x8, k4u32x4{r[0], r[1], r[2], r[3]});
+    unsigned w[4][NW];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) split_weights(p[2 * i], p[2 * i + 1], w[i]);
+#pragma unroll
+    for (int m = 0; m < NW; ++m) out[m] = __builtin_bit_cast(bf16x8, k4u32x4{w[0][m], w[1][m], w[2][m], w[3][m]});
   }
 };
 __device__ __forceinline__ float top_of(const float (&sc)[8]) {
@@ -344,7 +348,7 @@ constexpr size_t few_lds_bytes() {
 template <int HD, typename T, int TILES, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, TILES == 1 ? 4 : 2) void kv4_attend_kernel(Kv4AttendCall a, Kv4Clients clients) {
   constexpr int NP = pieces<T>(), NS = HD / 32, HT = HD / 16, ROW = HD + kKv4PartPad, STEP = WAVES * 32;
-  constexpr int SETS = sizeof(T) == 2 && HD == 64 ? 2 : 1;
+  constexpr int NW = weight_pieces<T>(), SETS = sizeof(T) == 2 && HD == 64 ? 2 : 1;
   constexpr bool Q_LDS = queries_in_lds<HD, T, TILES>();
   typedef typename std::conditional<HD == 128, k4u32x4, k4u32x2>::type Codes;
   extern __shared__ float lds[];
@@ -459,7 +463,7 @@ __global__ __launch_bounds__(WAVES * 64, TILES == 1 ? 4 : 2) void kv4_attend_ker
     }
     request_keys(i + SETS, SET);
     settle(score);
-    bf16x8 ph[TILES], pl[TILES];
+    bf16x8 p[TILES][NW];
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
       const f32x4 s0 = score[t][0], s1 = score[t][1];
@@ -467,7 +471,7 @@ __global__ __launch_bounds__(WAVES * 64, TILES == 1 ? 4 : 2) void kv4_attend_ker
       if (masked) hide(sc, tok0 + g * 4, lim[t]);
       const float top = top_of(sc);
       if (__ballot(top > run[t].moves) != 0) run[t].move_to(top, c1);
-      run[t].weights(sc, c1, ph[t], pl[t]);
+      run[t].weights(sc, c1, p[t]);
     }
     if (masked) {
 #pragma unroll
@@ -483,10 +487,11 @@ __global__ __launch_bounds__(WAVES * 64, TILES == 1 ? 4 : 2) void kv4_attend_ker
       for (int t = 0; t < TILES; ++t) {
         f32x4& x = run[t].acc[2 * b];
         f32x4& y = run[t].acc[2 * b + 1];
-        x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, ph[t], x, 0, 0, 0);
-        y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, ph[t], y, 0, 0, 0);
-        x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, pl[t], x, 0, 0, 0);
-        y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, pl[t], y, 0, 0, 0);
+#pragma unroll
+        for (int m = 0; m < NW; ++m) {
+          x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, p[t][m], x, 0, 0, 0);
+          y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, p[t][m], y, 0, 0, 0);
+        }
       }
     }
     request_values(i + SETS, SET);
@@ -623,7 +628,8 @@ constexpr bool alone() { return HD * pieces<T>() > 192; }
 
 template <int HD, typename T>
 __global__ __launch_bounds__(kKv4WideWaves * 64, (alone<HD, T>() ? 1 : 2)) void kv4_attend_many_kernel(Kv4AttendCall a, Kv4Clients clients) {
-  constexpr int NP = pieces<T>(), KS = HD / 16, HT = HD / 32, ROW = HD + kKv4PartPad, WAVES = kKv4WideWaves, WG_ROWS = WAVES * 32;
+  constexpr int NP = pieces<T>(), NW = weight_pieces<T>(), KS = HD / 16, HT = HD / 32, ROW = HD + kKv4PartPad;
+  constexpr int WAVES = kKv4WideWaves, WG_ROWS = WAVES * 32;
   constexpr bool ALONE = alone<HD, T>();
   typedef typename std::conditional<HD == 128, k4u32x4, k4u32x2>::type Codes;
   extern __shared__ float lds[];
@@ -713,13 +719,14 @@ __global__ __launch_bounds__(kKv4WideWaves * 64, (alone<HD, T>() ? 1 : 2)) void 
     value_to[((ch + 1) % HT * 2 * 64 + (ch + 1) / HT * 16) * 2] = odd;
   };
 
-  // A step's weights as two operands a block: upper and lower parts.  Two sets: the step's, and those of the step before, whose
-  // products are still to come.
-  unsigned up[2][8], low[2][8];
+  // A step's weights as NW operands a block.  Two sets: the step's, and those of the step before, whose products are still to come.
+  unsigned weight[2][8][NW];
 #pragma unroll
-  for (int x = 0; x < 8; ++x) up[1][x] = low[1][x] = 0u;
-  auto operand = [](const unsigned (&x)[8], int block) {
-    return __builtin_bit_cast(bf16x8, k4u32x4{x[4 * block], x[4 * block + 1], x[4 * block + 2], x[4 * block + 3]});
+  for (int x = 0; x < 8; ++x)
+#pragma unroll
+    for (int m = 0; m < NW; ++m) weight[1][x][m] = 0u;
+  auto operand = [](const unsigned (&x)[8][NW], int block, int m) {
+    return __builtin_bit_cast(bf16x8, k4u32x4{x[4 * block][m], x[4 * block + 1][m], x[4 * block + 2][m], x[4 * block + 3][m]});
   };
 
   k4u32x4 key[KS];
@@ -770,37 +777,36 @@ __global__ __launch_bounds__(kKv4WideWaves * 64, (alone<HD, T>() ? 1 : 2)) void 
         if (tok0 + (j >> 2) * 8 + half * 4 + (j & 3) >= lim) sc[j] = -INFINITY;
     }
     // The step before's products, and between them two weights of this step at a time; a step's last keys are read for the next.
-    constexpr int EACH = HT / 2;  // products for each pair of weights
+    constexpr int PRODUCTS = 2 * NW * HT;  // an eighth of them for each pair of weights
     float total = 0.f, p[2];
     auto weigh = [&](int x, float neg) {
       p[0] = __builtin_amdgcn_exp2f(fmaf(sc[2 * x], c1, neg));
       p[1] = __builtin_amdgcn_exp2f(fmaf(sc[2 * x + 1], c1, neg));
     };
     auto keep = [&](int x) {
-      up[NOW][x] = pack2_bf16(p[0], p[1]);
-      low[NOW][x] = lower_pair(p[0], p[1], up[NOW][x]);
+      split_weights(p[0], p[1], weight[NOW][x]);
       total += p[0] + p[1];
     };
     const k4u32x4* keys = key_lds + ((n + 1) & 3) * KS * 64 + lane;
     unsigned long long move = 0;
 #pragma unroll
     for (int x = 0; x < 8; ++x) {
+      const int first = x * PRODUCTS / 8, behind = (x + 1) * PRODUCTS / 8;
 #pragma unroll
-      for (int k = 0; k < EACH; ++k) {
-        const int y = x * EACH + k, block = y / (2 * HT), lower = y / HT % 2, j = y % HT;
+      for (int y = first; y < behind; ++y) {
+        const int block = y / (NW * HT), m = y / HT % NW, j = y % HT;
         __builtin_amdgcn_sched_barrier(0);
-        acc[0][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, value[block][j]), operand(lower ? low[BEFORE] : up[BEFORE], block),
-                                                           acc[0][j], 0, 0, 0);
+        acc[0][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, value[block][j]), operand(weight[BEFORE], block, m), acc[0][j], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
-        if (k == 0) {
+        if (y == first) {
           if (x == 0) weigh(0, neg_m);
           keep(x);
-          asm volatile("" ::"v"(low[NOW][x]));  // (here, not behind the branch below)
+          asm volatile("" ::"v"(weight[NOW][x][NW - 1]));  // (here, not behind the branch below)
           if (x < HT) value[1][x] = from[(x * 2 + 1) * 64];
           if (x >= 8 - KS) key[x - (8 - KS)] = keys[(x - (8 - KS)) * 64];
           if (x == 7) move = __ballot(!(total <= 4096.f));  // (before the last product: the branch need not wait for it)
         }
-        if (k == EACH - 1 && x < 7) weigh(x + 1, neg_m);
+        if (y == behind - 1 && x < 7) weigh(x + 1, neg_m);
       }
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -860,8 +866,8 @@ __global__ __launch_bounds__(kKv4WideWaves * 64, (alone<HD, T>() ? 1 : 2)) void 
 #pragma unroll
       for (int j = 0; j < HT; ++j) {
         const bf16x8 value = __builtin_bit_cast(bf16x8, from[(j * 2 + block) * 64]);
-        acc[0][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value, operand(up[1], block), acc[0][j], 0, 0, 0);
-        acc[0][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value, operand(low[1], block), acc[0][j], 0, 0, 0);
+#pragma unroll
+        for (int m = 0; m < NW; ++m) acc[0][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value, operand(weight[1], block, m), acc[0][j], 0, 0, 0);
       }
     settle<ALONE>(acc);
   }

@@ -96,9 +96,9 @@ struct Kv4Cost {
 };
 constexpr Kv4Cost kv4_cost(int tiles, int dtype, int head_dim) {
   const bool f32 = dtype == PIPESD_F32, wide = head_dim == 128;
-  if (tiles == 1) return Kv4Cost{2, 2.5, f32 ? (wide ? 0.15 : 0.105) : (wide ? 0.14 : 0.08), 1.15, 3, 2};
+  if (tiles == 1) return Kv4Cost{2, 2.5, f32 ? (wide ? 0.157 : 0.109) : (wide ? 0.14 : 0.08), 1.15, 3, 2};
   if (tiles == 2) return Kv4Cost{1, 7, f32 ? 1e30 : (wide ? 0.195 : 0.125), 1, 4, 1};
-  return Kv4Cost{10, 5, f32 ? (wide ? 1. : 0.65) : (wide ? 0.6 : 0.39), f32 && wide ? 1. : 1.8, 5, f32 && wide ? 1 : 2};
+  return Kv4Cost{10, 5, f32 ? (wide ? 1.22 : 0.73) : (wide ? 0.6 : 0.39), f32 && wide ? 1. : 1.8, 5, f32 && wide ? 1 : 2};
 }
 
 // The launches of a pass: clients of few and of many tiles apart, at most kKv4ClientsPerLaunch in one.  All splits of a kind are as
