@@ -423,6 +423,9 @@ int pipesd_kv4_append(pipesd_kv4 *kv, int32_t layer, const void *k, int64_t k_st
  *           each client of the pass, at this layer, mass[t] = decay * mass[t] + (sum of token t's weights over the client's rows
  *           and the query heads of the cache head), 0 <= decay <= 1; the pass's own tokens, and all with decay 0, start at 0
  *           whatever the buffer held.  A client without new rows only has its weights decayed.
+ *           The buffer is the caller's: a pass without mass leaves it alone, and so do pipesd_kv4_truncate and, beyond the kept
+ *           tokens, pipesd_kv4_evict.  What it holds for tokens that came in a pass without mass, an earlier token's weight where one
+ *           was forgotten or cut, counts in the next pass with decay > 0: clear it before, or weigh every pass behind a cut.
  * A row's result depends on its own client's tokens and queries alone.  Into how many pieces a context is cut, and so the
  * order of sums, goes by the lengths and numbers of rows of all clients of the pass; the same pass gives the same bits.
  * EINVAL: also a client longer than mass_stride, a decay outside [0, 1], or out over q where that is not allowed; ESTATE: no

@@ -601,7 +601,8 @@ class KV4Cache:
         """Attention of the pass's queries over a layer of the cache; returns `out` (a new tensor like q if None;
         may be q itself where no weights are asked for).  limits: int32 [rows], tokens that each row sees.  mass: float32
         [max_seqs][n_layers][n_kv_heads][tokens], the weight that cached tokens were given, accumulated (of a client of the pass
-        without new rows only decayed)."""
+        without new rows only decayed).  The pass's own tokens start at 0; of tokens that came in a pass without weights it
+        counts what `mass` holds, which is another token's weight where one was forgotten or cut: clear it before."""
         heads = self.shape.n_q_heads
         qp, qs = self._tensor(q, heads, "q")
         if out is None:
