@@ -419,6 +419,8 @@ int pipesd_kv4_append(pipesd_kv4 *kv, int32_t layer, const void *k, int64_t k_st
  * same address and stride); otherwise no row of out shares memory with one of q (columns of one wider matrix do not).
  *   limits  device int32 [rows]: how many of its client's tokens (from the first) a row sees, cut to 0 .. its length; NULL:
  *           all up to the row's own.  A row that sees nothing gets zeros.
+ *           (Weights, each up to 2^12 then, are multiplied with the values before they are divided by their sum: results from values
+ *           beyond 2^100, stored infinities among them, may overflow.)
  *   mass    device fp32 [max_seqs][n_layers][n_kv_heads][mass_stride], or NULL: what weight the cached tokens were given.  For
  *           each client of the pass, at this layer, mass[t] = decay * mass[t] + (sum of token t's weights over the client's rows
  *           and the query heads of the cache head), 0 <= decay <= 1; the pass's own tokens, and all with decay 0, start at 0

@@ -603,7 +603,7 @@ __global__ __launch_bounds__(WAVES * 64, TILES == 1 ? 4 : 2) void kv4_attend_ker
 
 // ---- many tiles: each of four waves has two of its own, 32 rows ----
 // Keys and values are converted once, a block by each wave, into operands in LDS that all read; a barrier for every 64 tokens.
-// Products of 32 x 32 x 16: 8 for a step's scores, 16 for its values, which are multiplied a step later: those products, which depend
+// Products of 32 x 32 x 16: 8 for a step's scores, 16 for its values (24 and 24 of an fp32 model), multiplied a step later: those, which depend
 // on nothing of the step, travel with the weights' instructions, the score products with half of the next round's conversion.  (The
 // matrix cores leave a wave 28 of a product's 32 cycles for other instructions, and one after another, products and instructions
 // would take both times.)  Chunks that the compiler keeps in order do it: left to itself it puts the products side by side.
@@ -1010,7 +1010,8 @@ hipError_t launch_kv4_attend(const Kv4AttendCall& c, const Kv4Launch& l, hipStre
 // tiles the four waves bring through LDS four at a time.  One writer per token, sums in a fixed order.  The scores are formed again: kept,
 // they would be 30 times the keys' bytes at 32 rows of 4 heads.  Bound by the way from block table to keys to products that each
 // short workgroup goes: 32 rows behind 12001 tokens of 8 heads of 64 8.0 us, 38 behind 65536 of 128 (64 tokens a wave in place of
-// 32: 10.9 and 39.9).
+// 32: 10.9 and 39.9).  For many rows by what stands behind every tile's products, their wait and the exponentials: 2048 rows behind 6144
+// tokens, 32 query heads on 8 of 128, 289 us beside the attention's 307, where the products alone are 96; in fp32 527 and 589.
 template <int HD, typename T>
 __global__ __launch_bounds__(256) void kv4_mass_kernel(Kv4AttendCall a, Kv4Clients cl, int first_piece) {
   constexpr int NP = pieces<T>(), NS = HD / 32, TT = 2;

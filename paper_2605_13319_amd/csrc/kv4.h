@@ -85,11 +85,12 @@ struct Kv4PlanNeeds {
 // What workgroups of one, two or eight tiles take, in us: a launch (with what joins eight tiles' splits), a workgroup to begin and end, 32 tokens
 // of it by compute unit with all `resident` workgroups that a compute unit holds, how much longer one takes alone, and a join.  Two
 // tiles share the conversion of keys and values, but leave registers for half the workgroups; eight share it through LDS, four times as
-// many rows to join.  Measured, 4 query heads on each of 8 cache heads of 128: 16 clients of 8 rows behind 4096 tokens 28.0 us with one
-// tile, 24.8 with two; 4 of 4 rows behind 20000 23.6 and 28; 32 rows behind 65536 63.5 with two, 68 with eight; 64 rows 115 and 98; 2048
-// rows behind 6144 349 and 265, of head dim 64 225 and 182.  Two in fp32 were never faster: 4 clients of 9 rows behind 4096 tokens
-// 32.9 us, 21.9 with one.  (40 cache heads, 4 clients of 17 rows behind 8192: 57.8; two tiles in four waves, two such workgroups to a
-// compute unit, 52.9, but 10 to 15 % longer wherever the rounds fit.)
+// many rows to join.  Measured on the same inputs again and again, 4 query heads on each of 8 cache heads of 128: 32 clients of 8 rows
+// behind 4096 tokens 37.7 us with one tile, 33.5 with two; 4 of 4 rows behind 20000 24.1 and 27.6; 32 rows behind 65536 65 with two, 67
+// to 69 with eight; 64 rows 113 and 105; 2048 rows behind 6144 382 and 301 to 307, of head dim 64 276 and 197.  In fp32 2048 rows behind
+// 2048 291 with one, 262 to 272 with eight; two were never faster, 4 clients of 9 rows behind 4096 tokens 32.9 and 21.9 with one (weights of
+// 16 bits then; 22.1 now).  (40 cache heads, 4 clients of 17 rows behind 8192, inputs changing: 57.8; two tiles in four waves, two such
+// workgroups to a compute unit, 52.9, but 10 to 15 % longer wherever the rounds fit.)
 struct Kv4Cost {
   double start, begin, step, alone, join;
   int resident;
