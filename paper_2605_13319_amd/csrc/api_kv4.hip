@@ -333,10 +333,13 @@ static bool kv4_rows_ok(const pipesd_config& c, const void* p, int64_t stride, i
 
 // Whether a row of a and a row of b share bytes: `rows` of `width` bytes each, strides of at least that.
 static bool kv4_rows_overlap(const void* a, int64_t a_stride, const void* b, int64_t b_stride, int64_t rows, int64_t width) {
-  const uintptr_t pa = (uintptr_t)a, pb = (uintptr_t)b;
-  const uintptr_t reach = (uintptr_t)((rows - 1) * (pa < pb ? a_stride : b_stride) + width);  // of the one that begins first
-  if ((pa < pb ? pb - pa : pa - pb) >= reach) return false;
-  int64_t at = (int64_t)(pb - pa);  // of b's row j, from a's row i
+  if ((uintptr_t)a > (uintptr_t)b) std::swap(a, b), std::swap(a_stride, b_stride);
+  int64_t at = (int64_t)((uintptr_t)b - (uintptr_t)a);  // of b's first row, from a's
+  if (at >= (rows - 1) * a_stride + width) return false;
+  if (a_stride == b_stride) {  // (columns of one matrix) b's rows lie between the same two rows of a each, or behind the last
+    const int64_t before = at / a_stride;
+    return at % a_stride < width || (before + 1 < rows && a_stride - at % a_stride < width);
+  }
   for (int64_t i = 0, j = 0; i < rows && j < rows;) {
     if (at >= width) ++i, at -= a_stride;
     else if (at <= -width) ++j, at += b_stride;

@@ -82,3 +82,24 @@ def test_overlaps_on_the_host():
            at(p + 2 * row, 512, 256), at(p + 3 * row, 512, 256), at(p + row - 16, 512, 256), at(p + 4 * row - 32, 512, 512)]
     assert set(good) == {nav.ESTATE}  # (no pool)
     assert set(bad) == {nav.EINVAL}
+
+
+def test_overlaps_of_all_strides_on_the_host():
+    """Against every row with every other."""
+    import random
+    lib, r = nav._lib, random.Random(3)
+    seen = {nav.EINVAL: 0, nav.ESTATE: 0}
+    for rows in (1, 2, 3, 7):
+        kv = nav.KV4Cache(shape_of(1, 1, 64, "f32"), 1, 8, on_device=False)
+        kv.extend([0], [rows])
+        for _ in range(1500):
+            p, width = 1 << 20, 64 * 4
+            qs = 64 + 4 * r.randrange(40)
+            os_ = r.choice([qs, 64 + 4 * r.randrange(40)])
+            o = p + 16 * r.randrange(-120, 121)
+            shared = any(p + i * qs * 4 < o + j * os_ * 4 + width and o + j * os_ * 4 < p + i * qs * 4 + width for i in range(rows) for j in range(rows))
+            for mass in (None, C.c_void_p(4096)):
+                want = nav.EINVAL if shared and not (mass is None and o == p and os_ == qs) else nav.ESTATE
+                assert lib.pipesd_kv4_attend(kv.handle, 0, p, qs, None, o, os_, mass, 64, 1.0, None) == want, (rows, qs, os_, o - p, mass)
+                seen[want] += 1
+    assert min(seen.values()) > 1000
