@@ -459,6 +459,125 @@ int pipesd_kv4_len(const pipesd_kv4 *kv, int32_t seq, int32_t *len);
 int pipesd_kv4_free_blocks(const pipesd_kv4 *kv, int32_t *n_free);
 int pipesd_kv4_seq_blocks(const pipesd_kv4 *kv, int32_t seq, int32_t *n_blocks);
 
+/* ---- A cache for trees of drafts ---------------------------------------------------------------
+ *
+ * A round may bring several continuations of the committed text that share their beginnings: a tree of drafts.  Its pass has a row
+ * for the pending token and one for every draft; a row's PARENT is the row whose token comes before its own, and a row sees the
+ * text before the pass, its ancestors and itself.  What is decided on a tree (pipesd_tree_accept) is a path from the first row on:
+ * pipesd_pages_compact keeps its rows and forgets the others.
+ *
+ * The cache is paged, in the config's dtype (PIPESD_F32 or PIPESD_BF16), and its operators work on a layer's keys, values and queries
+ * as a caller's own forward has them (keys already rotated, a row by the number of its ancestors).  Blocks may belong to several
+ * clients (pipesd_pages_fork): a client that writes into one gets its own first.
+ *
+ * A forward over new rows of some clients is a PASS, as on the 4-bit cache: pipesd_pages_extend makes room for the rows, then, layer
+ * by layer, pipesd_pages_append puts in that layer's keys and values and pipesd_pages_attend lets its queries read them.  Rows of a
+ * pass lie one client after the other, in the order of pipesd_pages_extend.  A pass ends when the next begins, or when one of its
+ * clients loses tokens or becomes another's copy.
+ *
+ * All device work of a handle has to be ordered by its caller: one stream, or events between streams.  Nothing in here waits for the
+ * device but creation, destruction and where stated; pointers to device memory need 16-byte alignment, strides are in elements and
+ * whole multiples of 16 bytes.
+ *
+ * Recorded into a graph, pipesd_pages_append, pipesd_pages_attend and pipesd_pages_read do at every replay what they did for the lengths,
+ * block tables and trees of the recording: replay while the clients hold the blocks that they held then, and, of a pass with
+ * trees, before another pass with trees begins.  On a stream that is being recorded pipesd_pages_extend returns ESTATE and changes
+ * nothing if it would have to write block tables, trees or tokens or grow scratch (it has not where rows of a chain that were taken back
+ * come again), and so do pipesd_pages_fork, pipesd_pages_copy and pipesd_pages_compact (unless no token changes its place). */
+typedef struct pipesd_pages pipesd_pages;
+enum { PIPESD_PAGES_MAX_PASS_SEQS = 256, PIPESD_PAGES_MAX_ROWS = 2048, PIPESD_TREE_MAX_ROWS = 256, PIPESD_TREE_MAX_VOCAB = 1 << 22 };
+
+/* Bytes of a block of block_tokens (16) tokens: all layers and heads, keys and values.  0 for what pipesd_pages_create refuses. */
+size_t pipesd_pages_block_bytes(const pipesd_config *cfg, int32_t block_tokens);
+
+/* Cache of up to max_seqs clients over a caller-allocated device pool of floor(pool_bytes / block bytes) blocks (borrowed until
+ * pipesd_pages_destroy).  Of the config it takes n_layers, n_q_heads, n_kv_heads (at most 256 query heads each), head_dim (64 or
+ * 128) and dtype.  Beside the pool it allocates the block tables and the scratch that any pass of up to 16 clients with up to 64 rows
+ * each takes at the lengths that the pool allows.  pool == NULL: bookkeeping only.
+ * EINVAL: an unsupported config, block_tokens != 16, max_seqs < 1, no room for one block, a pool that is not 256-byte aligned or of
+ * 2^31 tokens or table entries (max_seqs * blocks) and more; ENOMEM: an allocation failed. */
+int pipesd_pages_create(const pipesd_config *cfg, int32_t max_seqs, int32_t block_tokens, void *pool, size_t pool_bytes, pipesd_pages **out);
+int pipesd_pages_destroy(pipesd_pages *pg);
+
+/* Begin a pass: client seq_ids[i] (pairwise distinct, 1 <= n_seqs <= 256) gets n_new[i] >= 0 more tokens, at least one in all.
+ *   parents  host, one per row of the pass: which of its own client's rows of the pass (0: the first) comes before it, an earlier one, or
+ *            -1: the text does; at most PIPESD_TREE_MAX_ROWS rows a client.  NULL: rows follow each other.
+ * A pass in which no client gets more than PIPESD_PAGES_MAX_ROWS can attend; others only append.  Larger passes than
+ * pipesd_pages_create provided for grow the handle's scratch, which waits for the device; what it was before stays, for calls
+ * recorded with it, until pipesd_pages_destroy.
+ * ENOMEM: the pool has too few free blocks (one for a last block that other clients hold as well, too), or the scratch cannot grow;
+ * ESTATE: see above, of streams being recorded. */
+int pipesd_pages_extend(pipesd_pages *pg, int32_t n_seqs, const int32_t *seq_ids, const int32_t *n_new, const int32_t *parents, void *stream);
+
+/* Put the pass's keys and values of one layer into the cache: k, v device [rows][n_kv_heads * head_dim], rows k_stride and v_stride
+ * elements apart.  ESTATE: no pass, or no pool. */
+int pipesd_pages_append(pipesd_pages *pg, int32_t layer, const void *k, int64_t k_stride, const void *v, int64_t v_stride, void *stream);
+
+/* Attention of the pass's queries over one layer of the cache: q, out device [rows][n_q_heads * head_dim], softmax of
+ * q . k / sqrt(head_dim) over the tokens that a row sees, query head g reads head g / (n_q_heads / n_kv_heads) of the cache.  out may be q
+ * itself (the same address and stride); otherwise no row of out shares memory with one of q (columns of one wider matrix do not).
+ * What tokens hold that a row does not see, infinities and NaN among them, does not reach it.
+ * A row's result depends on what it sees alone.  Into how many pieces a context is cut, and so the order of sums, goes by the
+ * lengths and numbers of rows of all clients of the pass; the same pass gives the same bits.
+ * EINVAL: also out over q where that is not allowed; ESTATE: no pass that can attend, no pool. */
+int pipesd_pages_attend(pipesd_pages *pg, int32_t layer, const void *q, int64_t q_stride, void *out, int64_t out_stride, void *stream);
+
+/* Tokens first[i] .. first[i] + count[i] - 1 of client seq_ids[i], of layers layer0 .. layer0 + n_layers - 1, as rows: k_out, v_out device
+ * [n_layers][sum of count][n_kv_heads][head_dim].  ESTATE: a range beyond a client's length, no pool. */
+int pipesd_pages_read(const pipesd_pages *pg, int32_t n_seqs, const int32_t *seq_ids, const int32_t *first, const int32_t *count, int32_t layer0,
+                      int32_t n_layers, void *k_out, void *v_out, void *stream);
+
+/* Client into[i] becomes the first len[i] tokens of client seq_ids[i] (NULL: all of them) and loses what it held.  A client may be several
+ * times among seq_ids; into is pairwise distinct and shares no client with seq_ids.
+ *   fork  shares the blocks: no token is copied until one of the clients writes behind a text that ends inside a block;
+ *   copy  takes as many blocks of its own.
+ * ESTATE: a length beyond the client's, a stream being recorded; ENOMEM (copy): too few free blocks (what the targets hold alone
+ * counts).  If a launch fails (EHIP) the targets are empty. */
+int pipesd_pages_fork(pipesd_pages *pg, int32_t n_seqs, const int32_t *seq_ids, const int32_t *into, const int32_t *len, void *stream);
+int pipesd_pages_copy(pipesd_pages *pg, int32_t n_seqs, const int32_t *seq_ids, const int32_t *into, const int32_t *len, void *stream);
+
+/* Of what client seq_ids[i] (pairwise distinct) holds from token first[i] on, n_kept[i] tokens stay, in their order, side by side: those
+ * first[i] + kept[j], kept host, rising, one client's after the other's (NULL if there are none).  The others are forgotten, and
+ * the blocks behind given back.  In place; a block with other users that would be written is replaced by a free one (ENOMEM if there
+ * are too few).  ESTATE: first[i] or a kept token beyond the client's length, see above of streams being recorded. */
+int pipesd_pages_compact(pipesd_pages *pg, int32_t n_seqs, const int32_t *seq_ids, const int32_t *first, const int32_t *n_kept, const int32_t *kept,
+                         void *stream);
+
+/* Forget the tokens of clients from new_len[i] (0 .. its length, else ESTATE) on; blocks that nobody holds any more are free.  Host
+ * bookkeeping only. */
+int pipesd_pages_truncate(pipesd_pages *pg, int32_t n_seqs, const int32_t *seq_ids, const int32_t *new_len);
+int pipesd_pages_len(const pipesd_pages *pg, int32_t seq, int32_t *len);
+int pipesd_pages_free_blocks(const pipesd_pages *pg, int32_t *n_free);
+/* Blocks of a client, shared ones included. */
+int pipesd_pages_seq_blocks(const pipesd_pages *pg, int32_t seq, int32_t *n_blocks);
+
+/* The decision on trees of drafts, one for each of n_seqs clients.  Client i has rows[i] rows (1 .. PIPESD_TREE_MAX_ROWS); the clients'
+ * rows, and what belongs to them, lie one client after the other:
+ *   p         device fp32 [rows][p_stride], p_stride >= vocab: the target's distribution behind each row;
+ *   q         device fp32 [rows][q_stride]: the distribution that the drafts of a row's children were drawn from (rows without
+ *             children are not read), or NULL: token matching;
+ *   tokens    host: a row's draft token (a client's first row, the pending token, is not looked at);
+ *   parents   host: as for pipesd_pages_extend; -1 for a client's first row and for no other;
+ *   uniforms  host, in [0, 1): u_r tests row r, a client's first is that of the draw (NULL without q);
+ *   distinct  not 0: a row's children were drawn without putting back.
+ * Rule: from the first row on, a row's children are tried in the order of their rows.  With a = 0, b = 1, S = 1 before the first, child c
+ * with token x is accepted iff u_c < min(1, w / (b q(x))), w = max(0, p(x) - a q(x)) (0 / 0 refuses).  If it is refused, a grows by b, S
+ * (if distinct) falls by q(x), to no less than 2^-24, and b becomes T / S, T = sum of floor(2^40 max(0, p - a q)) / 2^40 over the vocabulary.
+ * The next token is drawn from max(0, p - a q) of the row whose children were all refused, or p of a row without children, by the
+ * integer inverse CDF of pipesd_nav_verify with u of the client's first row.  All are fp32 numbers; p - a q is rounded once, b q before
+ * the division, S and T / S are formed in fp64.  The accepted text has the target's distribution; a chain is decided as by pipesd_spec_accept.
+ * Without q a child is accepted iff its token is the row's argmax (lowest index of equals), which is the next token where the walk ends.
+ *   result    device int32 [n_seqs][result_stride], result_stride > any rows[i]: accepted drafts a, next token, the a accepted
+ *             rows, then -1; valid once the work enqueued on `stream` has completed;
+ *   workspace device, pipesd_tree_accept_workspace() bytes, 16-byte aligned, all zero before its first use: calls leave it as the next one
+ *             needs it.  Calls that may overlap need one each.
+ * Nothing is allocated, copied or waited for, so the call can be recorded into a graph.  For 256 rows or 16 clients at a time as many
+ * launches as the row with the most drafts behind it has (2 for token matching). */
+size_t pipesd_tree_accept_workspace(void);
+int pipesd_tree_accept(const float *p, int64_t p_stride, const float *q, int64_t q_stride, int32_t vocab, int32_t n_seqs, const int32_t *rows,
+                       const int32_t *tokens, const int32_t *parents, const float *uniforms, int32_t distinct, int32_t *result,
+                       int64_t result_stride, void *workspace, size_t workspace_bytes, void *stream);
+
 const char *pipesd_strerror(int status);
 /* Text of the HIP call that made this thread's most recent call return PIPESD_EHIP ("" if none). */
 const char *pipesd_last_hip_error(void);

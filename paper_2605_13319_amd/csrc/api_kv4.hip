@@ -4,6 +4,7 @@
 #include <vector>
 
 #include "kv4.h"
+#include "rows.h"
 #include "status.h"
 
 using namespace pipesd;
@@ -331,23 +332,6 @@ static bool kv4_rows_ok(const pipesd_config& c, const void* p, int64_t stride, i
   return p && ((uintptr_t)p & 15) == 0 && stride >= (int64_t)heads * c.head_dim && (stride * e) % 16 == 0;
 }
 
-// Whether a row of a and a row of b share bytes: `rows` of `width` bytes each, strides of at least that.
-static bool kv4_rows_overlap(const void* a, int64_t a_stride, const void* b, int64_t b_stride, int64_t rows, int64_t width) {
-  if ((uintptr_t)a > (uintptr_t)b) std::swap(a, b), std::swap(a_stride, b_stride);
-  int64_t at = (int64_t)((uintptr_t)b - (uintptr_t)a);  // of b's first row, from a's
-  if (at >= (rows - 1) * a_stride + width) return false;
-  if (a_stride == b_stride) {  // (columns of one matrix) b's rows lie between the same two rows of a each, or behind the last
-    const int64_t before = at / a_stride;
-    return at % a_stride < width || (before + 1 < rows && a_stride - at % a_stride < width);
-  }
-  for (int64_t i = 0, j = 0; i < rows && j < rows;) {
-    if (at >= width) ++i, at -= a_stride;
-    else if (at <= -width) ++j, at += b_stride;
-    else return true;
-  }
-  return false;
-}
-
 static void kv4_add_range(Kv4Ranges& r, int32_t table_off, int32_t first, int32_t count, int32_t row_off) {
   r.table_off[r.n] = table_off;
   r.first[r.n] = first;
@@ -383,7 +367,7 @@ extern "C" int pipesd_kv4_attend(pipesd_kv4* kv, int32_t layer, const void* q, i
   // The weights are formed from the queries again, when all results have been written.
   if (kv->pass_open && (mass || q != out || q_stride != out_stride)) {
     const int64_t e = kv->cfg.dtype == PIPESD_F32 ? 4 : 2, rows = kv->pass.back().row_off + kv->pass.back().n_rows;
-    if (kv4_rows_overlap(q, q_stride * e, out, out_stride * e, rows, (int64_t)kv->cfg.n_q_heads * kv->cfg.head_dim * e)) return PIPESD_EINVAL;
+    if (rows_overlap(q, q_stride * e, out, out_stride * e, rows, (int64_t)kv->cfg.n_q_heads * kv->cfg.head_dim * e)) return PIPESD_EINVAL;
   }
   if (!kv->pool || !kv->pass_open || !kv->attends) return PIPESD_ESTATE;
   if (mass) {

@@ -100,6 +100,24 @@ _SIGS = {
     "pipesd_kv4_len": (C.c_int, [C.c_void_p, C.c_int32, _i32p]),
     "pipesd_kv4_free_blocks": (C.c_int, [C.c_void_p, _i32p]),
     "pipesd_kv4_seq_blocks": (C.c_int, [C.c_void_p, C.c_int32, _i32p]),
+    "pipesd_pages_block_bytes": (C.c_size_t, [C.POINTER(Config), C.c_int32]),
+    "pipesd_pages_create": (C.c_int, [C.POINTER(Config), C.c_int32, C.c_int32, C.c_void_p, C.c_size_t, C.POINTER(C.c_void_p)]),
+    "pipesd_pages_destroy": (C.c_int, [C.c_void_p]),
+    "pipesd_pages_extend": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "pipesd_pages_append": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]),
+    "pipesd_pages_attend": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]),
+    "pipesd_pages_read": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
+                                    C.c_void_p]),
+    "pipesd_pages_fork": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "pipesd_pages_copy": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "pipesd_pages_compact": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "pipesd_pages_truncate": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]),
+    "pipesd_pages_len": (C.c_int, [C.c_void_p, C.c_int32, _i32p]),
+    "pipesd_pages_free_blocks": (C.c_int, [C.c_void_p, _i32p]),
+    "pipesd_pages_seq_blocks": (C.c_int, [C.c_void_p, C.c_int32, _i32p]),
+    "pipesd_tree_accept_workspace": (C.c_size_t, []),
+    "pipesd_tree_accept": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
+                                     C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]),
     "pipesd_strerror": (C.c_char_p, [C.c_int]),
     "pipesd_last_hip_error": (C.c_char_p, []),
 }
@@ -679,6 +697,198 @@ class KV4Cache:
         n = C.c_int32()
         _check(_lib.pipesd_kv4_seq_blocks(self.handle, seq, C.byref(n)), "pipesd_kv4_seq_blocks")
         return n.value
+
+
+class PageCache:
+    """Paged cache of keys and values in the shape's dtype over a torch-allocated device pool (or bookkeeping only), whose clients
+    may share blocks, and the operators that write and read it, attend over it with chains and trees of rows, share, copy and compact
+    it.  Tensors are of the shape's dtype and on the pool's device; rows of a pass lie one client after the other."""
+
+    def __init__(self, shape, max_seqs: int, n_blocks: int, block_tokens: int = 16, device: str = "cuda:0",
+                 on_device: bool = True):
+        self.shape, self.max_seqs = shape, max_seqs
+        self.handle = C.c_void_p()
+        cfg = config_of(shape)
+        bb = _lib.pipesd_pages_block_bytes(C.byref(cfg), block_tokens)
+        if bb == 0:
+            raise PipesdError(EINVAL, "pipesd_pages_block_bytes")
+        self.block_bytes = bb
+        self.dtype = torch.float32 if shape.dtype == 0 else torch.bfloat16
+        self.pool = self.device = self._device_index = None
+        pool_ptr = None
+        if on_device:
+            torch.cuda.set_device(device)
+            self.pool = torch.empty(n_blocks * bb, dtype=torch.uint8, device=device)
+            self.device = self.pool.device
+            self._device_index = self.device.index
+            pool_ptr = self.pool.data_ptr()
+        _check(_lib.pipesd_pages_create(C.byref(cfg), max_seqs, block_tokens, pool_ptr, n_blocks * bb, C.byref(self.handle)),
+               "pipesd_pages_create")
+        self._rows = 0
+
+    _stream = KV4Cache._stream
+    _tensor = KV4Cache._tensor
+
+    def _call(self, call, name: str, *args) -> None:
+        """A call that works on the pool's device, on its current stream."""
+        if self.pool is None or torch.cuda.current_device() == self._device_index:
+            _check(call(self.handle, *args, self._stream()), name)
+        else:
+            with torch.cuda.device(self._device_index):
+                _check(call(self.handle, *args, self._stream()), name)
+
+    def close(self) -> None:
+        if self.handle:
+            _lib.pipesd_pages_destroy(self.handle)
+            self.handle = C.c_void_p()
+            self.pool = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def extend(self, seqs: Sequence[int], n_new: Sequence[int], parents: Optional[Sequence[int]] = None) -> None:
+        """Begin a pass: n_new[i] more tokens for client seqs[i].  parents: for every row of the pass the row of its own client's (0: the
+        first) that comes before it, -1: the text does; None: rows follow each other."""
+        (s, n, _ids, _), (c, m, _new, total) = _numbers(seqs), _numbers(n_new)
+        if n != m:
+            raise ValueError(f"{n} clients, {m} numbers of tokens")
+        up = None
+        if parents is not None:
+            up, rows, _up, _ = _numbers(parents)
+            if rows != total:
+                raise ValueError(f"{total} rows, {rows} parents")
+        self._call(_lib.pipesd_pages_extend, "pipesd_pages_extend", n, s, c, up)
+        self._rows = total
+
+    def append(self, layer: int, k, v) -> None:
+        """Put the pass's keys and values of a layer into the cache."""
+        heads = self.shape.n_kv_heads
+        kp, ks = self._tensor(k, heads, "k")
+        vp, vs = self._tensor(v, heads, "v")
+        self._call(_lib.pipesd_pages_append, "pipesd_pages_append", layer, kp, ks, vp, vs)
+
+    def attend(self, layer: int, q, out=None):
+        """Attention of the pass's queries over a layer of the cache; returns `out` (a new tensor like q if None; may be q itself)."""
+        heads = self.shape.n_q_heads
+        qp, qs = self._tensor(q, heads, "q")
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        op, os_ = self._tensor(out, heads, "out")
+        self._call(_lib.pipesd_pages_attend, "pipesd_pages_attend", layer, qp, qs, op, os_)
+        return out
+
+    def read(self, seqs: Sequence[int], first: Sequence[int], count: Sequence[int], layer0: int = 0, n_layers: Optional[int] = None):
+        """(keys, values) [n_layers][sum of count][n_kv_heads][head_dim] of ranges of the clients' tokens."""
+        s = self.shape
+        n_layers = s.n_layers - layer0 if n_layers is None else n_layers
+        (ids, n, _ids, _), (f, nf, _first, _), (c, nc, _count, rows) = _numbers(seqs), _numbers(first), _numbers(count)
+        if n != nf or n != nc:
+            raise ValueError(f"{n} clients, {nf} and {nc} ends of ranges")
+        size = (2, max(n_layers, 0), max(rows, 0), s.n_kv_heads, s.head_dim)
+        k, v = torch.empty(size, dtype=self.dtype, device=self.device).unbind(0)
+        # (a tensor of no elements has no address)
+        self._call(_lib.pipesd_pages_read, "pipesd_pages_read", n, ids, f, c, layer0, n_layers, k.data_ptr() or self.pool.data_ptr(),
+                                      v.data_ptr() or self.pool.data_ptr())
+        return k, v
+
+    def _become(self, call, name: str, seqs, into, lengths) -> None:
+        (ids, n, _ids, _), (to, m, _into, _) = _numbers(seqs), _numbers(into)
+        lp, nl, _len, _ = (None, n, None, 0) if lengths is None else _numbers(lengths)
+        if n != m or n != nl:
+            raise ValueError(f"{n} clients into {m}, {nl} lengths")
+        self._call(call, name, n, ids, to, lp)
+
+    def fork(self, seqs: Sequence[int], into: Sequence[int], lengths: Optional[Sequence[int]] = None) -> None:
+        """Client into[i] becomes the first lengths[i] tokens (None: all) of client seqs[i], in the same blocks; who writes into a shared
+        one gets its own first."""
+        self._become(_lib.pipesd_pages_fork, "pipesd_pages_fork", seqs, into, lengths)
+
+    def copy(self, seqs: Sequence[int], into: Sequence[int], lengths: Optional[Sequence[int]] = None) -> None:
+        """The same in blocks of its own."""
+        self._become(_lib.pipesd_pages_copy, "pipesd_pages_copy", seqs, into, lengths)
+
+    def compact(self, seqs: Sequence[int], first: Sequence[int], kept: Sequence[Sequence[int]]) -> None:
+        """Of what client seqs[i] holds from token first[i] on, the tokens first[i] + kept[i][j] stay (rising), side by side."""
+        (ids, n, _ids, _), (f, m, _first, _) = _numbers(seqs), _numbers(first)
+        if n != m or n != len(kept):
+            raise ValueError(f"{n} clients, {m} beginnings, {len(kept)} lists of tokens")
+        (c, _nc, _count, _), (k, _nk, _kept, _) = _numbers([len(x) for x in kept]), _numbers([int(t) for x in kept for t in x])
+        self._call(_lib.pipesd_pages_compact, "pipesd_pages_compact", n, ids, f, c, k)
+
+    def truncate(self, seqs: Sequence[int], lengths: Sequence[int]) -> None:
+        """Forget the clients' tokens from lengths[i] on."""
+        (s, n, _ids, _), (c, m, _new, _) = _numbers(seqs), _numbers(lengths)
+        if n != m:
+            raise ValueError(f"{n} clients, {m} lengths")
+        _check(_lib.pipesd_pages_truncate(self.handle, n, s, c), "pipesd_pages_truncate")
+
+    def length(self, seq: int) -> int:
+        n = C.c_int32()
+        _check(_lib.pipesd_pages_len(self.handle, seq, C.byref(n)), "pipesd_pages_len")
+        return n.value
+
+    def free_blocks(self) -> int:
+        n = C.c_int32()
+        _check(_lib.pipesd_pages_free_blocks(self.handle, C.byref(n)), "pipesd_pages_free_blocks")
+        return n.value
+
+    def seq_blocks(self, seq: int) -> int:
+        n = C.c_int32()
+        _check(_lib.pipesd_pages_seq_blocks(self.handle, seq, C.byref(n)), "pipesd_pages_seq_blocks")
+        return n.value
+
+
+def tree_workspace(n_seqs: int, rows: int, device: str = "cuda:0"):
+    """What calls of tree_accept for up to n_seqs clients of up to `rows` rows in all need; one for calls that may overlap each."""
+    return torch.zeros(_lib.pipesd_tree_accept_workspace(), dtype=torch.uint8, device=device)
+
+
+def tree_accept(p, q, tokens: Sequence[int], parents: Sequence[int], uniforms, rows: Optional[Sequence[int]] = None, distinct: bool = False,
+                result=None, workspace=None):
+    """The decision on trees of drafts, one client's rows after the other's: p, q torch CUDA float32 [rows][V] (q None: token matching),
+    rows: the clients' numbers of them (None: one client).  Enqueues the work on the current stream of p's device and returns `result`,
+    int32 [clients][more than any rows]: accepted drafts a, next token, the a accepted rows, then -1 (a new tensor if None)."""
+    (t, n, _tokens, _), (up, m, _parents, _) = _numbers(tokens), _numbers(parents)
+    if rows is None:
+        rows = [n]
+    r, clients, counts, total = _numbers(rows)
+    if n != total or m != total or clients < 1:
+        raise ValueError(f"{clients} clients of {total} rows, {n} tokens, {m} parents")
+    for x, name in ((p, "p"), (q, "q")):
+        if x is None and name == "q":
+            continue
+        if x.dtype is not torch.float32 or not x.is_cuda or x.device != p.device or x.dim() != 2 or x.shape != p.shape or (x.stride(1) != 1 and x.shape[1] > 1):
+            raise ValueError(f"{name}: a float32 tensor [rows][vocabulary], tokens side by side, on a GPU")
+    if p.shape[0] != total:
+        raise ValueError(f"{p.shape[0]} distributions, {total} rows")
+    u = None
+    if q is not None:
+        if uniforms is None or len(uniforms) != total:
+            raise ValueError(f"{total} rows need as many uniforms")
+        u = _floats(uniforms)
+    width = max(counts) + 1
+    if result is None:
+        result = torch.empty((clients, width), dtype=torch.int32, device=p.device)
+    elif (result.dtype is not torch.int32 or result.device != p.device or result.dim() != 2 or result.shape[0] != clients or result.shape[1] < width
+          or not result.is_contiguous()):
+        raise ValueError(f"result: a contiguous int32 tensor [{clients}][{width} or more] on {p.device}")
+    if workspace is None:
+        workspace = tree_workspace(clients, total, p.device)
+    elif workspace.dtype is not torch.uint8 or workspace.device != p.device or not workspace.is_contiguous():
+        raise ValueError(f"workspace: what tree_workspace returns, on {p.device}")
+    if torch.cuda.current_device() != p.device.index:
+        with torch.cuda.device(p.device):
+            return tree_accept(p, q, tokens, parents, uniforms, rows, distinct, result, workspace)
+    vocab = p.shape[1]
+    stream = _raw_stream(p.device.index) if _raw_stream is not None else int(torch.cuda.current_stream(p.device).cuda_stream)
+    _check(_lib.pipesd_tree_accept(p.data_ptr(), max(p.stride(0), vocab), None if q is None else q.data_ptr(),
+                                   0 if q is None else max(q.stride(0), vocab), vocab, clients, r, t, up, u, 1 if distinct else 0,
+                                   result.data_ptr(), result.shape[1], workspace.data_ptr(), workspace.numel(), stream),
+           "pipesd_tree_accept")
+    return result
 
 
 def spec_accept(p, q, drafts: Sequence[int], uniforms) -> tuple:
