@@ -242,19 +242,25 @@ static bool pages_unsent(const PagesSeq& s, int32_t from) {
   return !std::equal(s.blocks.begin() + from, s.blocks.end(), s.sent.begin() + from);
 }
 
-// Sends what is new of the block tables, and the trees of a pass (parents of all rows, or nullptr), some per launch.  (A block that a
-// client gave back and got again is there already.)
-static int pages_send(pipesd_pages* pg, int32_t n, const int32_t* seq_ids, const int32_t* from, const std::vector<PagesClient>& trees,
+// Sends what is new of the block tables, the blocks to copy (pg->from, pg->to) and the trees of a pass (parents of all rows, or nullptr),
+// some per launch.  (A block that a client gave back and got again is there already.)
+static int pages_send(pipesd_pages* pg, int32_t n, const int32_t* seq_ids, const int32_t* from, bool own, const std::vector<PagesClient>& trees,
                       const int32_t* parents, hipStream_t st) {
   PagesBegin b;
-  b.n = b.trees = 0;
+  b.n = b.trees = b.own = 0;
   int32_t rows = 0;
   auto flush = [&]() -> int {
-    if (b.n == 0 && b.trees == 0) return PIPESD_OK;
-    HIP_TRY(launch_pages_begin(b, pg->table, pg->masks, st));
-    b.n = b.trees = rows = 0;
+    if (b.n == 0 && b.trees == 0 && b.own == 0) return PIPESD_OK;
+    HIP_TRY(launch_pages_begin(pg->cfg.dtype, pg->view(), pg->cfg.n_layers, b, pg->table, pg->masks, st));
+    b.n = b.trees = b.own = rows = 0;
     return PIPESD_OK;
   };
+  for (size_t i = 0; own && i < pg->from.size(); ++i) {
+    if (b.own == kPagesOwnPerLaunch)
+      if (int rc = flush()) return rc;
+    b.own_from[b.own] = pg->from[i];
+    b.own_to[b.own++] = pg->to[i];
+  }
   for (int32_t k = 0; k < n; ++k) {
     PagesSeq& s = pg->seqs[seq_ids[k]];
     const int32_t off = pg->table_off(seq_ids[k]), nb = (int32_t)s.blocks.size();
@@ -346,8 +352,8 @@ extern "C" int pipesd_pages_extend(pipesd_pages* pg, int32_t n_seqs, const int32
       plan.reserve(n_seqs);
       pg->from.clear();
       pg->to.clear();
-      pg->from.reserve((size_t)n_seqs * kBlockTokens);
-      pg->to.reserve((size_t)n_seqs * kBlockTokens);
+      pg->from.reserve(n_seqs);
+      pg->to.reserve(n_seqs);
       int32_t row = 0;
       for (int32_t i = 0; i < n_seqs; ++i) {
         PagesSeq& s = pg->seqs[seq_ids[i]];
@@ -383,10 +389,8 @@ extern "C" int pipesd_pages_extend(pipesd_pages* pg, int32_t n_seqs, const int32
       PagesSeq& s = pg->seqs[seq_ids[i]];
       if (own[i] >= 0) {
         s.blocks.back() = pg->take();
-        for (int32_t t = 0; t < s.len % kBlockTokens; ++t) {
-          pg->from.push_back(own[i] * kBlockTokens + t);
-          pg->to.push_back(s.blocks.back() * kBlockTokens + t);
-        }
+        pg->from.push_back(own[i]);
+        pg->to.push_back(s.blocks.back());
         --had[i];  // (blocks that stay as they were)
       }
       s.len += n_new[i];
@@ -397,8 +401,7 @@ extern "C" int pipesd_pages_extend(pipesd_pages* pg, int32_t n_seqs, const int32
       for (int32_t i = 0; i < n_seqs; ++i) unsent = unsent || pages_unsent(pg->seqs[seq_ids[i]], had[i]);
       if (unsent)
         if (int e = pages_not_recorded(st)) return e;
-      if (int e = pages_moves(pg, false, st)) return e;
-      return pages_send(pg, n_seqs, seq_ids, had.data(), plan, trees ? parents : nullptr, st);
+      return pages_send(pg, n_seqs, seq_ids, had.data(), true, plan, trees ? parents : nullptr, st);
     };
     if (pg->pool && (rc = launch())) {
       for (int32_t i = n_seqs - 1; i >= 0; --i) {  // (backwards: the free blocks' order too is as it was)
@@ -611,7 +614,7 @@ extern "C" int pipesd_pages_copy(pipesd_pages* pg, int32_t n_seqs, const int32_t
     }
     if (!pg->pool) return PIPESD_OK;
     int rc = pages_moves(pg, true, st);
-    if (!rc) rc = pages_send(pg, n_seqs, into, nullptr, {}, nullptr, st);
+    if (!rc) rc = pages_send(pg, n_seqs, into, nullptr, false, {}, nullptr, st);
     if (rc) {
       pages_clear_targets(pg, n_seqs, into);
       for (int32_t i = 0; i < n_seqs; ++i) std::fill(pg->seqs[into[i]].sent.begin(), pg->seqs[into[i]].sent.end(), -1);
@@ -705,7 +708,7 @@ extern "C" int pipesd_pages_compact(pipesd_pages* pg, int32_t n_seqs, const int3
         std::vector<int32_t> from(n_seqs);
         for (int32_t i = 0; i < n_seqs; ++i) from[i] = range(i).b0;
         if (int e = pages_moves(pg, false, st)) return e;
-        return replaced.empty() ? PIPESD_OK : pages_send(pg, n_seqs, seq_ids, from.data(), {}, nullptr, st);
+        return replaced.empty() ? PIPESD_OK : pages_send(pg, n_seqs, seq_ids, from.data(), false, {}, nullptr, st);
       };
       if (int rc = launch()) {  // (tokens behind `first` may have been moved, as by a call that has run)
         for (size_t j = replaced.size(); j-- > 0;) {

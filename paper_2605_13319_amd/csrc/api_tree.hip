@@ -32,6 +32,7 @@ extern "C" int pipesd_tree_accept(const float* p, int64_t p_stride, const float*
   c.q_stride = q ? q_stride : 0;
   c.V = vocab;
   c.distinct = distinct != 0;
+  c.chunks = std::min(kTreeChunks, (vocab + kTreeChunk - 1) / kTreeChunk);
   c.result_stride = result_stride;
   c.ws = tree_workspace(workspace);
   int64_t row0 = 0;  // of the launch's first client
@@ -43,15 +44,16 @@ extern "C" int pipesd_tree_accept(const float* p, int64_t p_stride, const float*
       const int32_t n = rows[i0 + c.n];
       c.row_off[c.n] = many;
       c.rows[c.n] = n;
-      std::fill_n(c.children + many, n, (uint8_t)0);
+      for (int32_t r = 0; r < n; ++r) c.row[many + r].children = 0;
       for (int32_t r = 0; r < n; ++r) {
         const int64_t at = row0 + many + r;
         const int32_t up = parents[at];
-        c.token[many + r] = tokens[at];
-        c.u[many + r] = q ? uniforms[at] : 0.f;
-        c.parent[many + r] = (int16_t)up;
-        c.nth[many + r] = up < 0 ? 0 : c.children[many + up]++;
-        if (up >= 0) c.stages = std::max(c.stages, (int32_t)c.children[many + up]);
+        TreeRow& row = c.row[many + r];
+        row.token = r > 0 ? tokens[at] : 0;
+        row.u = q ? uniforms[at] : 0.f;
+        row.parent = (int16_t)up;
+        row.nth = up < 0 ? 0 : c.row[many + up].children++;
+        if (up >= 0) c.stages = std::max(c.stages, (int32_t)c.row[many + up].children);
       }
       many += n;
       ++c.n;

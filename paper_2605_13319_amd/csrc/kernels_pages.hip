@@ -3,16 +3,53 @@
 
 namespace pipesd {
 
+// 16 bytes
+typedef __attribute__((ext_vector_type(4))) unsigned piece_t;
+struct BlockPieces {  // blocks in pieces
+  piece_t* pool;
+  int64_t layer, v;  // between layers; from keys to values
+  int block;
+  BlockPieces(int dtype, const KvView& view) {
+    const int elems = dtype == PIPESD_F32 ? 4 : 8;  // (a block of a head is a multiple)
+    pool = (piece_t*)view.pool;
+    layer = view.layer_stride / elems;
+    v = view.v_offset / elems;
+    block = view.block_elems / elems;
+  }
+  // part: 2 * layer, and 1 for values
+  __device__ __forceinline__ void copy(int part, int from_block, int to_block) const {
+    piece_t* base = pool + (part >> 1) * layer + (part & 1 ? v : 0);
+    const piece_t* from = base + (int64_t)from_block * block;
+    piece_t* to = base + (int64_t)to_block * block;
+    constexpr int N = 4;
+    int i = threadIdx.x;
+    for (; i + (N - 1) * 256 < block; i += N * 256) {
+      piece_t x[N];
+#pragma unroll
+      for (int j = 0; j < N; ++j) x[j] = from[i + j * 256];
+#pragma unroll
+      for (int j = 0; j < N; ++j) to[i + j * 256] = x[j];
+    }
+    for (; i < block; i += 256) to[i] = from[i];
+  }
+};
+
 // ------------------------------------------------------------------------------------------------
-// what a pass begins with: new entries of the block tables, and what every row of its trees sees
+// what a pass begins with: new entries of the block tables, what every row of its trees sees, and blocks copied for clients that write
+// into one that others hold as well
 // ------------------------------------------------------------------------------------------------
-// Workgroup: a tree, a thread a row, which walks up to the root; the first also writes the entries.
-__global__ __launch_bounds__(kPagesTreeRows) void pages_begin_kernel(PagesBegin b, int32_t* table, uint32_t* masks) {
+// The first workgroups have a tree each, a thread a row, which walks up to the root (the very first also writes the entries); the others the
+// keys or values of a block and layer.
+__global__ __launch_bounds__(kPagesTreeRows) void pages_begin_kernel(BlockPieces pool, PagesBegin b, int32_t* table, uint32_t* masks) {
   __shared__ int parent[kPagesTreeRows];
   __shared__ uint32_t bits[kPagesTreeRows][kPagesMaskWords];
   const int tid = threadIdx.x, tree = blockIdx.x;
   if (tree == 0 && tid < b.n) table[b.at[tid]] = b.v[tid];
-  if (tree >= b.trees) return;  // (whole workgroup)
+  if (tree >= b.trees) {  // (whole workgroup)
+    const int i = tree - b.trees;
+    if (b.own) pool.copy(i / b.own, b.own_from[i % b.own], b.own_to[i % b.own]);
+    return;
+  }
   int first = 0;  // of the tree's rows among the launch's
   for (int i = 0; i < tree; ++i) first += b.n_rows[i];
   const int n = b.n_rows[tree], lead = b.before[tree] & 31;
@@ -28,9 +65,9 @@ __global__ __launch_bounds__(kPagesTreeRows) void pages_begin_kernel(PagesBegin 
   const uint32_t* from = &bits[0][0];
   for (int i = tid; i < n * kPagesMaskWords; i += kPagesTreeRows) out[i] = from[i];
 }
-static_assert(kPagesEntriesPerLaunch <= kPagesTreeRows, "a thread an entry");
-hipError_t launch_pages_begin(const PagesBegin& b, int32_t* table, uint32_t* masks, hipStream_t st) {
-  pages_begin_kernel<<<std::max(1, b.trees), kPagesTreeRows, 0, st>>>(b, table, masks);
+static_assert(kPagesEntriesPerLaunch <= kPagesTreeRows && kPagesTreeRows == 256, "a thread an entry; threads that copy");
+hipError_t launch_pages_begin(int dtype, const KvView& v, int n_layers, const PagesBegin& b, int32_t* table, uint32_t* masks, hipStream_t st) {
+  pages_begin_kernel<<<std::max(1, b.trees + b.own * 2 * n_layers), kPagesTreeRows, 0, st>>>(BlockPieces(dtype, v), b, table, masks);
   return hipGetLastError();
 }
 
@@ -226,28 +263,12 @@ hipError_t launch_pages_move(int dtype, const KvView& v, int n_layers, const Pag
 // ------------------------------------------------------------------------------------------------
 // copy: workgroup (block, its keys or values of a layer)
 // ------------------------------------------------------------------------------------------------
-typedef __attribute__((ext_vector_type(4))) unsigned piece_t;
-__global__ __launch_bounds__(256) void pages_copy_kernel(piece_t* pool, int layer0, int64_t layer_stride, int64_t v_offset, int block_pieces,
-                                                         PagesMoves m) {
-  piece_t* part = pool + (layer0 + (int64_t)(blockIdx.y >> 1)) * layer_stride + (blockIdx.y & 1 ? v_offset : 0);
-  const piece_t* from = part + (int64_t)m.from[blockIdx.x] * block_pieces;
-  piece_t* to = part + (int64_t)m.to[blockIdx.x] * block_pieces;
-  constexpr int N = 4;
-  int i = threadIdx.x;
-  for (; i + (N - 1) * 256 < block_pieces; i += N * 256) {
-    piece_t x[N];
-#pragma unroll
-    for (int j = 0; j < N; ++j) x[j] = from[i + j * 256];
-#pragma unroll
-    for (int j = 0; j < N; ++j) to[i + j * 256] = x[j];
-  }
-  for (; i < block_pieces; i += 256) to[i] = from[i];
+__global__ __launch_bounds__(256) void pages_copy_kernel(BlockPieces pool, int part0, PagesMoves m) {
+  pool.copy(part0 + blockIdx.y, m.from[blockIdx.x], m.to[blockIdx.x]);
 }
 hipError_t launch_pages_copy(int dtype, const KvView& v, int n_layers, const PagesMoves& m, hipStream_t st) {
-  const int elems = dtype == PIPESD_F32 ? 4 : 8;  // of 16 bytes (a block of a head is a multiple)
-  for (int l0 = 0; l0 < n_layers; l0 += 32767) {
-    const int nl = std::min(32767, n_layers - l0);
-    pages_copy_kernel<<<dim3(m.n, nl * 2), 256, 0, st>>>((piece_t*)v.pool, l0, v.layer_stride / elems, v.v_offset / elems, v.block_elems / elems, m);
+  for (int p0 = 0; p0 < 2 * n_layers; p0 += 65534) {
+    pages_copy_kernel<<<dim3(m.n, std::min(65534, 2 * n_layers - p0)), 256, 0, st>>>(BlockPieces(dtype, v), p0, m);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

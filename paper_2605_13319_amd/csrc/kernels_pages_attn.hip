@@ -10,6 +10,7 @@
 // waves of a workgroup share its tiles of query rows, take every fourth 32 tokens of the span and join their states through LDS at the
 // end; a context that is cut into splits is joined by the last workgroup that arrives, or by a kernel of its own.
 #include "device_attend.h"
+#include "device_dma.h"
 #include "lds_limit.h"
 #include "pages.h"
 
@@ -131,34 +132,83 @@ __device__ __forceinline__ void join_splits(const PagesWork<HD, T>& wk, float* l
   }
 }
 
+// States of waves that shared rows, [wave][row] in LDS, joined: rows of the result, or a split's partial rows (written
+// through, unless a kernel of its own reads them).
+template <int HD, typename T, int ROWS, int SHARES, int NT>
+__device__ __forceinline__ void join_waves(const PagesWork<HD, T>& wk, int split, bool apart, const float* lds, int tid) {
+  constexpr int TPR = HD / 4, ROW = HD + kPagesPartPad;
+  const float(*states)[ROWS][ROW] = (const float(*)[ROWS][ROW])lds;
+  const int tasks = min(ROWS, wk.group_rows - wk.first_row) * TPR;  // a task: (row, 4 channels)
+#pragma unroll 1
+  for (int task = tid; task < tasks; task += NT) {
+    const int mr = task / TPR, e0 = (task % TPR) * 4;
+    f32x2 ml[SHARES];
+    float m = -INFINITY;
+#pragma unroll
+    for (int ww = 0; ww < SHARES; ++ww) {
+      ml[ww] = *(const f32x2*)&states[ww][mr][HD];
+      m = fmaxf(m, ml[ww].x);
+    }
+    const float m_ref = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ww = 0; ww < SHARES; ++ww) {
+      const float sw = __builtin_amdgcn_exp2f(ml[ww].x - m_ref);
+      l += ml[ww].y * sw;
+      o += *(const f32x4*)&states[ww][mr][e0] * sw;
+    }
+    if (wk.nsplit == 1) {
+      wk.finish(wk.first_row + mr, e0, o, l);
+    } else {
+      float* dst = wk.all + ((size_t)split * ROWS + mr) * ROW;
+      const f32x4 stats = f32x4{partial_maximum(m, l), l, 0.f, 0.f};
+      if (apart) {
+        *(f32x4*)(dst + e0) = o;
+        if (e0 == 0) *(f32x4*)(dst + HD) = stats;
+      } else {
+        Xwg<true>::st4f(dst + e0, o);
+        if (e0 == 0) Xwg<true>::st4f(dst + HD, stats);
+      }
+    }
+  }
+}
+
+typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
 template <typename T>
 __device__ __forceinline__ bool not_finite(T x) {
   if constexpr (sizeof(T) == 4) return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u;
   else return (x & 0x7f80u) == 0x7f80u;
 }
 
-// LDS: states [tile][wave][row], later what joins the splits; then the queries that registers do not hold; a word
+// ---- few rows: waves share one or two tiles of 16 ----
+// Eight waves take every eighth step of the span, 32 tokens of bf16 numbers or 16 of fp32 ones.  Of a step a lane (c, g) has the scores of
+// query row c with 8 or 4 tokens:
+//   bf16  tokens 8 g .. + 7: what a product over 32 tokens takes of their weights, and of a channel's values with one load.  The
+//         first four are row 4 g + .. of the first 16 x 16 product of keys, the others of the second: row r of product tt is token
+//         8 (r / 4) + 4 tt + r % 4.
+//   fp32  tokens 4 g .. + 3; a load of 4 channels of a key, or 4 tokens of a value, serves 4 products (k = 4).
+// LDS: states [wave][row], later what joins the splits; then the queries that registers do not hold; a word
 template <int HD, int TILES>
-constexpr size_t state_floats() { return (size_t)TILES * kPagesWaves * 16 * (HD + kPagesPartPad); }
+constexpr size_t state_floats() { return (size_t)TILES * kPagesFewWaves * 16 * (HD + kPagesPartPad); }
 template <int HD, typename T, int TILES>
 constexpr bool queries_in_lds() { return TILES * HD * (int)sizeof(T) > 512; }  // (more than 32 registers)
 template <int HD, typename T, int TILES>
 constexpr size_t attend_lds_bytes() {
   return state_floats<HD, TILES>() * sizeof(float) + (queries_in_lds<HD, T, TILES>() ? (size_t)TILES * HD * sizeof(T) * 16 : 0) + 16;
 }
-
-// A wave walks tokens 32 at a time (a step): scores, weights, products with the values.  Of a step a lane (c, g) has the scores of
-// query row c with 8 tokens:
-//   bf16  tokens 8 g .. + 7: what a product over 32 tokens takes of their weights, and of a channel's values with one load.  The
-//         first four are row 4 g + .. of the first 16 x 16 product of keys, the others of the second: row r of product tt is token
-//         8 (r / 4) + 4 tt + r % 4.
-//   fp32  tokens 4 g .. + 3 of both blocks; a load of 4 channels of a key, or 4 tokens of a value, serves 4 products (k = 4).
+// sets of keys and values that a wave has on their way
 template <int HD, typename T, int TILES>
-__global__ __launch_bounds__(kPagesWaves * 64, 2) void pages_attend_kernel(PagesAttend a, PagesClients clients) {
+constexpr int few_sets() { return sizeof(T) == 2 && TILES * HD > 128 ? 1 : 2; }
+
+template <int HD, typename T, int TILES>
+__global__ __launch_bounds__(kPagesFewWaves * 64, 2) void pages_attend_kernel(PagesAttend a, PagesClients clients) {
   constexpr bool F32 = sizeof(T) == 4;
-  constexpr int HT = HD / 16, ROW = HD + kPagesPartPad, WAVES = kPagesWaves, STEP = kPagesStep, NT = WAVES * 64;
+  constexpr int HT = HD / 16, ROW = HD + kPagesPartPad, WAVES = kPagesFewWaves, NT = WAVES * 64, SETS = few_sets<HD, T, TILES>();
+  constexpr int NB = F32 ? 1 : 2, TOKENS = NB * kBlockTokens, STEP = WAVES * TOKENS;  // blocks and tokens of a wave's step; of the workgroup's
+  constexpr int NX = 4 * NB;                   // scores of a lane
   constexpr int NK = F32 ? HD / 16 : HD / 32;  // 16-byte pieces of a key that a lane has
-  constexpr int NV = F32 ? 2 * HT : HT;        // and of values
+  constexpr int NV = HT;                       // and of values
   constexpr bool Q_LDS = queries_in_lds<HD, T, TILES>();
   extern __shared__ float lds[];
   int* word = (int*)((char*)lds + attend_lds_bytes<HD, T, TILES>() - 16);
@@ -167,13 +217,13 @@ __global__ __launch_bounds__(kPagesWaves * 64, 2) void pages_attend_kernel(Pages
   const int c = lane & 15, g = lane >> 4;
   const PagesItem it = find_item(clients, blockIdx.y, lane);
   const PagesWork<HD, T> wk(a, clients, it, kvh, TILES);
-  const int len = wk.len, before = len - wk.n_rows, span0 = it.split * clients.span, first = span0 + w * 32;
+  const int len = wk.len, before = len - wk.n_rows, span0 = it.split * clients.span, first = span0 + w * TOKENS;
 
-  // 64 steps' blocks sit in the lanes: lane L has the two of step L
-  int step_blk[2];
+  // 64 steps' blocks sit in the lanes: lane L has those of step L
+  int step_blk[NB];
   auto load_blocks = [&](int it0) {
 #pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
+    for (int tt = 0; tt < NB; ++tt) {
       const int64_t tok = (int64_t)first + (int64_t)(it0 + lane) * STEP + tt * 16;
       step_blk[tt] = wk.table[tok < len ? (int)(tok / kBlockTokens) : 0];
     }
@@ -209,14 +259,17 @@ __global__ __launch_bounds__(kPagesWaves * 64, 2) void pages_attend_kernel(Pages
   }
   const int end = min(it.split + 1 < wk.nsplit ? span0 + clients.span : len, hi);
   const int nsteps = end > first ? (end - first + STEP - 1) / STEP : 0;
-  // which of the 32 tokens from tok0 on a row sees
+  // which of a step's tokens a row sees
   auto seen = [&](int t, int tok0) -> uint32_t {
-    if (a.masks != nullptr) return a.masks[(size_t)row_of[t] * kPagesMaskWords + min((tok0 - (before & ~31)) >> 5, kPagesMaskWords - 1)];
+    if (a.masks != nullptr) {
+      const int at = tok0 - (before & ~31);
+      return a.masks[(size_t)row_of[t] * kPagesMaskWords + min(at >> 5, kPagesMaskWords - 1)] >> (at & 31);
+    }
     const int n = before + 1 + row_of[t] - wk.row_off - tok0;
     return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
   };
   // (the first that are asked for travel with the keys)
-  const int first_masked = first > lo - 32 ? 0 : (lo - 32 - first) / STEP + 1;
+  const int first_masked = first > lo - TOKENS ? 0 : (lo - TOKENS - first) / STEP + 1;
   uint32_t next_seen[TILES];
 #pragma unroll
   for (int t = 0; t < TILES; ++t) next_seen[t] = first_masked < nsteps ? seen(t, first + first_masked * STEP) : 0u;
@@ -226,73 +279,86 @@ __global__ __launch_bounds__(kPagesWaves * 64, 2) void pages_attend_kernel(Pages
   for (int t = 0; t < TILES; ++t) run[t].clear();
   const float c1 = attend_scale<HD>();
 
-  // Keys and values of a step travel from where those of the step before have been used until they are.
-  k4u32x4 k[2][NK], v[NV];
+  // Keys and values of a step travel from where those of the step before (or of the one before that, with registers for two) have been
+  // used until they are.
+  k4u32x4 k[SETS][NB][NK], v[SETS][NV];
   const char* head_base = (const char*)((const T*)a.view.pool + (int64_t)a.layer * a.view.layer_stride + (int64_t)kvh * kBlockTokens * HD);
   auto block_base = [&](int i, int tt) {
     return head_base + (int64_t)__builtin_amdgcn_readlane(step_blk[tt], i & 63) * a.view.block_elems * (int)sizeof(T);
   };
-  auto request_keys = [&](int i) {
+  auto request_keys = [&](int i, int set) {
     if (i >= nsteps) return;
     if (i > 0 && (i & 63) == 0) load_blocks(i);
-    const char *b0 = block_base(i, 0), *b1 = block_base(i, 1);
+    if constexpr (F32) {
+      const char* p = block_base(i, 0) + c * HD * 4 + g * 16;
 #pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
-      const char* p;
-      if constexpr (F32) p = (tt ? b1 : b0) + c * HD * 4 + g * 16;
-      else p = (c >> 3 ? b1 : b0) + (8 * ((c >> 2) & 1) + 4 * tt + (c & 3)) * HD * 2 + g * 16;
+      for (int s = 0; s < NK; ++s) k[set][0][s] = *(const k4u32x4*)(p + s * 64);
+    } else {
+      const char *b0 = block_base(i, 0), *b1 = block_base(i, 1);
 #pragma unroll
-      for (int s = 0; s < NK; ++s) k[tt][s] = *(const k4u32x4*)(p + s * 64);
+      for (int tt = 0; tt < NB; ++tt) {
+        const char* p = (c >> 3 ? b1 : b0) + (8 * ((c >> 2) & 1) + 4 * tt + (c & 3)) * HD * 2 + g * 16;
+#pragma unroll
+        for (int s = 0; s < NK; ++s) k[set][tt][s] = *(const k4u32x4*)(p + s * 64);
+      }
     }
   };
-  auto request_values = [&](int i) {
+  auto request_values = [&](int i, int set) {
     if (i >= nsteps) return;
-    const char *b0 = block_base(i, 0) + a.view.v_offset * (int)sizeof(T), *b1 = block_base(i, 1) + a.view.v_offset * (int)sizeof(T);
+    const int64_t off = a.view.v_offset * (int)sizeof(T);
     if constexpr (F32) {
+      const char* p = block_base(i, 0) + off + c * 64 + g * 16;
 #pragma unroll
-      for (int j = 0; j < NV; ++j) v[j] = *(const k4u32x4*)((j / HT ? b1 : b0) + ((j % HT) * 16 + c) * 64 + g * 16);
+      for (int j = 0; j < NV; ++j) v[set][j] = *(const k4u32x4*)(p + j * 1024);
     } else {
+      const char *b0 = block_base(i, 0) + off, *b1 = block_base(i, 1) + off;
       const char* p = (g >> 1 ? b1 : b0) + c * 32 + (g & 1) * 16;
 #pragma unroll
-      for (int j = 0; j < NV; ++j) v[j] = *(const k4u32x4*)(p + j * 512);
+      for (int j = 0; j < NV; ++j) v[set][j] = *(const k4u32x4*)(p + j * 512);
     }
   };
-  // the lane's token of score x, of the step's 32
-  auto token_of = [&](int x) { return F32 ? 16 * (x >> 2) + 4 * g + (x & 3) : 8 * g + x; };
+  auto token_of = [&](int x) { return NX * g + x; };  // the lane's token of score x, of the step's
 
   // Values of tokens that not every row sees.  Behind the client's last token there may be anything: 0 instead.  A value that is not
   // finite must reach the rows that see its token and no other, but a product would take it times 0 to all: it becomes 0 here, too, and
   // `apart_of` has a bit for its token.
-  auto drop_values = [&](int tok0, uint32_t& apart_of) {
+  auto drop_values = [&](k4u32x4 (&v)[NV], int tok0, uint32_t& apart_of) {
     uint32_t odd = 0;  // bit x: of the lane's token x
     if constexpr (F32) {
+      uint32_t largest = 0;
 #pragma unroll
       for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int x = (j / HT) * 4 + i;
-          const bool there = tok0 + token_of(x) < len, bad = (v[j][i] & 0x7f800000u) == 0x7f800000u;
-          if (there && bad) odd |= 1u << x;
-          if (!there || bad) v[j][i] = 0u;
+          if (tok0 + token_of(i) >= len) v[j][i] = 0u;
+          largest = max(largest, v[j][i] & 0x7fffffffu);
         }
-    } else {
-      const int n = min(8, max(0, len - tok0 - 8 * g));
-      uint32_t any = 0;  // (an exponent of ones carries into the sign)
+      if (__ballot(largest >= 0x7f800000u) != 0) {
 #pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        const uint32_t keep = n >= 2 * d + 2 ? ~0u : n == 2 * d + 1 ? 0xffffu : 0u;
+        for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-          v[j][d] &= keep;
-          any |= (v[j][d] & 0x7f807f80u) + 0x00800080u;
-        }
+          for (int i = 0; i < 4; ++i)
+            if ((v[j][i] & 0x7f800000u) == 0x7f800000u) odd |= 1u << i, v[j][i] = 0u;
       }
-      if (__ballot((any & 0x80008000u) != 0) != 0) {
+    } else {
+      if (tok0 + TOKENS > len) {
+        const int n = min(8, max(0, len - tok0 - 8 * g));
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+          for (int j = 0; j < NV; ++j) v[j][d] &= n >= 2 * d + 2 ? ~0u : n == 2 * d + 1 ? 0xffffu : 0u;
+      }
+      u16x2 largest = u16x2{0, 0};
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) largest = __builtin_elementwise_max(largest, __builtin_bit_cast(u16x2, v[j][d] & 0x7fff7fffu));
+      if (__ballot(max(largest.x, largest.y) >= 0x7f80) != 0) {
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
           for (int d = 0; d < 4; ++d) {
-            const uint32_t bad = ((v[j][d] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+            const uint32_t bad = ((v[j][d] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;  // (an exponent of ones carries)
             if (bad & 0x8000u) odd |= 1u << (2 * d), v[j][d] &= 0xffff0000u;
             if (bad & 0x80000000u) odd |= 2u << (2 * d), v[j][d] &= 0xffffu;
           }
@@ -301,23 +367,23 @@ __global__ __launch_bounds__(kPagesWaves * 64, 2) void pages_attend_kernel(Pages
     apart_of = 0;
     if (__ballot(odd != 0) == 0) return;
 #pragma unroll
-    for (int x = 0; x < 8; ++x) {
+    for (int x = 0; x < NX; ++x) {
       const unsigned long long who = __ballot((odd >> x) & 1);
 #pragma unroll
       for (int gg = 0; gg < 4; ++gg)
-        if ((who >> (16 * gg)) & 0xffff) apart_of |= 1u << (F32 ? 16 * (x >> 2) + 4 * gg + (x & 3) : 8 * gg + x);
+        if ((who >> (16 * gg)) & 0xffff) apart_of |= 1u << (NX * gg + x);
     }
   };
   // those values, for the rows that see them (LDS: the wave's own states, which nobody reads before its walk has ended)
-  float* scratch = lds + (size_t)w * 16 * ROW;
-  auto add_apart = [&](Running<HT>& r, const float (&p)[8], uint32_t sees, uint32_t apart_of, int i, int tok0) {
+  float* scratch = lds + (size_t)w * TILES * 16 * ROW;
+  auto add_apart = [&](Running<HT>& r, const float (&p)[NX], uint32_t sees, uint32_t apart_of, int i) {
 #pragma unroll
-    for (int x = 0; x < 8; ++x) scratch[c * 33 + token_of(x)] = p[x];
+    for (int x = 0; x < NX; ++x) scratch[c * 33 + token_of(x)] = p[x];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll 1
     for (uint32_t left = apart_of; left != 0; left &= left - 1) {
       const int tok = __builtin_ctz(left);
-      const T* from = (const T*)(block_base(i, tok >> 4) + a.view.v_offset * (int)sizeof(T)) + (tok & 15);
+      const T* from = (const T*)(block_base(i, NB == 2 ? tok >> 4 : 0) + a.view.v_offset * (int)sizeof(T)) + (tok & 15);
       const float pt = scratch[c * 33 + tok];
 #pragma unroll
       for (int j = 0; j < HT; ++j)
@@ -330,164 +396,446 @@ __global__ __launch_bounds__(kPagesWaves * 64, 2) void pages_attend_kernel(Pages
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   };
 
-  request_keys(0);
-  request_values(0);
-#pragma unroll 1
-  for (int i = 0; i < nsteps; ++i) {
-    const int tok0 = first + i * STEP;
-    const bool masked = tok0 + 32 > lo;  // (of the wave) some row does not see all 32 tokens
-    f32x4 score[TILES][2];
 #pragma unroll
-    for (int t = 0; t < TILES; ++t) score[t][0] = score[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int set = 0; set < SETS; ++set) request_keys(set, set), request_values(set, set);
+  auto step = [&](int i, auto which) {
+    constexpr int SET = decltype(which)::value;
+    const int tok0 = first + i * STEP;
+    const bool masked = tok0 + TOKENS > lo;  // (of the wave) some row does not see all tokens
+    f32x4 score[TILES][NB];
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+      for (int tt = 0; tt < NB; ++tt) score[t][tt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < NK; ++s)
 #pragma unroll
       for (int t = 0; t < TILES; ++t) {
         const k4u32x4 qs = query(t, s);
+        if constexpr (F32) {
 #pragma unroll
-        for (int tt = 0; tt < 2; ++tt) {
-          if constexpr (F32) {
+          for (int e = 0; e < 4; ++e)
+            score[t][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[SET][0][s][e]), __uint_as_float(qs[e]), score[t][0], 0, 0, 0);
+        } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              score[t][tt] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[tt][s][e]), __uint_as_float(qs[e]), score[t][tt], 0, 0, 0);
-          } else {
-            score[t][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[tt][s]), __builtin_bit_cast(bf16x8, qs), score[t][tt], 0, 0, 0);
-          }
+          for (int tt = 0; tt < NB; ++tt)
+            score[t][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[SET][tt][s]), __builtin_bit_cast(bf16x8, qs), score[t][tt], 0, 0, 0);
         }
       }
-    request_keys(i + 1);
+    request_keys(i + SETS, SET);
     settle(score);
-    float p[TILES][8];
+    float p[TILES][NX];
     uint32_t sees[TILES];
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
-      float sc[8] = {score[t][0][0], score[t][0][1], score[t][0][2], score[t][0][3], score[t][1][0], score[t][1][1], score[t][1][2], score[t][1][3]};
+#pragma unroll
+      for (int x = 0; x < NX; ++x) p[t][x] = score[t][x >> 2][x & 3];
       if (masked) {
         sees[t] = next_seen[t];
         if (i + 1 < nsteps) next_seen[t] = seen(t, tok0 + STEP);
 #pragma unroll
-        for (int x = 0; x < 8; ++x)
-          if (!((sees[t] >> token_of(x)) & 1)) sc[x] = -INFINITY;
+        for (int x = 0; x < NX; ++x)
+          if (!((sees[t] >> token_of(x)) & 1)) p[t][x] = -INFINITY;
       }
-      const float top = top_of(sc);
+      float top = max3(p[t][0], p[t][1], p[t][2]);
+      if constexpr (NX == 8) top = max3(max3(top, p[t][3], p[t][4]), max3(p[t][5], p[t][6], p[t][7]), p[t][7]);
+      else top = max3(top, p[t][3], p[t][3]);
       if (__ballot(top > run[t].moves) != 0) run[t].move_to(top, c1);
 #pragma unroll
-      for (int x = 0; x < 8; ++x) p[t][x] = __builtin_amdgcn_exp2f(fmaf(sc[x], c1, run[t].neg_m));
-      run[t].l += ((p[t][0] + p[t][1]) + (p[t][2] + p[t][3])) + ((p[t][4] + p[t][5]) + (p[t][6] + p[t][7]));
+      for (int x = 0; x < NX; ++x) p[t][x] = __builtin_amdgcn_exp2f(fmaf(p[t][x], c1, run[t].neg_m));
+#pragma unroll
+      for (int x = 0; x < NX; x += 4) run[t].l += (p[t][x] + p[t][x + 1]) + (p[t][x + 2] + p[t][x + 3]);
     }
     uint32_t apart_of = 0;
-    if (masked) drop_values(tok0, apart_of);
+    if (masked) drop_values(v[SET], tok0, apart_of);
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
       if constexpr (F32) {
 #pragma unroll
-        for (int x = 0; x < 8; ++x)
+        for (int x = 0; x < NX; ++x)
 #pragma unroll
           for (int j = 0; j < HT; ++j)
-            run[t].acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[(x >> 2) * HT + j][x & 3]), p[t][x], run[t].acc[j], 0, 0, 0);
+            run[t].acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[SET][j][x]), p[t][x], run[t].acc[j], 0, 0, 0);
       } else {
         unsigned pw[4][2];
 #pragma unroll
         for (int d = 0; d < 4; ++d) split_weights(p[t][2 * d], p[t][2 * d + 1], pw[d]);
 #pragma unroll
-        for (int j = 0; j < HT; ++j)
+        for (int m = 0; m < 2; ++m)
 #pragma unroll
-          for (int m = 0; m < 2; ++m)
-            run[t].acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v[j]), __builtin_bit_cast(bf16x8, k4u32x4{pw[0][m], pw[1][m], pw[2][m], pw[3][m]}),
+          for (int j = 0; j < HT; ++j)
+            run[t].acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v[SET][j]), __builtin_bit_cast(bf16x8, k4u32x4{pw[0][m], pw[1][m], pw[2][m], pw[3][m]}),
                                                                     run[t].acc[j], 0, 0, 0);
       }
     }
     settle(run);
     if (apart_of != 0) {
 #pragma unroll
-      for (int t = 0; t < TILES; ++t) add_apart(run[t], p[t], sees[t], apart_of, i, tok0);
+      for (int t = 0; t < TILES; ++t) add_apart(run[t], p[t], sees[t], apart_of, i);
     }
-    request_values(i + 1);
+    request_values(i + SETS, SET);
+  };
+#pragma unroll 1
+  for (int i = 0; i < nsteps; i += SETS) {
+    step(i, std::integral_constant<int, 0>{});
+    if constexpr (SETS == 2)
+      if (i + 1 < nsteps) step(i + 1, std::integral_constant<int, 1>{});
   }
 
-  // ---- the waves' states joined: rows, or a split's partial rows (written through) ----
-  constexpr int ROWS = TILES * 16, TPR = HD / 4;
-  const int rows_here = min(ROWS, wk.group_rows - wk.first_row), tasks = rows_here * TPR;  // a task: (row, 4 channels)
-  float(*states)[WAVES][16][ROW] = (float(*)[WAVES][16][ROW])lds;  // a row: its channels, its maximum and sum
+  float(*states)[TILES * 16][ROW] = (float(*)[TILES * 16][ROW])lds;  // [wave][row] its channels, its maximum and sum
 #pragma unroll
   for (int t = 0; t < TILES; ++t) {
 #pragma unroll
-    for (int j = 0; j < HT; ++j) *(f32x4*)&states[t][w][c][j * 16 + 4 * g] = run[t].acc[j];
+    for (int j = 0; j < HT; ++j) *(f32x4*)&states[w][t * 16 + c][j * 16 + 4 * g] = run[t].acc[j];
     const float l = fold_groups(run[t].l, LaneAdd{});
-    if (g == 0) *(f32x2*)&states[t][w][c][HD] = f32x2{partial_maximum(run[t].maximum(), l), l};
+    if (g == 0) *(f32x2*)&states[w][t * 16 + c][HD] = f32x2{partial_maximum(run[t].maximum(), l), l};
   }
   __syncthreads();
+  join_waves<HD, T, TILES * 16, WAVES, NT>(wk, it.split, clients.apart, lds, tid);
+  if (wk.nsplit == 1 || clients.apart || !wk.arrives_last(word)) return;
+  static_assert(join_floats<TILES * 16, NT>() <= (int)state_floats<HD, TILES>(), "what joins fits the states' LDS");
+  join_splits<HD, T, TILES * 16, NT>(wk, lds, tid);
+}
+
+// ---- many rows: waves have 32 rows each, over tokens that all of them read from LDS ----
+// bf16, products of 32 x 32 x 16.  WR waves have different rows, the others the same rows over other tokens: a workgroup has WR * 32
+// rows and takes 128 / WR tokens at a time (a stage).  Stages are copied from memory straight into a ring of LDS, one or two ahead: a wave
+// copies the keys or the values of a block.
+//
+// Layout of a product: operand lane (r, h) holds row (column) r, k = 8 h .. + 7; the result's register 4 u + i holds row 8 u + 4 h + i
+// of column r.  Row 8 a + 4 h + i of a block's keys is its token 8 h + 4 a + i: then a lane has the scores of 8 neighbouring tokens
+// of each block, which is what a product takes of their weights, and of a channel's values with one read.
+// LDS of 32 tokens: [block][keys, values], as the pool has them but for the order of 16-byte pieces, in which lanes that read together
+// find theirs in different banks: a key's piece c at c ^ (token), a channel's half u of its tokens at u ^ (channel / 4 % 2).
+template <int HD, int WR>
+struct Wide {
+  static constexpr int kShares = kPagesWaves / WR, kRows = WR * 32, kTokens = kShares * 32;  // of a workgroup; of a stage
+  static constexpr int kPart = kBlockTokens * HD * 2, kStage = kShares * 4 * kPart;          // bytes of a block's keys; of a stage
+  static constexpr int kRing = WR == 4 ? 3 : 2;
+  static constexpr size_t kStates = (size_t)kShares * kRows * (HD + kPagesPartPad) * sizeof(float);
+  static constexpr size_t kLds = (kRing * kStage > (int)kStates ? kRing * kStage : kStates) + 16;
+};
+
+template <int HD, int WR>
+__global__ __launch_bounds__(kPagesWaves * 64, 2) void pages_attend_wide_kernel(PagesAttend a, PagesClients clients) {
+  typedef Wide<HD, WR> W;
+  constexpr int KS = HD / 16, HT = HD / 32, ROW = HD + kPagesPartPad, SHARES = W::kShares, ROWS = W::kRows, STAGE = W::kTokens, RING = W::kRing;
+  constexpr int COPIES = HD / 32;  // instructions, of 1 KB, for a block's keys
+  extern __shared__ float lds[];
+
+  const int kvh = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r = lane & 31, h = lane >> 5, wr = w % WR, share = w / WR;
+  const PagesItem it = find_item(clients, blockIdx.y, lane);
+  const PagesWork<HD, uint16_t> wk(a, clients, it, kvh, ROWS / 16);
+  const int len = wk.len, before = len - wk.n_rows, span0 = it.split * clients.span;
+
+  // All rows of the workgroup see the first `lo` tokens, none sees any from `hi` on.
+  int lo = before, hi = len;
+  if (a.masks == nullptr) {
+    lo = before + 1 + div_by(wk.first_row, wk.group_rinv);
+    hi = before + 1 + div_by(min(wk.first_row + ROWS, wk.group_rows) - 1, wk.group_rinv);
+  }
+  const int end = min(it.split + 1 < wk.nsplit ? span0 + clients.span : len, hi);
+  const int nstages = end > span0 ? (end - span0 + STAGE - 1) / STAGE : 0;
+
+  // Copies: wave w has part w % 2 of block w / 2 of each 32 tokens.  64 stages' blocks sit in the lanes.
+  const bool values = w & 1;
+  int stage_blk[SHARES];
+  auto load_blocks = [&](int it0) {
+#pragma unroll
+    for (int sh = 0; sh < SHARES; ++sh) {
+      const int64_t tok = (int64_t)span0 + (int64_t)(it0 + lane) * STAGE + sh * 32 + (w >> 1) * 16;
+      stage_blk[sh] = wk.table[tok < len ? (int)(tok / kBlockTokens) : 0];
+    }
+  };
+  load_blocks(0);
+  unsigned from[COPIES];  // lane's bytes in the part
+#pragma unroll
+  for (int i = 0; i < COPIES; ++i) {
+    const int x = i * 64 + lane;  // where the piece lies in LDS
+    constexpr int PPT = HD / 8;   // pieces of a token
+    from[i] = values ? (x >> 1) * 32 + (((x & 1) ^ ((x >> 3) & 1)) << 4) : (x / PPT) * (HD * 2) + (((x % PPT) ^ (x / PPT % PPT)) << 4);
+  }
+  const char* part_base = (const char*)((const uint16_t*)a.view.pool + (int64_t)a.layer * a.view.layer_stride + (values ? a.view.v_offset : 0) +
+                                        (int64_t)kvh * kBlockTokens * HD);
+  const unsigned lds0 = (unsigned)(unsigned long long)(__attribute__((address_space(3))) char*)lds;
+  auto copy = [&](int i) {
+    if ((i & 63) == 0 && i > 0 && i < nstages) load_blocks(i);
+    const unsigned to = lds0 + (i % RING) * W::kStage + w * W::kPart;
+#pragma unroll
+    for (int sh = 0; sh < SHARES; ++sh) {
+      const char* p = part_base + (int64_t)__builtin_amdgcn_readlane(stage_blk[sh], i & 63) * a.view.block_elems * 2;
+#pragma unroll
+      for (int n = 0; n < COPIES; ++n) lds_dma16(p, from[n], to + sh * 4 * W::kPart + n * 1024);
+    }
+  };
+
+  // queries as operand B
+  const TileRow tr = wk.row(wk.first_row + wr * 32 + r);
+  const bool idle = wk.first_row + wr * 32 >= wk.group_rows;  // (of the wave) there are no such rows
+  k4u32x4 q[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) q[s] = *(const k4u32x4*)((const uint16_t*)a.q + tr.row * a.q_stride + tr.head * HD + s * 16 + h * 8);
+  // Which of the 32 tokens from tok0 on the row sees.  The words of a tree of up to 97 rows come with the queries: a load in the walk
+  // would wait for all copies.
+  constexpr int AHEAD = 4;
+  const uint32_t* words = a.masks + (size_t)tr.row * kPagesMaskWords;
+  uint32_t early[AHEAD] = {0, 0, 0, 0};
+  if (a.masks != nullptr) {
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) early[i] = words[i];
+  }
+  auto seen = [&](int tok0) -> uint32_t {
+    if (a.masks == nullptr) {
+      const int n = before + 1 + tr.row - wk.row_off - tok0;
+      return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
+    }
+    const int at = (tok0 - (before & ~31)) >> 5;
+    if (at >= AHEAD) return words[min(at, kPagesMaskWords - 1)];
+    uint32_t word = early[0];
+#pragma unroll
+    for (int i = 1; i < AHEAD; ++i) word = at == i ? early[i] : word;
+    return word;
+  };
+
+  f32x16 acc[1][HT];
+#pragma unroll
+  for (int j = 0; j < HT; ++j)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) acc[0][j][x] = 0.f;
+  float neg_m = 0.f, moves = -INFINITY, l = 0.f;  // as of a Running
+  auto maximum = [&] { return moves == -INFINITY ? -INFINITY : -neg_m; };
+  const float c1 = attend_scale<HD>();
+
+  // where the lane finds a key and a channel in a part
+  const int kt = 8 * ((r >> 2) & 1) + 4 * ((r >> 3) & 1) + (r & 3);
+  const unsigned key_at = (unsigned)((r >> 4) * 2 * W::kPart + kt * (HD * 2) + ((h ^ (kt % (HD / 8))) << 4));
+  const unsigned value_at = (unsigned)(W::kPart + r * 32 + ((h ^ ((r >> 2) & 1)) << 4));
+
+  auto step = [&](const char* at, int tok0) {
+    const bool masked = tok0 + 32 > lo;  // (of the workgroup) some row does not see all 32 tokens
+    f32x16 score[1][1];
+#pragma unroll
+    for (int x = 0; x < 16; ++x) score[0][0][x] = 0.f;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const k4u32x4 key = *(const k4u32x4*)(at + (key_at ^ (32u * s)));
+      score[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, key), __builtin_bit_cast(bf16x8, q[s]), score[0][0], 0, 0, 0);
+    }
+    k4u32x4 v[2][HT];  // [block]: tokens 8 h .. + 7 of a channel
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int j = 0; j < HT; ++j) v[s][j] = *(const k4u32x4*)(at + s * 2 * W::kPart + value_at + j * 1024);
+    settle(score);
+    float p[16];
+#pragma unroll
+    for (int x = 0; x < 16; ++x) p[x] = score[0][0][x];
+    uint32_t sees = ~0u, odd = 0;  // odd: (see the kernel of few rows) bits 8 s + x: token 16 s + 8 h + x
+    if (masked) {
+      sees = seen(tok0);
+#pragma unroll
+      for (int x = 0; x < 16; ++x)
+        if (!((sees >> (16 * (x >> 3) + 8 * h + (x & 7))) & 1)) p[x] = -INFINITY;
+      if (tok0 + 32 > len) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const int n = min(8, max(0, len - tok0 - 16 * s - 8 * h));
+#pragma unroll
+          for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int j = 0; j < HT; ++j) v[s][j][d] &= n >= 2 * d + 2 ? ~0u : n == 2 * d + 1 ? 0xffffu : 0u;
+        }
+      }
+      u16x2 largest = u16x2{0, 0};
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int j = 0; j < HT; ++j)
+#pragma unroll
+          for (int d = 0; d < 4; ++d) largest = __builtin_elementwise_max(largest, __builtin_bit_cast(u16x2, v[s][j][d] & 0x7fff7fffu));
+      if (__ballot(max(largest.x, largest.y) >= 0x7f80) != 0) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int j = 0; j < HT; ++j)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+              const uint32_t bad = ((v[s][j][d] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;  // (an exponent of ones carries)
+              odd |= (bad & 0x8000u ? 1u << (8 * s + 2 * d) : 0u) | (bad & 0x80000000u ? 2u << (8 * s + 2 * d) : 0u);
+              v[s][j][d] &= (bad & 0x8000u ? 0u : 0xffffu) | (bad & 0x80000000u ? 0u : 0xffff0000u);
+            }
+      }
+    }
+    float top = max3(p[0], p[1], p[2]);
+#pragma unroll
+    for (int x = 3; x < 15; x += 2) top = max3(top, p[x], p[x + 1]);
+    top = max3(top, p[15], p[15]);
+    if (__ballot(top > moves) != 0) {  // (the maximum moves only when a score passes it by 2^8)
+      const float m_old = maximum(), m_new = fmaxf(m_old, fold32(top, LaneMax{}) * c1);
+      const float alpha = m_new == m_old ? 1.f : __builtin_amdgcn_exp2f(m_old - m_new);
+      if (m_new != -INFINITY) {
+        neg_m = -m_new;
+        moves = (m_new + 8.f) * (1.f / c1);
+      }
+      l *= alpha;
+#pragma unroll
+      for (int j = 0; j < HT; ++j)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) acc[0][j][x] *= alpha;
+    }
+    unsigned pw[8][2];
+#pragma unroll
+    for (int x = 0; x < 16; ++x) p[x] = __builtin_amdgcn_exp2f(fmaf(p[x], c1, neg_m));
+#pragma unroll
+    for (int x = 0; x < 16; x += 4) l += (p[x] + p[x + 1]) + (p[x + 2] + p[x + 3]);
+#pragma unroll
+    for (int d = 0; d < 8; ++d) split_weights(p[2 * d], p[2 * d + 1], pw[d]);
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int j = 0; j < HT; ++j)
+          acc[0][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[s][j]), __builtin_bit_cast(bf16x8, k4u32x4{pw[4 * s][m], pw[4 * s + 1][m], pw[4 * s + 2][m], pw[4 * s + 3][m]}),
+                                                              acc[0][j], 0, 0, 0);
+    settle(acc);
+    if (__ballot(odd != 0) != 0) {  // values that are no numbers, for the rows that see them
+      uint32_t apart_of = 0;
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        const unsigned long long who = __ballot((odd >> x) & 1);
+        apart_of |= ((uint32_t)who ? 1u << (16 * (x >> 3) + (x & 7)) : 0u) | ((who >> 32) ? 1u << (16 * (x >> 3) + 8 + (x & 7)) : 0u);
+      }
 #pragma unroll 1
-  for (int task = tid; task < tasks; task += NT) {
-    const int mr = task / TPR, e0 = (task % TPR) * 4;
-    const float(*rows)[16][ROW] = states[mr / 16];
-    f32x2 ml[WAVES];
-    float m = -INFINITY;
+      for (; apart_of != 0; apart_of &= apart_of - 1) {
+        const int tok = __builtin_ctz(apart_of), x = 8 * (tok >> 4) + (tok & 7);
+        float pt = 0.f;
 #pragma unroll
-    for (int ww = 0; ww < WAVES; ++ww) {
-      ml[ww] = *(const f32x2*)&rows[ww][mr % 16][HD];
-      m = fmaxf(m, ml[ww].x);
-    }
-    const float m_ref = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
-    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < 16; ++i) pt = x == i ? p[i] : pt;
+        pt = __shfl(pt, r + 32 * ((tok >> 3) & 1), 64);
 #pragma unroll
-    for (int ww = 0; ww < WAVES; ++ww) {
-      const float sw = __builtin_amdgcn_exp2f(ml[ww].x - m_ref);
-      l += ml[ww].y * sw;
-      o += *(const f32x4*)&rows[ww][mr % 16][e0] * sw;
+        for (int j = 0; j < HT; ++j)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int ch = j * 32 + 8 * (e >> 2) + 4 * h + (e & 3);
+            const uint16_t y = *(const uint16_t*)(at + (tok >> 4) * 2 * W::kPart + W::kPart + ch * 32 + ((((tok >> 3) & 1) ^ ((ch >> 2) & 1)) << 4) + (tok & 7) * 2);
+            if (not_finite(y) && ((sees >> tok) & 1)) acc[0][j][e] += pt * bf16_bits_to_f32(y);
+          }
+      }
     }
-    if (wk.nsplit == 1) {
-      wk.finish(wk.first_row + mr, e0, o, l);
-    } else {
-      float* dst = wk.all + ((size_t)it.split * ROWS + mr) * ROW;
-      Xwg<true>::st4f(dst + e0, o);
-      if (e0 == 0) Xwg<true>::st4f(dst + HD, f32x4{partial_maximum(m, l), l, 0.f, 0.f});
+  };
+
+  constexpr int PER = SHARES * COPIES;  // copies of a stage that a wave has on their way
+#pragma unroll
+  for (int i = 0; i < RING - 1; ++i)
+    if (i < nstages) copy(i);
+#pragma unroll
+  for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(q[s]));  // (here: a wait in the walk would be one for copies, which the compiler does not count)
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) asm volatile("" : "+v"(early[i]));
+#pragma unroll 1
+  for (int i = 0; i < nstages; ++i) {
+    if (RING == 3 && i + 1 < nstages) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(PER) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();  // the stage has landed, and what the next copies go over has been read
+    if (i + RING - 1 < nstages) copy(i + RING - 1);
+    const int tok0 = span0 + i * STAGE + share * 32;
+    if (!idle && tok0 < end) {
+      const char* at = (const char*)lds + (i % RING) * W::kStage + share * 4 * W::kPart;
+      step(at, tok0);
     }
   }
-  if (wk.nsplit == 1 || clients.apart || !wk.arrives_last(word)) return;
-  static_assert(join_floats<ROWS, NT>() <= (int)state_floats<HD, TILES>(), "what joins fits the states' LDS");
-  join_splits<HD, T, ROWS, NT>(wk, lds, tid);
+  __syncthreads();
+  float(*states)[ROWS][ROW] = (float(*)[ROWS][ROW])lds;
+#pragma unroll
+  for (int j = 0; j < HT; ++j)
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      *(f32x4*)&states[share][wr * 32 + r][j * 32 + 8 * u + 4 * h] = f32x4{acc[0][j][4 * u], acc[0][j][4 * u + 1], acc[0][j][4 * u + 2], acc[0][j][4 * u + 3]};
+  l = fold32(l, LaneAdd{});
+  if (h == 0) *(f32x2*)&states[share][wr * 32 + r][HD] = f32x2{partial_maximum(maximum(), l), l};
+  __syncthreads();
+  join_waves<HD, uint16_t, ROWS, SHARES, kPagesWaves * 64>(wk, it.split, true, lds, tid);
 }
 
-// The splits of clients that their last workgroup would take long to join: workgroup (cache head, client's group of tiles).
-template <int HD, typename T, int TILES>
-__global__ __launch_bounds__(kPagesWaves * 64) void pages_join_kernel(PagesAttend a, PagesClients clients) {
-  __shared__ float lds[join_floats<TILES * 16, kPagesWaves * 64>()];
-  int group = blockIdx.y, ci = 0;
+// The splits of a workgroup's rows joined apart: workgroup (cache head, some rows of a client's group), a thread 4 channels of a row.
+template <int HD, typename T, int ROWS>
+__global__ __launch_bounds__(256) void pages_join_kernel(PagesAttend a, PagesClients clients) {
+  constexpr int TPR = HD / 4, ROW = HD + kPagesPartPad, PER = 256 / TPR, BATCH = 8;
+  int group = blockIdx.y / (ROWS / PER), ci = 0;
   while (group >= clients.groups[ci]) group -= clients.groups[ci++];
-  if (clients.nsplit[ci] == 1) return;  // (whole workgroup)
-  const PagesWork<HD, T> wk(a, clients, PagesItem{ci, group, 0}, blockIdx.x, TILES);
-  join_splits<HD, T, TILES * 16, kPagesWaves * 64>(wk, lds, threadIdx.x);
+  if (clients.nsplit[ci] == 1) return;
+  const PagesWork<HD, T> wk(a, clients, PagesItem{ci, group, 0}, blockIdx.x, ROWS / 16);
+  const int mr = blockIdx.y % (ROWS / PER) * PER + threadIdx.x / TPR, e0 = threadIdx.x % TPR * 4;
+  if (wk.first_row + mr >= wk.group_rows) return;
+  const float* from = wk.all + (size_t)mr * ROW;
+  float m = -INFINITY, l = 0.f;
+  f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+  for (int s0 = 0; s0 < wk.nsplit; s0 += BATCH) {
+    f32x4 ob[BATCH];
+    f32x2 ml[BATCH];
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j) {
+      const float* p = from + (size_t)min(s0 + j, wk.nsplit - 1) * (ROWS * ROW);
+      ob[j] = *(const f32x4*)(p + e0);
+      ml[j] = *(const f32x2*)(p + HD);
+      if (s0 + j >= wk.nsplit) ml[j].x = -INFINITY;
+    }
+    float top = m;
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j) top = fmaxf(top, ml[j].x);
+    const float back = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+    l *= back;
+    o *= back;
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j) {
+      if (ml[j].x == -INFINITY) continue;
+      const float sw = __builtin_amdgcn_exp2f(ml[j].x - top);
+      l += ml[j].y * sw;
+      o += ob[j] * sw;
+    }
+    m = top;
+  }
+  wk.finish(wk.first_row + mr, e0, o, l);
 }
 
-template <int HD, typename T, int TILES>
-static hipError_t launch(const PagesAttend& a, const PagesClients& c, hipStream_t st) {
-  static std::atomic<uint64_t> allowed;
-  constexpr size_t bytes = attend_lds_bytes<HD, T, TILES>();
+template <class Kernel, class Join>
+static hipError_t launch(Kernel kernel, Join join, std::atomic<uint64_t>& allowed, size_t bytes, int waves, int rows, const PagesAttend& a,
+                         const PagesClients& c, hipStream_t st) {
   if (bytes > 65536) {
-    const hipError_t e = allow_lds(allowed, (const void*)pages_attend_kernel<HD, T, TILES>, bytes);
+    const hipError_t e = allow_lds(allowed, (const void*)kernel, bytes);
     if (e != hipSuccess) return e;
   }
-  pages_attend_kernel<HD, T, TILES><<<dim3(a.view.n_kv_heads, c.items), kPagesWaves * 64, bytes, st>>>(a, c);
-  hipError_t e = hipGetLastError();
+  kernel<<<dim3(a.view.n_kv_heads, c.items), waves * 64, bytes, st>>>(a, c);
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !c.apart) return e;
   int groups = 0;
   for (int i = 0; i < c.n; ++i) groups += c.groups[i];
-  pages_join_kernel<HD, T, TILES><<<dim3(a.view.n_kv_heads, groups), kPagesWaves * 64, 0, st>>>(a, c);
+  join<<<dim3(a.view.n_kv_heads, groups * (rows / (1024 / a.view.head_dim))), 256, 0, st>>>(a, c);
   return hipGetLastError();
+}
+template <int HD, typename T, int TILES>
+static hipError_t launch_few(const PagesAttend& a, const PagesClients& c, hipStream_t st) {
+  static std::atomic<uint64_t> allowed;
+  return launch(pages_attend_kernel<HD, T, TILES>, pages_join_kernel<HD, T, TILES * 16>, allowed, attend_lds_bytes<HD, T, TILES>(), kPagesFewWaves, TILES * 16, a, c, st);
+}
+template <int HD, int WR>
+static hipError_t launch_wide(const PagesAttend& a, const PagesClients& c, hipStream_t st) {
+  static std::atomic<uint64_t> allowed;
+  return launch(pages_attend_wide_kernel<HD, WR>, pages_join_kernel<HD, uint16_t, WR * 32>, allowed, Wide<HD, WR>::kLds, kPagesWaves, WR * 32, a, c, st);
 }
 
 hipError_t launch_pages_attend(const PagesAttend& a, const PagesLaunch& l, hipStream_t st) {
-  auto tiles = [&](auto hd, auto t) {
-    typedef decltype(t) T;
+  auto go = [&](auto hd) {
     constexpr int HD = decltype(hd)::value;
-    return l.tiles == 1 ? launch<HD, T, 1>(a, l.c, st) : launch<HD, T, 2>(a, l.c, st);
+    if (a.dtype == PIPESD_F32) return l.tiles == 1 ? launch_few<HD, float, 1>(a, l.c, st) : launch_few<HD, float, 2>(a, l.c, st);
+    if (l.tiles == 1) return launch_few<HD, uint16_t, 1>(a, l.c, st);
+    if (l.tiles == 2) return launch_few<HD, uint16_t, 2>(a, l.c, st);
+    return l.tiles == 4 ? launch_wide<HD, 2>(a, l.c, st) : launch_wide<HD, 4>(a, l.c, st);
   };
-  typedef std::integral_constant<int, 64> H64;
-  typedef std::integral_constant<int, 128> H128;
-  if (a.view.head_dim == 128) return a.dtype == PIPESD_F32 ? tiles(H128{}, float{}) : tiles(H128{}, uint16_t{});
-  return a.dtype == PIPESD_F32 ? tiles(H64{}, float{}) : tiles(H64{}, uint16_t{});
+  return a.view.head_dim == 128 ? go(std::integral_constant<int, 128>{}) : go(std::integral_constant<int, 64>{});
 }
 
 }  // namespace pipesd

@@ -4,6 +4,7 @@
 // value blocks [kv_head][head_dim][token].  Blocks may belong to several clients: what writes gets its own first.
 #pragma once
 
+#include <math.h>
 #include "common.h"
 
 namespace pipesd {
@@ -19,14 +20,16 @@ constexpr int kPagesMaskWords = (31 + kPagesTreeRows + 31) / 32;
 // A client's query rows are taken with the heads that share a head of the cache: row rr of a cache head is pass row rr /
 // group, head rr % group of the group; 16 of them make a tile.  A workgroup has `tiles` of them, of one client and cache head, and a
 // span of the context.
-constexpr int kPagesWaves = 4;
-constexpr int kPagesStep = kPagesWaves * 32;  // tokens that a workgroup takes at a time
+constexpr int kPagesFewWaves = 8;  // of a workgroup of one or two tiles
+constexpr int kPagesWaves = 4;     // of one of more
+constexpr int kPagesStep = 128;    // spans are a multiple of so many tokens
 constexpr int kPagesMaxSplits = 64;
 // a client's last split takes up to so many tokens more than the others
 constexpr int kPagesSplitSlack = 64;
 inline int pages_splits(int64_t len, int64_t span) { return (int)std::max<int64_t>(1, (len - kPagesSplitSlack + span - 1) / span); }
 constexpr int kPagesCutRounds = 4;  // workgroups whose rows are to be joined, in rounds that fill the device: bounds the partial rows
 
+constexpr int kPagesPartPad = 4;  // a partial row is [head_dim values, max, sum, 2 unused]
 constexpr int kPagesPerLaunch = 32;     // clients of a launch, by value
 constexpr int kPagesMaxItems = 65535;   // workgroups of a grid in y
 struct PagesClients {
@@ -50,17 +53,25 @@ struct PagesNeeds {
   size_t part_tiles, counters;
 };
 
-// What workgroups of one and two tiles take, in us: a launch, a workgroup to begin and end, 32 tokens of it by compute unit with both
-// workgroups that one holds, how much longer one takes alone, and a join.
+// What workgroups of one, two, four and eight tiles take: tokens of a step, its time in us on a compute unit by itself and with as many
+// workgroups as one holds, and what a workgroup's beginning and end add.  One or two tiles ask for as much as a compute unit gets (58 GB/s).
+// Fitted to 8 heads of 128: 4096 tokens more of one client 36, 38, 78 and 107 us with 8 workgroups; 64 rows behind 32768 75 us with
+// 512 of four tiles, 71 with 512 of eight, 78 with 256 of them.
 struct PagesCost {
-  double start, begin, step, alone, join;
-  int resident;
+  int tokens, resident;
+  double alone, full, begin;
 };
+constexpr int kPagesTiles[4] = {1, 2, 4, 8};
 constexpr PagesCost pages_cost(int tiles, int dtype, int head_dim) {
-  const bool f32 = dtype == PIPESD_F32;
-  const double bytes = 4. * head_dim * 32 * (f32 ? 2 : 1);  // of 32 tokens
-  return PagesCost{2, 3, bytes / 22000 * (tiles == 1 ? 1 : 1.15), 0.6, 4, 2};
+  const double part = head_dim == 128 ? 1 : tiles <= 2 ? 0.5 : 0.75;  // (the weights' instructions do not get fewer)
+  if (dtype == PIPESD_F32) return tiles == 1 ? PagesCost{128, 1, 2.9 * part, 2.9 * part, 4} : PagesCost{128, 1, tiles == 2 ? 4.5 * part : 1e30, 4.5 * part, 4};
+  if (tiles == 1) return PagesCost{256, 1, 2.25 * part, 2.25 * part, 4};
+  if (tiles == 2) return PagesCost{256, 1, 2.35 * part, 2.35 * part, 4};
+  if (tiles == 4) return PagesCost{64, 2, 1.4 * part, 1.87 * part, 5};
+  return PagesCost{32, 2, 1 * part, 1.75 * part, 5};
 }
+constexpr double kPagesLaunchUs = 2, kPagesJoinUs = 3.5, kPagesApartUs = 4;  // a launch; what joins splits, in the last workgroup and apart
+constexpr double kPagesMemory = 5.8e6, kPagesCaches = 12e6, kPagesParts = 2.9e6;  // bytes a us: of the cache once, again, of partial rows (there and back)
 
 // The launches of a pass, at most kPagesPerLaunch clients in one.  All splits are as long, some part of the longest context: as short
 // as pays for what begins and joins them, in rounds of workgroups that fill the device.  So what a row's sums are cut into depends on
@@ -72,53 +83,63 @@ inline PagesNeeds pages_plan(const PagesClient* cl, int n, int dtype, int head_d
   PagesNeeds need{0, 0};
   auto sets = [&](const PagesClient& c, int tiles) { return ((int64_t)group * c.n_rows + 16 * tiles - 1) / (16 * tiles); };
   int longest = 0;
+  double once = 0;  // tokens of all clients and heads
   for (int i = 0; i < n; ++i)
-    if (cl[i].n_rows > 0) longest = std::max(longest, (int)cl[i].len);
+    if (cl[i].n_rows > 0) longest = std::max(longest, (int)cl[i].len), once += (double)n_kv_heads * cl[i].len;
   if (longest == 0) return need;
+  const double token_bytes = 2. * head_dim * (dtype == PIPESD_F32 ? 4 : 2), row_bytes = 4. * (head_dim + kPagesPartPad);
   auto best = [&](int tiles, int64_t* span) {
     const PagesCost cost = pages_cost(tiles, dtype, head_dim);
     const int64_t room = (int64_t)cost.resident * n_cu, cut = std::max<int64_t>(1, longest - kPagesSplitSlack);
-    double tokens = 0, time = 1e300;  // tokens: that all workgroups walk
-    for (int i = 0; i < n; ++i) tokens += (double)n_kv_heads * sets(cl[i], tiles) * cl[i].len;
+    double walked = 0, time = 1e300;  // walked: by all workgroups, tokens
+    for (int i = 0; i < n; ++i) walked += (double)n_kv_heads * sets(cl[i], tiles) * cl[i].len;
+    const double memory = std::max(once * token_bytes / kPagesMemory, walked * token_bytes / kPagesCaches);
     int64_t last = 0;
     for (int halves = 2; halves <= 2 * kPagesMaxSplits; halves += halves < 16 ? 1 : 2) {  // half parts of the longest context
       const int64_t s = ((2 * cut + halves - 1) / halves + kPagesStep - 1) / kPagesStep * kPagesStep;
       if (s == last) continue;
       last = s;
       int64_t groups = 0, cut_groups = 0;
+      double cut_rows = 0;
       for (int i = 0; i < n; ++i) {
         if (cl[i].n_rows == 0) continue;
         const int nsplit = pages_splits(cl[i].len, s);
         const int64_t g = (int64_t)n_kv_heads * sets(cl[i], tiles) * nsplit;
         groups += g;
-        if (nsplit > 1) cut_groups += g;
+        if (nsplit > 1) cut_groups += g, cut_rows += (double)n_q_heads * cl[i].n_rows * nsplit;
       }
       if (cut_groups > kPagesCutRounds * room) break;  // (more still with shorter ones)
-      const double walk = std::min<double>(s, longest) / 32 * cost.step;
+      const double walk = (std::min<int64_t>(s + kPagesSplitSlack, longest) + cost.tokens - 1) / cost.tokens;
       // rounds of workgroups that all walk as far as the longest does, or all walks shared evenly and then one of the longest
       const int64_t rounds = groups / room, left = groups % room;
-      const double by_rounds = rounds * (walk * cost.resident + cost.begin) +
-                               (left ? walk * (left <= n_cu ? cost.alone : cost.resident) + cost.begin : 0);
-      const double by_tokens = tokens / 32 * cost.step / n_cu + walk * cost.alone + (1 + (double)groups / room) * cost.begin;
-      const double t = cost.start + (n > 1 ? std::min(by_rounds, by_tokens) : by_rounds) + (s < cut ? cost.join : 0);
+      const double by_rounds = rounds * (walk * cost.full + cost.begin) + (left ? walk * (left <= n_cu ? cost.alone : cost.full) + cost.begin : 0);
+      const double by_tokens = walked / cost.tokens * cost.full / room + walk * cost.alone + (1 + (double)groups / room) * cost.begin;
+      const double walks = n > 1 ? std::min(by_rounds, by_tokens) : by_rounds;
+      // (work and memory that take as long do not quite run side by side)
+      const double t = kPagesLaunchUs + sqrt(sqrt(walks * walks * walks * walks + memory * memory * memory * memory)) +
+                       (s >= cut ? 0 : tiles <= 2 ? kPagesJoinUs : kPagesApartUs + cut_rows * row_bytes / kPagesParts);
       if (t < time) time = t, *span = s;
     }
     return time;
   };
-  int64_t span1 = 0, span2 = 0;
-  const double time1 = best(1, &span1), time2 = best(2, &span2);
-  const int tiles = time1 <= time2 ? 1 : 2;
-  const int64_t span = tiles == 1 ? span1 : span2;
+  int tiles = 1;
+  int64_t span = 0;
+  double time = 1e300;
+  for (int k : kPagesTiles) {
+    int64_t its = 0;
+    const double t = best(k, &its);
+    if (t < time) time = t, tiles = k, span = its;
+  }
   PagesLaunch l{};
   auto flush = [&] {
     if (l.c.n == 0) return;
     for (int i = l.c.n; i < kPagesPerLaunch; ++i) l.c.first[i] = l.c.items;
     for (int i = 0; i < l.c.n; ++i) {  // (where the last workgroup would go to memory 4 times and more)
-      const int threads = kPagesWaves * 64, tasks = std::min(group * l.c.n_rows[i], tiles * 16) * (head_dim / 4);
+      const int threads = kPagesFewWaves * 64, tasks = std::min(group * l.c.n_rows[i], tiles * 16) * (head_dim / 4);
       int shares = 1;
       while (2 * shares * tasks <= threads) shares *= 2;
       const int turns = (tasks + threads - 1) / threads * ((l.c.nsplit[i] + 8 * shares - 1) / (8 * shares));
-      if (l.c.nsplit[i] > 1 && turns > 3) l.c.apart = 1;
+      if (l.c.nsplit[i] > 1 && (tiles > 2 || turns > 3)) l.c.apart = 1;
     }
     out.push_back(l);
     l = PagesLaunch{};
@@ -152,7 +173,7 @@ inline PagesNeeds pages_plan_most(int clients, int rows, int64_t len, int dtype,
   const int64_t all = ((int64_t)(n_q_heads / n_kv_heads) * rows + 15) / 16;
   const int64_t splits = std::min<int64_t>(kPagesMaxSplits, pages_splits(len, kPagesStep));
   size_t most = 0;
-  for (int tiles : {1, 2}) {
+  for (int tiles : kPagesTiles) {
     const int64_t cut = std::min<int64_t>((int64_t)clients * n_kv_heads * ((all + tiles - 1) / tiles) * splits,
                                           (int64_t)kPagesCutRounds * pages_cost(tiles, dtype, head_dim).resident * n_cu);
     if (splits > 1) most = std::max(most, (size_t)(cut * tiles));
@@ -161,17 +182,21 @@ inline PagesNeeds pages_plan_most(int clients, int rows, int64_t len, int dtype,
 }
 
 // ---- bookkeeping on the device -----------------------------------------------------------------
-// Entries of the block tables that changed and the trees of a pass, by value: no copy that the host would have to keep.
+// Entries of the block tables that changed, blocks that are copied and the trees of a pass, by value: no copy that the host would have
+// to keep.
 constexpr int kPagesEntriesPerLaunch = 128;
 constexpr int kPagesParentsPerLaunch = 1024;
+constexpr int kPagesOwnPerLaunch = 32;
 struct PagesBegin {
+  int32_t own;                                                      // blocks that clients get for one that others hold as well
+  int32_t own_from[kPagesOwnPerLaunch], own_to[kPagesOwnPerLaunch];
   int32_t n;                                                        // entries
   int32_t at[kPagesEntriesPerLaunch], v[kPagesEntriesPerLaunch];    // table[at[i]] = v[i]
   int32_t trees;
   int32_t row_off[kPagesPerLaunch], n_rows[kPagesPerLaunch], before[kPagesPerLaunch];  // before: tokens in front of the pass
   int16_t parent[kPagesParentsPerLaunch];                           // the trees' rows one after the other: within the tree, -1 for none
 };
-hipError_t launch_pages_begin(const PagesBegin& b, int32_t* table, uint32_t* masks, hipStream_t st);
+hipError_t launch_pages_begin(int dtype, const KvView& v, int n_layers, const PagesBegin& b, int32_t* table, uint32_t* masks, hipStream_t st);
 // rows of block tables copied on the device
 struct PagesForks {
   int32_t n, most;
@@ -210,7 +235,6 @@ struct PagesAttend {
   float* part;
   unsigned* counters;
 };
-constexpr int kPagesPartPad = 4;  // a partial row is [head_dim values, max, sum, 2 unused]
 hipError_t launch_pages_attend(const PagesAttend& a, const PagesLaunch& l, hipStream_t st);
 
 }  // namespace pipesd

@@ -7,7 +7,9 @@ namespace pipesd {
 
 constexpr int kTreeRows = 256;      // of a client, and of the clients of a launch together
 constexpr int kTreeClients = 16;    // of a launch
-constexpr int kTreeChunks = 64;     // workgroups that share a row of the vocabulary
+constexpr int kTreeChunks = 64;     // workgroups that share a row of the vocabulary, at most
+constexpr int kTreeChunk = 2048;    // tokens of one, unless there are more
+constexpr int kTreeSmall = 8192;    // vocabulary that one workgroup decides on alone
 
 // what the launches of a call hand on, in the caller's memory; the counters are zero between launches
 struct TreeWorkspace {
@@ -32,16 +34,21 @@ inline TreeWorkspace tree_workspace(void* p) {
   return w;
 }
 
+struct TreeRow {
+  int32_t token;
+  float u;
+  int16_t parent;          // within the client's rows
+  uint8_t nth, children;   // which child of its parent it is; how many it has
+};
 struct TreeCall {
-  const float *p, *q;  // rows of the launch's first client on; q: nullptr for token matching
+  const float *p, *q;      // rows of the launch's first client on; q: nullptr for token matching
   int64_t p_stride, q_stride;
-  int32_t V, n, distinct, stages;  // stages: children of the row that has the most
+  int32_t V, n, distinct;
+  int32_t stages;          // children of the row that has the most
+  int32_t chunks;          // workgroups that share a row of the vocabulary
   int32_t row_off[kTreeClients], rows[kTreeClients];
-  int32_t token[kTreeRows];
-  float u[kTreeRows];
-  int16_t parent[kTreeRows];       // within the client's rows
-  uint8_t nth[kTreeRows], children[kTreeRows];  // which child of its parent a row is; how many it has
-  int32_t* result;                 // [clients][result_stride]
+  TreeRow row[kTreeRows];
+  int32_t* result;         // [clients][result_stride]
   int64_t result_stride;
   TreeWorkspace ws;
 };

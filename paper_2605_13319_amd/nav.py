@@ -195,6 +195,9 @@ def _floats(a):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _stream() -> int:
     """The current stream's handle (0.5 us; 2.8 through a Stream object)."""
     if _raw_stream is not None and torch.cuda.is_initialized():
@@ -731,7 +734,7 @@ class PageCache:
 
     def _call(self, call, name: str, *args) -> None:
         """A call that works on the pool's device, on its current stream."""
-        if self.pool is None or torch.cuda.current_device() == self._device_index:
+        if self.pool is None or _current_device() == self._device_index:
             _check(call(self.handle, *args, self._stream()), name)
         else:
             with torch.cuda.device(self._device_index):
@@ -846,47 +849,55 @@ def tree_workspace(n_seqs: int, rows: int, device: str = "cuda:0"):
     return torch.zeros(_lib.pipesd_tree_accept_workspace(), dtype=torch.uint8, device=device)
 
 
+def _rows_of(x, name: str, device: int, shape=None):
+    """(shape, elements between rows) of a float32 matrix on a GPU whose rows' elements lie side by side."""
+    if x.dtype is not torch.float32 or x.get_device() != device or device < 0:
+        raise ValueError(f"{name}: a float32 tensor on a GPU, the same for all, not {x.dtype} on {x.device}")
+    size = x.shape
+    if len(size) != 2 or (shape is not None and size != shape):
+        raise ValueError(f"{name}: rows of distributions{'' if shape is None else f' {tuple(shape)}'}, not {tuple(size)}")
+    apart, step = x.stride()
+    if step != 1 and size[1] > 1:
+        raise ValueError(f"{name}: tokens side by side, not {step} apart")
+    return size, max(apart, size[1])
+
+
 def tree_accept(p, q, tokens: Sequence[int], parents: Sequence[int], uniforms, rows: Optional[Sequence[int]] = None, distinct: bool = False,
                 result=None, workspace=None):
     """The decision on trees of drafts, one client's rows after the other's: p, q torch CUDA float32 [rows][V] (q None: token matching),
     rows: the clients' numbers of them (None: one client).  Enqueues the work on the current stream of p's device and returns `result`,
     int32 [clients][more than any rows]: accepted drafts a, next token, the a accepted rows, then -1 (a new tensor if None)."""
+    device = p.get_device()
+    if device >= 0 and device != _current_device():
+        with torch.cuda.device(device):
+            return tree_accept(p, q, tokens, parents, uniforms, rows, distinct, result, workspace)
     (t, n, _tokens, _), (up, m, _parents, _) = _numbers(tokens), _numbers(parents)
-    if rows is None:
-        rows = [n]
-    r, clients, counts, total = _numbers(rows)
+    r, clients, counts, total = _numbers([n] if rows is None else rows)
     if n != total or m != total or clients < 1:
         raise ValueError(f"{clients} clients of {total} rows, {n} tokens, {m} parents")
-    for x, name in ((p, "p"), (q, "q")):
-        if x is None and name == "q":
-            continue
-        if x.dtype is not torch.float32 or not x.is_cuda or x.device != p.device or x.dim() != 2 or x.shape != p.shape or (x.stride(1) != 1 and x.shape[1] > 1):
-            raise ValueError(f"{name}: a float32 tensor [rows][vocabulary], tokens side by side, on a GPU")
-    if p.shape[0] != total:
-        raise ValueError(f"{p.shape[0]} distributions, {total} rows")
-    u = None
+    size, ps = _rows_of(p, "p", device)
+    qp, qs, u = None, 0, None
     if q is not None:
         if uniforms is None or len(uniforms) != total:
             raise ValueError(f"{total} rows need as many uniforms")
-        u = _floats(uniforms)
+        qp, qs, u = q.data_ptr(), _rows_of(q, "q", device, size)[1], _floats(uniforms)
+    if size[0] != total:
+        raise ValueError(f"{size[0]} distributions, {total} rows")
     width = max(counts) + 1
     if result is None:
         result = torch.empty((clients, width), dtype=torch.int32, device=p.device)
-    elif (result.dtype is not torch.int32 or result.device != p.device or result.dim() != 2 or result.shape[0] != clients or result.shape[1] < width
-          or not result.is_contiguous()):
-        raise ValueError(f"result: a contiguous int32 tensor [{clients}][{width} or more] on {p.device}")
+    else:
+        got = result.shape
+        if (result.dtype is not torch.int32 or result.get_device() != device or len(got) != 2 or got[0] != clients or got[1] < width
+                or not result.is_contiguous()):
+            raise ValueError(f"result: a contiguous int32 tensor [{clients}][{width} or more] on {p.device}")
+        width = got[1]
     if workspace is None:
         workspace = tree_workspace(clients, total, p.device)
-    elif workspace.dtype is not torch.uint8 or workspace.device != p.device or not workspace.is_contiguous():
+    elif workspace.dtype is not torch.uint8 or workspace.get_device() != device or not workspace.is_contiguous():
         raise ValueError(f"workspace: what tree_workspace returns, on {p.device}")
-    if torch.cuda.current_device() != p.device.index:
-        with torch.cuda.device(p.device):
-            return tree_accept(p, q, tokens, parents, uniforms, rows, distinct, result, workspace)
-    vocab = p.shape[1]
-    stream = _raw_stream(p.device.index) if _raw_stream is not None else int(torch.cuda.current_stream(p.device).cuda_stream)
-    _check(_lib.pipesd_tree_accept(p.data_ptr(), max(p.stride(0), vocab), None if q is None else q.data_ptr(),
-                                   0 if q is None else max(q.stride(0), vocab), vocab, clients, r, t, up, u, 1 if distinct else 0,
-                                   result.data_ptr(), result.shape[1], workspace.data_ptr(), workspace.numel(), stream),
+    _check(_lib.pipesd_tree_accept(p.data_ptr(), ps, qp, qs, size[1], clients, r, t, up, u, 1 if distinct else 0, result.data_ptr(), width,
+                                   workspace.data_ptr(), workspace.numel(), _stream() if _raw_stream is None else _raw_stream(device)),
            "pipesd_tree_accept")
     return result
 
