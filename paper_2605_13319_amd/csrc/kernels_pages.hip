@@ -117,6 +117,17 @@ __global__ __launch_bounds__(256) void pages_store_kernel(KvView v, int layer, P
   T* kb = (T*)v.pool + base;
   T* vb = (T*)v.pool + base + v.v_offset;
   const int64_t row0 = rg.row_off[c] + (t0 - first);  // (of the block's first token; before the rows where the pass begins in it)
+  // What other tokens of a block have is written again: the workgroup is the only one that writes there.  (It is asked for with the rows.)
+  constexpr int PIECES = HD * P::kOfTokens, PER = (PIECES + 255) / 256;
+  const bool whole = lo == 0 && hi == kBlockTokens;
+  uint4 there[PER];
+#pragma unroll
+  for (int n = 0; n < PER; ++n) there[n] = make_uint4(0, 0, 0, 0);
+  if (!whole) {
+#pragma unroll
+    for (int n = 0; n < PER; ++n)
+      if (tid + n * 256 < PIECES) there[n] = ((const uint4*)vb)[tid + n * 256];
+  }
   for (int i = tid; i < kBlockTokens * P::kOfRow; i += 256) {
     const int t = i / P::kOfRow, e = i % P::kOfRow * P::kElems;
     if (t < lo || t >= hi) continue;
@@ -127,21 +138,16 @@ __global__ __launch_bounds__(256) void pages_store_kernel(KvView v, int layer, P
     for (int j = 0; j < P::kElems; ++j) tile.v[e + j][t] = xs[j];
   }
   __syncthreads();
-  if (lo == 0 && hi == kBlockTokens) {
-    for (int i = tid; i < HD * P::kOfTokens; i += 256) {
-      const int e = i / P::kOfTokens, t = i % P::kOfTokens * P::kElems;
-      uint4 x;
-      T* xs = (T*)&x;
 #pragma unroll
-      for (int j = 0; j < P::kElems; ++j) xs[j] = tile.v[e][t + j];
-      *(uint4*)(vb + e * kBlockTokens + t) = x;
-    }
-  } else {  // (the block's other tokens stay as they are)
-    const int n = hi - lo;
-    for (int i = tid; i < HD * n; i += 256) {
-      const int e = i / n, t = lo + i % n;
-      vb[e * kBlockTokens + t] = tile.v[e][t];
-    }
+  for (int n = 0; n < PER; ++n) {
+    const int i = tid + n * 256, e = i / P::kOfTokens, t = i % P::kOfTokens * P::kElems;
+    if (i >= PIECES) break;
+    T* xs = (T*)&there[n];
+    bool any = false;
+#pragma unroll
+    for (int j = 0; j < P::kElems; ++j)
+      if (t + j >= lo && t + j < hi) xs[j] = tile.v[e][t + j], any = true;
+    if (any) ((uint4*)vb)[i] = there[n];
   }
 }
 

@@ -49,15 +49,17 @@ struct PagesWork {
   }
   __device__ __forceinline__ TileRow row(int rr) const { return tile_row(rr, a.group, group_rinv, n_rows, row_off, kvh); }
 
-  __device__ __forceinline__ void finish(int rr, int e0, const f32x4& o, float l) const {  // 4 channels of a row: o / l
-    const TileRow tr = row(rr);
-    if (!tr.live) return;
-    float inv = __builtin_amdgcn_rcpf(l);  // (a row sees itself: l is 0 only where all its scores are -inf, and then there is no number)
-    inv = inv * (2.f - l * inv);
-    const f32x4 y = o * inv;
-    T* out = (T*)a.out + tr.row * a.out_stride + tr.head * HD + e0;
+  static __device__ __forceinline__ float inverse(float l) {  // (a row sees itself: l is 0 only where all its scores are -inf, and then there is no number)
+    const float inv = __builtin_amdgcn_rcpf(l);
+    return inv * (2.f - l * inv);
+  }
+  static __device__ __forceinline__ void store(T* out, const f32x4& y) {
     if constexpr (sizeof(T) == 4) *(f32x4*)out = y;
     else *(uint2*)out = make_uint2(pack2_bf16(y[0], y[1]), pack2_bf16(y[2], y[3]));
+  }
+  __device__ __forceinline__ void finish(int rr, int e0, const f32x4& o, float l) const {  // 4 channels of a row: o / l
+    const TileRow tr = row(rr);
+    if (tr.live) store((T*)a.out + tr.row * a.out_stride + tr.head * HD + e0, o * inverse(l));
   }
 
   // The partial rows have been written through; whoever of the splits arrives last joins them.  All threads of the workgroup.
@@ -512,8 +514,8 @@ struct Wide {
   static constexpr int kShares = kPagesWaves / WR, kRows = WR * 32, kTokens = kShares * 32;  // of a workgroup; of a stage
   static constexpr int kPart = kBlockTokens * HD * 2, kStage = kShares * 4 * kPart;          // bytes of a block's keys; of a stage
   static constexpr int kRing = WR == 4 ? 3 : 2;
-  static constexpr size_t kStates = (size_t)kShares * kRows * (HD + kPagesPartPad) * sizeof(float);
-  static constexpr size_t kLds = (kRing * kStage > (int)kStates ? kRing * kStage : kStates) + 16;
+  static constexpr size_t kStates = kShares > 1 ? (size_t)kShares * kRows * (HD + kPagesPartPad) * sizeof(float) : 0;
+  static constexpr size_t kLds = kRing * kStage > (int)kStates ? kRing * kStage : kStates;
 };
 
 template <int HD, int WR>
@@ -594,7 +596,10 @@ __global__ __launch_bounds__(kPagesWaves * 64, 2) void pages_attend_wide_kernel(
     if (at >= AHEAD) return words[min(at, kPagesMaskWords - 1)];
     uint32_t word = early[0];
 #pragma unroll
-    for (int i = 1; i < AHEAD; ++i) word = at == i ? early[i] : word;
+    for (int i = 1; i < AHEAD; ++i) {
+      word = at == i ? early[i] : word;
+      asm("" : "+v"(word));  // (or the compiler makes a table of them in memory)
+    }
     return word;
   };
 
@@ -746,17 +751,35 @@ __global__ __launch_bounds__(kPagesWaves * 64, 2) void pages_attend_wide_kernel(
       step(at, tok0);
     }
   }
-  __syncthreads();
-  float(*states)[ROWS][ROW] = (float(*)[ROWS][ROW])lds;
+  if constexpr (SHARES == 1) {  // the rows are the wave's own
+    l = fold32(l, LaneAdd{});
+    if (!tr.live) return;
+    const float inv = wk.inverse(l);
+    uint16_t* out = (uint16_t*)a.out + tr.row * a.out_stride + tr.head * HD;
+    float* dst = wk.all + ((size_t)it.split * ROWS + wr * 32 + r) * ROW;
 #pragma unroll
-  for (int j = 0; j < HT; ++j)
+    for (int j = 0; j < HT; ++j)
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      *(f32x4*)&states[share][wr * 32 + r][j * 32 + 8 * u + 4 * h] = f32x4{acc[0][j][4 * u], acc[0][j][4 * u + 1], acc[0][j][4 * u + 2], acc[0][j][4 * u + 3]};
-  l = fold32(l, LaneAdd{});
-  if (h == 0) *(f32x2*)&states[share][wr * 32 + r][HD] = f32x2{partial_maximum(maximum(), l), l};
-  __syncthreads();
-  join_waves<HD, uint16_t, ROWS, SHARES, kPagesWaves * 64>(wk, it.split, true, lds, tid);
+      for (int u = 0; u < 4; ++u) {
+        const f32x4 o = f32x4{acc[0][j][4 * u], acc[0][j][4 * u + 1], acc[0][j][4 * u + 2], acc[0][j][4 * u + 3]};
+        const int e0 = j * 32 + 8 * u + 4 * h;
+        if (wk.nsplit == 1) wk.store(out + e0, o * inv);
+        else *(f32x4*)(dst + e0) = o;
+      }
+    if (wk.nsplit > 1 && h == 0) *(f32x2*)(dst + HD) = f32x2{partial_maximum(maximum(), l), l};
+  } else {
+    __syncthreads();
+    float(*states)[ROWS][ROW] = (float(*)[ROWS][ROW])lds;
+#pragma unroll
+    for (int j = 0; j < HT; ++j)
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        *(f32x4*)&states[share][wr * 32 + r][j * 32 + 8 * u + 4 * h] = f32x4{acc[0][j][4 * u], acc[0][j][4 * u + 1], acc[0][j][4 * u + 2], acc[0][j][4 * u + 3]};
+    l = fold32(l, LaneAdd{});
+    if (h == 0) *(f32x2*)&states[share][wr * 32 + r][HD] = f32x2{partial_maximum(maximum(), l), l};
+    __syncthreads();
+    join_waves<HD, uint16_t, ROWS, SHARES, kPagesWaves * 64>(wk, it.split, true, lds, tid);
+  }
 }
 
 // The splits of a workgroup's rows joined apart: workgroup (cache head, some rows of a client's group), a thread 4 channels of a row.
@@ -830,10 +853,14 @@ static hipError_t launch_wide(const PagesAttend& a, const PagesClients& c, hipSt
 hipError_t launch_pages_attend(const PagesAttend& a, const PagesLaunch& l, hipStream_t st) {
   auto go = [&](auto hd) {
     constexpr int HD = decltype(hd)::value;
-    if (a.dtype == PIPESD_F32) return l.tiles == 1 ? launch_few<HD, float, 1>(a, l.c, st) : launch_few<HD, float, 2>(a, l.c, st);
+    if (a.dtype == PIPESD_F32) {
+      if (l.tiles == 1) return launch_few<HD, float, 1>(a, l.c, st);
+      return l.tiles == 2 ? launch_few<HD, float, 2>(a, l.c, st) : hipErrorInvalidValue;
+    }
     if (l.tiles == 1) return launch_few<HD, uint16_t, 1>(a, l.c, st);
     if (l.tiles == 2) return launch_few<HD, uint16_t, 2>(a, l.c, st);
-    return l.tiles == 4 ? launch_wide<HD, 2>(a, l.c, st) : launch_wide<HD, 4>(a, l.c, st);
+    if (l.tiles == 4) return launch_wide<HD, 2>(a, l.c, st);
+    return l.tiles == 8 ? launch_wide<HD, 4>(a, l.c, st) : hipErrorInvalidValue;
   };
   return a.view.head_dim == 128 ? go(std::integral_constant<int, 128>{}) : go(std::integral_constant<int, 64>{});
 }

@@ -64,14 +64,24 @@ struct PagesCost {
 constexpr int kPagesTiles[4] = {1, 2, 4, 8};
 constexpr PagesCost pages_cost(int tiles, int dtype, int head_dim) {
   const double part = head_dim == 128 ? 1 : tiles <= 2 ? 0.5 : 0.75;  // (the weights' instructions do not get fewer)
-  if (dtype == PIPESD_F32) return tiles == 1 ? PagesCost{128, 1, 2.9 * part, 2.9 * part, 4} : PagesCost{128, 1, tiles == 2 ? 4.5 * part : 1e30, 4.5 * part, 4};
-  if (tiles == 1) return PagesCost{256, 1, 2.25 * part, 2.25 * part, 4};
-  if (tiles == 2) return PagesCost{256, 1, 2.35 * part, 2.35 * part, 4};
-  if (tiles == 4) return PagesCost{64, 2, 1.4 * part, 1.87 * part, 5};
-  return PagesCost{32, 2, 1 * part, 1.75 * part, 5};
+  if (dtype == PIPESD_F32) return tiles == 1 ? PagesCost{128, 1, 2.9 * part, 2.9 * part, 3.5} : tiles == 2 ? PagesCost{128, 1, 4.5 * part, 4.5 * part, 5.5} : PagesCost{32, 1, 1e30, 1e30, 5};
+  if (tiles == 1) return PagesCost{256, 1, 2.25 * part, 2.25 * part, 3.5};
+  if (tiles == 2) return PagesCost{256, 1, 2.35 * part, 2.35 * part, 5.5};
+  if (tiles == 4) return PagesCost{64, 2, 1.3 * part, 1.7 * part, 5};
+  return PagesCost{32, 2, 0.92 * part, 1.6 * part, 5};
 }
-constexpr double kPagesLaunchUs = 2, kPagesJoinUs = 3.5, kPagesApartUs = 4;  // a launch; what joins splits, in the last workgroup and apart
+constexpr double kPagesLaunchUs = 2, kPagesJoinUs = 3, kPagesApartUs = 4;  // a launch; what joins splits, in the last workgroup and apart
 constexpr double kPagesMemory = 5.8e6, kPagesCaches = 12e6, kPagesParts = 2.9e6;  // bytes a us: of the cache once, again, of partial rows (there and back)
+
+// Whether splits of `rows` query rows of a cache head are joined by a kernel of their own: always those of more than two tiles, others
+// where the last workgroup would go to memory 4 times and more.
+inline bool pages_apart(int tiles, int64_t rows, int nsplit, int head_dim) {
+  if (nsplit == 1 || tiles > 2) return nsplit > 1;
+  const int threads = kPagesFewWaves * 64, tasks = (int)std::min<int64_t>(rows, tiles * 16) * (head_dim / 4);
+  int shares = 1;
+  while (2 * shares * tasks <= threads) shares *= 2;
+  return (tasks + threads - 1) / threads * ((nsplit + 8 * shares - 1) / (8 * shares)) > 3;
+}
 
 // The launches of a pass, at most kPagesPerLaunch clients in one.  All splits are as long, some part of the longest context: as short
 // as pays for what begins and joins them, in rounds of workgroups that fill the device.  So what a row's sums are cut into depends on
@@ -101,15 +111,17 @@ inline PagesNeeds pages_plan(const PagesClient* cl, int n, int dtype, int head_d
       last = s;
       int64_t groups = 0, cut_groups = 0;
       double cut_rows = 0;
+      bool apart = false;
       for (int i = 0; i < n; ++i) {
         if (cl[i].n_rows == 0) continue;
         const int nsplit = pages_splits(cl[i].len, s);
         const int64_t g = (int64_t)n_kv_heads * sets(cl[i], tiles) * nsplit;
         groups += g;
         if (nsplit > 1) cut_groups += g, cut_rows += (double)n_q_heads * cl[i].n_rows * nsplit;
+        apart = apart || pages_apart(tiles, (int64_t)group * cl[i].n_rows, nsplit, head_dim);
       }
       if (cut_groups > kPagesCutRounds * room) break;  // (more still with shorter ones)
-      const double walk = (std::min<int64_t>(s + kPagesSplitSlack, longest) + cost.tokens - 1) / cost.tokens;
+      const double walk = std::max(1., (double)std::min<int64_t>(s + kPagesSplitSlack, longest) / cost.tokens);
       // rounds of workgroups that all walk as far as the longest does, or all walks shared evenly and then one of the longest
       const int64_t rounds = groups / room, left = groups % room;
       const double by_rounds = rounds * (walk * cost.full + cost.begin) + (left ? walk * (left <= n_cu ? cost.alone : cost.full) + cost.begin : 0);
@@ -117,7 +129,7 @@ inline PagesNeeds pages_plan(const PagesClient* cl, int n, int dtype, int head_d
       const double walks = n > 1 ? std::min(by_rounds, by_tokens) : by_rounds;
       // (work and memory that take as long do not quite run side by side)
       const double t = kPagesLaunchUs + sqrt(sqrt(walks * walks * walks * walks + memory * memory * memory * memory)) +
-                       (s >= cut ? 0 : tiles <= 2 ? kPagesJoinUs : kPagesApartUs + cut_rows * row_bytes / kPagesParts);
+                       (s >= cut ? 0 : !apart ? kPagesJoinUs : kPagesApartUs + cut_rows * row_bytes / kPagesParts);
       if (t < time) time = t, *span = s;
     }
     return time;
@@ -134,13 +146,8 @@ inline PagesNeeds pages_plan(const PagesClient* cl, int n, int dtype, int head_d
   auto flush = [&] {
     if (l.c.n == 0) return;
     for (int i = l.c.n; i < kPagesPerLaunch; ++i) l.c.first[i] = l.c.items;
-    for (int i = 0; i < l.c.n; ++i) {  // (where the last workgroup would go to memory 4 times and more)
-      const int threads = kPagesFewWaves * 64, tasks = std::min(group * l.c.n_rows[i], tiles * 16) * (head_dim / 4);
-      int shares = 1;
-      while (2 * shares * tasks <= threads) shares *= 2;
-      const int turns = (tasks + threads - 1) / threads * ((l.c.nsplit[i] + 8 * shares - 1) / (8 * shares));
-      if (l.c.nsplit[i] > 1 && (tiles > 2 || turns > 3)) l.c.apart = 1;
-    }
+    for (int i = 0; i < l.c.n; ++i)
+      if (pages_apart(tiles, (int64_t)group * l.c.n_rows[i], l.c.nsplit[i], head_dim)) l.c.apart = 1;
     out.push_back(l);
     l = PagesLaunch{};
   };
