@@ -787,8 +787,8 @@ template <int HD, typename T, int ROWS>
 __global__ __launch_bounds__(256) void pages_join_kernel(PagesAttend a, PagesClients clients) {
   constexpr int TPR = HD / 4, ROW = HD + kPagesPartPad, PER = 256 / TPR, BATCH = 8;
   int group = blockIdx.y / (ROWS / PER), ci = 0;
-  while (group >= clients.groups[ci]) group -= clients.groups[ci++];
-  if (clients.nsplit[ci] == 1) return;
+  for (; clients.nsplit[ci] == 1 || group >= clients.groups[ci]; ++ci)
+    if (clients.nsplit[ci] > 1) group -= clients.groups[ci];
   const PagesWork<HD, T> wk(a, clients, PagesItem{ci, group, 0}, blockIdx.x, ROWS / 16);
   const int mr = blockIdx.y % (ROWS / PER) * PER + threadIdx.x / TPR, e0 = threadIdx.x % TPR * 4;
   if (wk.first_row + mr >= wk.group_rows) return;
@@ -834,9 +834,7 @@ static hipError_t launch(Kernel kernel, Join join, std::atomic<uint64_t>& allowe
   kernel<<<dim3(a.view.n_kv_heads, c.items), waves * 64, bytes, st>>>(a, c);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !c.apart) return e;
-  int groups = 0;
-  for (int i = 0; i < c.n; ++i) groups += c.groups[i];
-  join<<<dim3(a.view.n_kv_heads, groups * (rows / (1024 / a.view.head_dim))), 256, 0, st>>>(a, c);
+  join<<<dim3(a.view.n_kv_heads, pages_join_groups(c) * (rows / (1024 / a.view.head_dim))), 256, 0, st>>>(a, c);
   return hipGetLastError();
 }
 template <int HD, typename T, int TILES>

@@ -83,6 +83,14 @@ inline bool pages_apart(int tiles, int64_t rows, int nsplit, int head_dim) {
   return (tasks + threads - 1) / threads * ((nsplit + 8 * shares - 1) / (8 * shares)) > 3;
 }
 
+// Groups of clients whose splits are joined (kPagesCutRounds bounds them, however many others there are).
+inline int pages_join_groups(const PagesClients& c) {
+  int groups = 0;
+  for (int i = 0; i < c.n; ++i)
+    if (c.nsplit[i] > 1) groups += c.groups[i];
+  return groups;
+}
+
 // The launches of a pass, at most kPagesPerLaunch clients in one.  All splits are as long, some part of the longest context: as short
 // as pays for what begins and joins them, in rounds of workgroups that fill the device.  So what a row's sums are cut into depends on
 // the pass, not on timing.

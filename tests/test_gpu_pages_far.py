@@ -110,3 +110,24 @@ def test_a_pass_allocates_nothing_on_the_device():
     pg.compact(list(range(16)), [1000] * 16, [[0, 1, 5]] * 16)
     torch.cuda.synchronize()
     assert torch.cuda.mem_get_info()[0] == free
+
+
+@gpu
+def test_one_long_context_among_many_rows():
+    """Only its rows have splits to join."""
+    nq, nkv, dim, n, rows, clients = 128, 1, 64, 40000, 700, 12
+    pg = nav.PageCache(shape_of(nq, nkv, dim), 1 + clients, n // 16 + 2 + clients * 45)
+    k, v = (random_rows(n + 1, nkv, dim, "bf16", j) for j in (1, 2))
+    fill(pg, 0, 5, k, v, n, chunk=20000)
+    ks, vs = (random_rows(rows, nkv, dim, "bf16", j) for j in (3, 4))
+    q = random_rows(1 + clients * rows, nq, dim, "bf16", 5)
+    others = [c for c in range(1 + clients) if c != 5]
+    pg.extend(others[:7] + [5] + others[7:], [rows] * 7 + [1] + [rows] * (clients - 7))
+    at = 7 * rows
+    put = lambda one, x: torch.cat([x] * 7 + [one[n:]] + [x] * (clients - 7)).cuda()
+    pg.append(0, put(k, ks), put(v, vs))
+    out = pg.attend(0, q.cuda())
+    check_rows(out[at:at + 1], *reference(q[at:at + 1], k, v, sees(n, [-1])), "bf16")
+    for first in (0, at + 1):
+        part = slice(first, first + rows)
+        check_rows(out[part], *reference(q[part], ks, vs, sees(0, list(range(-1, rows - 1)))), "bf16")

@@ -63,6 +63,7 @@ static void check(int nq, int nkv, int hd, int dtype, int n_cu, const std::vecto
     }
     for (int j = l.c.n; j < kPagesPerLaunch; ++j) CHECK(l.c.first[j] == l.c.items);
     CHECK(item == l.c.items);
+    CHECK(!l.c.apart || (int64_t)pages_join_groups(l.c) * (l.tiles * 16 / (1024 / hd)) <= 65535);  // (a grid's workgroups in y)
   }
   for (size_t i = 0; i < cl.size(); ++i) CHECK(seen[i] == (cl[i].n_rows > 0));
   CHECK(need.part_tiles == parts && need.counters == counters);
@@ -101,6 +102,12 @@ int main(int argc, char** argv) {
       row += rows;
     }
     check(h[0], h[1], r() % 2 ? 128 : 64, r() % 2 ? PIPESD_BF16 : PIPESD_F32, r() % 5 ? 256 : pick(1, 304), cl);
+  }
+  {  // one long context among many rows that are not cut
+    std::vector<PagesClient> cl;
+    for (int c = 0; c < 32; ++c) cl.push_back(PagesClient{c, c ? kPagesMaxRows : 1, c * kPagesMaxRows, c ? kPagesMaxRows : 100000, c});
+    for (int dtype : {PIPESD_F32, PIPESD_BF16})
+      for (int hd : {64, 128}) check(256, 1, hd, dtype, 256, cl);
   }
   for (int rows : {1, kPagesMaxRows}) {
     std::vector<PagesClient> cl;
