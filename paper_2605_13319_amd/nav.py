@@ -859,7 +859,11 @@ def _rows_of(x, name: str, device: int, shape=None):
     apart, step = x.stride()
     if step != 1 and size[1] > 1:
         raise ValueError(f"{name}: tokens side by side, not {step} apart")
-    return size, max(apart, size[1])
+    if size[0] < 2:  # (a row alone may have any)
+        return size, size[1]
+    if apart < size[1]:
+        raise ValueError(f"{name}: rows {apart} elements apart share {size[1]} tokens (an expanded tensor?)")
+    return size, apart
 
 
 def tree_accept(p, q, tokens: Sequence[int], parents: Sequence[int], uniforms, rows: Optional[Sequence[int]] = None, distinct: bool = False,

@@ -202,3 +202,16 @@ def test_a_recorded_decision():
         want = expect([(p2, q2, tokens, parents, u)], True)
         assert result.cpu().tolist() == want
         assert nav.tree_accept(pd, qd, tokens, parents, u, distinct=True, workspace=other).cpu().tolist() == want
+
+
+@gpu
+def test_rows_that_share_memory_are_refused():
+    one = torch.full((1, 50), 0.02, device="cuda")
+    p = one.expand(3, 50).contiguous()
+    shared = torch.rand(200, device="cuda").as_strided((3, 50), (40, 1))
+    for bad in (one.expand(3, 50), shared):
+        with pytest.raises(ValueError, match="apart"):
+            nav.tree_accept(bad, None, [0, 1, 2], [-1, 0, 0], None)
+        with pytest.raises(ValueError, match="apart"):
+            nav.tree_accept(p, bad, [0, 1, 2], [-1, 0, 0], [0.5] * 3)
+    assert nav.tree_accept(one.as_strided((1, 50), (1, 1)), None, [0], [-1], None).tolist() == [[0, 0]]
