@@ -782,29 +782,32 @@ __global__ __launch_bounds__(kPagesWaves * 64, 2) void pages_attend_wide_kernel(
   }
 }
 
-// The splits of a workgroup's rows joined apart: workgroup (cache head, some rows of a client's group), a thread 4 channels of a row.
+// The splits of a workgroup's rows joined apart: workgroup (cache head, some rows of a client's group), a thread 4 channels of a row and of
+// every `shares`-th split, 8 at a time.  The shares of a task are joined through LDS in order.
 template <int HD, typename T, int ROWS>
-__global__ __launch_bounds__(256) void pages_join_kernel(PagesAttend a, PagesClients clients) {
+__global__ __launch_bounds__(256) void pages_join_kernel(PagesAttend a, PagesClients clients, PagesJoin join) {
   constexpr int TPR = HD / 4, ROW = HD + kPagesPartPad, PER = 256 / TPR, BATCH = 8;
-  int group = blockIdx.y / (ROWS / PER), ci = 0;
-  for (; clients.nsplit[ci] == 1 || group >= clients.groups[ci]; ++ci)
-    if (clients.nsplit[ci] > 1) group -= clients.groups[ci];
-  const PagesWork<HD, T> wk(a, clients, PagesItem{ci, group, 0}, blockIdx.x, ROWS / 16);
-  const int mr = blockIdx.y % (ROWS / PER) * PER + threadIdx.x / TPR, e0 = threadIdx.x % TPR * 4;
-  if (wk.first_row + mr >= wk.group_rows) return;
-  const float* from = wk.all + (size_t)mr * ROW;
+  __shared__ float joined[256][6];
+  const int tid = threadIdx.x, lane = tid & 63, shares = 1 << join.log_shares, per = PER >> join.log_shares, wgs = ROWS / per;
+  const int ci = __builtin_amdgcn_readfirstlane(__popcll(__ballot(lane < clients.n && (int)blockIdx.y >= join.first[lane & (kPagesPerLaunch - 1)])) - 1);
+  const int at = blockIdx.y - join.first[ci];
+  const PagesWork<HD, T> wk(a, clients, PagesItem{ci, at / wgs, 0}, blockIdx.x, ROWS / 16);
+  const int row0 = at % wgs * per, share = tid / (per * TPR), mr = row0 + tid / TPR % per, e0 = tid % TPR * 4;
+  if (wk.first_row + row0 >= wk.group_rows) return;  // (whole workgroup)
+  const float* from = wk.all + (size_t)min(mr, wk.group_rows - wk.first_row - 1) * ROW;
   float m = -INFINITY, l = 0.f;
   f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
-  for (int s0 = 0; s0 < wk.nsplit; s0 += BATCH) {
+  for (int s0 = share; s0 < wk.nsplit; s0 += BATCH * shares) {
     f32x4 ob[BATCH];
     f32x2 ml[BATCH];
 #pragma unroll
     for (int j = 0; j < BATCH; ++j) {
-      const float* p = from + (size_t)min(s0 + j, wk.nsplit - 1) * (ROWS * ROW);
+      const int sp = s0 + j * shares;
+      const float* p = from + (size_t)min(sp, wk.nsplit - 1) * (ROWS * ROW);
       ob[j] = *(const f32x4*)(p + e0);
       ml[j] = *(const f32x2*)(p + HD);
-      if (s0 + j >= wk.nsplit) ml[j].x = -INFINITY;
+      if (sp >= wk.nsplit) ml[j].x = -INFINITY;
     }
     float top = m;
 #pragma unroll
@@ -821,6 +824,24 @@ __global__ __launch_bounds__(256) void pages_join_kernel(PagesAttend a, PagesCli
     }
     m = top;
   }
+  if (shares > 1) {
+    float* x = joined[tid];
+    x[0] = o[0], x[1] = o[1], x[2] = o[2], x[3] = o[3], x[4] = l, x[5] = m;
+    __syncthreads();
+    if (share > 0) return;
+    float top = m;
+    for (int sh = 1; sh < shares; ++sh) top = fmaxf(top, joined[sh * per * TPR + tid][5]);
+    const float own = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+    l *= own;
+    o *= own;
+    for (int sh = 1; sh < shares; ++sh) {
+      const float* y = joined[sh * per * TPR + tid];
+      if (y[5] == -INFINITY) continue;
+      const float sw = __builtin_amdgcn_exp2f(y[5] - top);
+      l += y[4] * sw;
+      o += f32x4{y[0], y[1], y[2], y[3]} * sw;
+    }
+  }
   wk.finish(wk.first_row + mr, e0, o, l);
 }
 
@@ -834,7 +855,9 @@ static hipError_t launch(Kernel kernel, Join join, std::atomic<uint64_t>& allowe
   kernel<<<dim3(a.view.n_kv_heads, c.items), waves * 64, bytes, st>>>(a, c);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !c.apart) return e;
-  join<<<dim3(a.view.n_kv_heads, pages_join_groups(c) * (rows / (1024 / a.view.head_dim))), 256, 0, st>>>(a, c);
+  PagesJoin how;
+  const int wgs = pages_join_plan(c, rows, a.view.head_dim, &how);
+  join<<<dim3(a.view.n_kv_heads, wgs), 256, 0, st>>>(a, c, how);
   return hipGetLastError();
 }
 template <int HD, typename T, int TILES>

@@ -56,7 +56,8 @@ struct PagesNeeds {
 // What workgroups of one, two, four and eight tiles take: tokens of a step, its time in us on a compute unit by itself and with as many
 // workgroups as one holds, and what a workgroup's beginning and end add.  One or two tiles ask for as much as a compute unit gets (58 GB/s).
 // Fitted to 8 heads of 128: 4096 tokens more of one client 36, 38, 78 and 107 us with 8 workgroups; 64 rows behind 32768 75 us with
-// 512 of four tiles, 71 with 512 of eight, 78 with 256 of them.
+// 512 of four tiles, 70 with 512 of eight, 78 with 256 of them.  Heads of 64: 9 rows behind 65536, 43.5 us where two groups of two tiles
+// walk them, 39 with one of four.
 struct PagesCost {
   int tokens, resident;
   double alone, full, begin;
@@ -71,7 +72,7 @@ constexpr PagesCost pages_cost(int tiles, int dtype, int head_dim) {
   return PagesCost{32, 2, 0.92 * part, 1.6 * part, 5};
 }
 constexpr double kPagesLaunchUs = 2, kPagesJoinUs = 3, kPagesApartUs = 4;  // a launch; what joins splits, in the last workgroup and apart
-constexpr double kPagesMemory = 5.8e6, kPagesCaches = 12e6, kPagesParts = 2.9e6;  // bytes a us: of the cache once, again, of partial rows (there and back)
+constexpr double kPagesMemory = 5.8e6, kPagesCaches = 12e6, kPagesParts = 3.5e6;  // bytes a us: of the cache once, again, of partial rows (there and back)
 
 // Whether splits of `rows` query rows of a cache head are joined by a kernel of their own: always those of more than two tiles, others
 // where the last workgroup would go to memory 4 times and more.
@@ -83,12 +84,24 @@ inline bool pages_apart(int tiles, int64_t rows, int nsplit, int head_dim) {
   return (tasks + threads - 1) / threads * ((nsplit + 8 * shares - 1) / (8 * shares)) > 3;
 }
 
-// Groups of clients whose splits are joined (kPagesCutRounds bounds them, however many others there are).
-inline int pages_join_groups(const PagesClients& c) {
-  int groups = 0;
+// What joins splits apart: workgroups per cache head, for the groups that have splits (kPagesCutRounds bounds them, however many others
+// there are), and threads that share the splits of 4 channels: more while one would go to memory again, up to 8, or 1024 workgroups.
+struct PagesJoin {
+  int32_t log_shares;
+  int32_t first[kPagesPerLaunch];  // workgroup of a client (of one without splits: the next one's)
+};
+inline int pages_join_plan(const PagesClients& c, int rows, int head_dim, PagesJoin* join) {
+  int groups = 0, most = 1;
   for (int i = 0; i < c.n; ++i)
-    if (c.nsplit[i] > 1) groups += c.groups[i];
-  return groups;
+    if (c.nsplit[i] > 1) groups += c.groups[i], most = std::max(most, c.nsplit[i]);
+  int per_group = rows / (1024 / head_dim), log = 0, wgs = 0;
+  while (log < 3 && most > 8 << log && 2 * groups * per_group <= 1024) per_group *= 2, ++log;
+  join->log_shares = log;
+  for (int i = 0; i < kPagesPerLaunch; ++i) {
+    join->first[i] = wgs;
+    if (i < c.n && c.nsplit[i] > 1) wgs += c.groups[i] * per_group;
+  }
+  return wgs;
 }
 
 // The launches of a pass, at most kPagesPerLaunch clients in one.  All splits are as long, some part of the longest context: as short
@@ -111,7 +124,8 @@ inline PagesNeeds pages_plan(const PagesClient* cl, int n, int dtype, int head_d
     const int64_t room = (int64_t)cost.resident * n_cu, cut = std::max<int64_t>(1, longest - kPagesSplitSlack);
     double walked = 0, time = 1e300;  // walked: by all workgroups, tokens
     for (int i = 0; i < n; ++i) walked += (double)n_kv_heads * sets(cl[i], tiles) * cl[i].len;
-    const double memory = std::max(once * token_bytes / kPagesMemory, walked * token_bytes / kPagesCaches);
+    // (workgroups that walk the same tokens do it side by side: what the second one asks for is often not in the caches yet)
+    const double memory = std::max(once / kPagesMemory + std::min(once, walked - once) / kPagesCaches, walked / kPagesCaches) * token_bytes;
     int64_t last = 0;
     for (int halves = 2; halves <= 2 * kPagesMaxSplits; halves += halves < 16 ? 1 : 2) {  // half parts of the longest context
       const int64_t s = ((2 * cut + halves - 1) / halves + kPagesStep - 1) / kPagesStep * kPagesStep;

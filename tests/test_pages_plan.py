@@ -63,7 +63,15 @@ static void check(int nq, int nkv, int hd, int dtype, int n_cu, const std::vecto
     }
     for (int j = l.c.n; j < kPagesPerLaunch; ++j) CHECK(l.c.first[j] == l.c.items);
     CHECK(item == l.c.items);
-    CHECK(!l.c.apart || (int64_t)pages_join_groups(l.c) * (l.tiles * 16 / (1024 / hd)) <= 65535);  // (a grid's workgroups in y)
+    if (l.c.apart) {
+      PagesJoin join;
+      const int wgs = pages_join_plan(l.c, l.tiles * 16, hd, &join), per = (1024 / hd) >> join.log_shares;
+      CHECK(wgs >= 1 && wgs <= 65535 && join.log_shares >= 0 && per >= 1);  // (a grid's in y)
+      for (int j = 0; j < kPagesPerLaunch; ++j) {
+        const int next = j + 1 < kPagesPerLaunch ? join.first[j + 1] : wgs;
+        CHECK(next - join.first[j] == (j < l.c.n && l.c.nsplit[j] > 1 ? l.c.groups[j] * (l.tiles * 16 / per) : 0));
+      }
+    }
   }
   for (size_t i = 0; i < cl.size(); ++i) CHECK(seen[i] == (cl[i].n_rows > 0));
   CHECK(need.part_tiles == parts && need.counters == counters);
@@ -85,7 +93,11 @@ int main(int argc, char** argv) {
     std::vector<PagesLaunch> out;
     pages_plan(cl.data(), (int)cl.size(), atoi(argv[5]), atoi(argv[4]), atoi(argv[2]), atoi(argv[3]), 256, out);
     for (const PagesLaunch& l : out)
-      for (int j = 0; j < l.c.n; ++j) printf("%d %d\n", l.tiles, l.c.nsplit[j]);
+      for (int j = 0; j < l.c.n; ++j) {
+        PagesJoin join;
+        pages_join_plan(l.c, l.tiles * 16, atoi(argv[4]), &join);
+        printf("%d %d %d\n", l.tiles, l.c.nsplit[j], l.c.apart ? 1 << join.log_shares : 0);
+      }
     return 0;
   }
   std::mt19937 r(7);
@@ -140,6 +152,7 @@ def plan(tmp_path_factory):
 
 
 def kinds(plan, heads, dtype, before, rows):
+    """(tiles, splits, threads that share a task of the join apart; 0: none is) of every client."""
     text = plan("kind", *heads, 0 if dtype == "f32" else 1, *[x for b, r in zip(before, rows) for x in (b + r, r)])
     return [tuple(map(int, line.split())) for line in text.splitlines()]
 
@@ -150,7 +163,7 @@ def test_passes_are_covered_once(plan):
 
 def test_what_passes_are_given_to(plan):
     """(tiles of a workgroup, splits) where the kinds have been measured: the fastest, or within 5 % of it (us)."""
-    tiles = lambda *a: {t for t, _ in kinds(plan, *a)}
+    tiles = lambda *a: {t for t, _, _ in kinds(plan, *a)}
     h8, h64 = (32, 8, 128), (32, 8, 64)
     assert tiles(h8, "bf16", [2048], [9]) == {1}      # 11.0; 14.6 with two, 14.9 with four, 15.5 with eight
     assert tiles(h8, "bf16", [4096], [1]) == {1}      # 11.6; 13.1, 16.3, 17.0
@@ -160,7 +173,19 @@ def test_what_passes_are_given_to(plan):
     assert tiles(h8, "bf16", [32768], [64]) <= {4, 8}  # 77 and 72; 155 with one, 94 with two
     assert tiles(h8, "bf16", [2048], [1024]) == {4}   # 77; 203, 112, 95
     assert tiles(h8, "f32", [8000], [1]) == {1}       # 19; 25 with two
-    assert kinds(plan, h64, "bf16", [200], [1]) == [(1, 1)]
+    assert kinds(plan, h64, "bf16", [200], [1]) == [(1, 1, 0)]
+
+
+def test_passes_that_are_joined_apart(plan):
+    """The cases of test_gpu_pages_join.py reach one to eight threads that share a task, and clients without splits beside them."""
+    one = [kinds(plan, (16, 2, dim), "bf16", [before], [rows])[0] for before in (6000, 20011, 70000) for rows in (5, 16, 33, 64, 128) for dim in (64, 128)]
+    one += [kinds(plan, (8, 1, dim), "bf16", [100], [2048])[0] for dim in (64, 128)]
+    assert {shares for _, _, shares in one} == {0, 1, 2, 4, 8}
+    assert {tiles for tiles, _, shares in one if shares > 0} == {1, 2, 4, 8}
+    before, rows = [0, 30000, 17, 4000, 200, 9000, 1], [3, 9, 40, 17, 1, 33, 64]
+    for dtype in ("bf16", "f32"):
+        ragged = kinds(plan, (16, 2, 128), dtype, before, rows)
+        assert {s > 0 for _, _, s in ragged} == {True} and min(n for _, n, _ in ragged) == 1 and max(n for _, n, _ in ragged) > 8
 
 
 def test_no_early_read_of_matrix_core_results(tmp_path):
