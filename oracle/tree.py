@@ -34,7 +34,9 @@ def nested_rule(p, q, tokens: Sequence[int], distinct: bool):
 
 
 def left_of(p: np.ndarray, q: np.ndarray, a) -> np.ndarray:
-    """max(0, p - a q) in fp32, the difference rounded once (products of fp32 numbers are exact in fp64)."""
+    """max(0, p - a q) in fp32, the difference rounded once.  (Products of fp32 numbers are exact in fp64, their difference from p mostly is: where
+    it needs more than 53 bits, and what is cut off decides a tie of the rounding to fp32, one operation on fp32 numbers is off by an ulp,
+    about once in 2^28.)"""
     return np.maximum(F32(0), (p.astype(np.float64) - np.float64(a) * q.astype(np.float64)).astype(F32))
 
 

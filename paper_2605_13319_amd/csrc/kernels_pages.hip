@@ -39,7 +39,8 @@ struct BlockPieces {  // blocks in pieces
 // into one that others hold as well
 // ------------------------------------------------------------------------------------------------
 // The first workgroups have a tree each, a thread a row, which walks up to the root (the very first also writes the entries); the others the
-// keys or values of a block and layer.
+// keys or values of a block and layer.  One launch, because it is nothing but latency: 1.3 us for entries and trees, 3.5 with 15 blocks of
+// two layers copied beside them.
 __global__ __launch_bounds__(kPagesTreeRows) void pages_begin_kernel(BlockPieces pool, PagesBegin b, int32_t* table, uint32_t* masks) {
   __shared__ int parent[kPagesTreeRows];
   __shared__ uint32_t bits[kPagesTreeRows][kPagesMaskWords];
@@ -92,7 +93,10 @@ static void by_type(int dtype, int head_dim, F go) {
 }
 
 // ------------------------------------------------------------------------------------------------
-// store and read: a workgroup has a block of a head.  Keys lie as the rows do; values go through LDS to lie token beside token.
+// store and read: a workgroup has a block of a head.  Keys lie as the rows do; values go through LDS to lie token beside token, which is
+// how the attention's products take them: turned once here and not in every pass.  Stores of some rows are latency (the table, then the
+// rows with what the block holds): 3.7 to 4.1 us.  Long ones are bound by memory: 131071 rows of 8 heads of 128 stored 193 us, 5.6 TB/s both
+// ways; 6200 tokens of four layers read 30.8 us, 6.5 TB/s.
 // ------------------------------------------------------------------------------------------------
 template <typename T, int HD>
 struct Piece {  // 16 bytes
@@ -214,7 +218,9 @@ hipError_t launch_pages_read(int dtype, const KvView& v, int layer0, int n_layer
 
 // ------------------------------------------------------------------------------------------------
 // move: workgroup (16 bytes of a token's key, or as many channels of its value; layer and head), a thread a token.  What the tokens of
-// a launch are moved over may be other tokens of it: all are read first.
+// a launch are moved over may be other tokens of it: all are read first, by the workgroup that writes them, and no wait between
+// workgroups is needed.  Values cost a load of 2 bytes a channel: made for the rows of trees (some tens of tokens of four layers 4.4 us, latency);
+// moves of thousands of tokens run at 0.9 TB/s.
 // ------------------------------------------------------------------------------------------------
 template <int HD, typename T>
 __global__ __launch_bounds__(kPagesMovesPerLaunch) void pages_move_kernel(KvView v, int layer0, PagesMoves m) {
@@ -267,7 +273,8 @@ hipError_t launch_pages_move(int dtype, const KvView& v, int n_layers, const Pag
 }
 
 // ------------------------------------------------------------------------------------------------
-// copy: workgroup (block, its keys or values of a layer)
+// copy: workgroup (block, its keys or values of a layer), four pieces of 16 bytes a thread at a time.  65536 tokens of four layers (8 heads
+// of 128, 2.1 GB both ways) 400 us, 5.4 TB/s: a large copy.
 // ------------------------------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void pages_copy_kernel(BlockPieces pool, int part0, PagesMoves m) {
   pool.copy(part0 + blockIdx.y, m.from[blockIdx.x], m.to[blockIdx.x]);

@@ -6,9 +6,10 @@
 // bf16: keys, values and queries are operands as they are; weights are cut into two bf16 numbers, 16 bits where results have 8, as in
 // the other attentions of the library.  fp32: products of fp32 numbers on the matrix cores.  Maxima and sums are fp32.
 //
-// One pass over the cache: keys and values go from memory into the registers that the products take them from and are not kept.  The
-// waves of a workgroup share its tiles of query rows, take every fourth 32 tokens of the span and join their states through LDS at the
-// end; a context that is cut into splits is joined by the last workgroup that arrives, or by a kernel of its own.
+// One pass over the cache with a running maximum and sum.  Few rows are bound by what a compute unit can ask for: keys and values go
+// from memory into the registers that the products take them from, each wave has tokens of its own, and the waves' states are joined
+// through LDS at the end.  Many rows are bound by products and exponentials: waves have rows of their own over tokens in LDS.  A context
+// that is cut into splits is joined by the last workgroup that arrives, or by a kernel of its own.
 #include "device_attend.h"
 #include "device_dma.h"
 #include "lds_limit.h"
@@ -190,6 +191,12 @@ __device__ __forceinline__ bool not_finite(T x) {
 //         first four are row 4 g + .. of the first 16 x 16 product of keys, the others of the second: row r of product tt is token
 //         8 (r / 4) + 4 tt + r % 4.
 //   fp32  tokens 4 g .. + 3; a load of 4 channels of a key, or 4 tokens of a value, serves 4 products (k = 4).
+// What bounds it: a compute unit gets 58 GB/s, with 4 waves asking as with 8: 256 tokens of 128 bf16 channels take 2.25 us for one tile
+// and 2.35 for two, so two are taken where there are the rows.  fp32 products take as long as their operands' way: 128 tokens of 128
+// channels 2.9 us for one tile, 4.5 for two, 3.4 of them products.  fp32 numbers cut into three bf16 pieces, for six bf16 products
+// instead of one, took 4.2 in registers and 5.7 through LDS.
+// 8 heads of 128, bf16: behind 2048 tokens 1 row 9.3 us, 9 rows 10.9, 64 rows 16.5 (launch, table, keys, 3 us to join: trips to memory
+// one after the other); fp32: 1 row behind 2048 12.8, behind 131071 183 (5.9 TB/s).
 // LDS: states [wave][row], later what joins the splits; then the queries that registers do not hold; a word
 template <int HD, int TILES>
 constexpr size_t state_floats() { return (size_t)TILES * kPagesFewWaves * 16 * (HD + kPagesPartPad); }
@@ -507,6 +514,11 @@ __global__ __launch_bounds__(kPagesFewWaves * 64, 2) void pages_attend_kernel(Pa
 // Layout of a product: operand lane (r, h) holds row (column) r, k = 8 h .. + 7; the result's register 4 u + i holds row 8 u + 4 h + i
 // of column r.  Row 8 a + 4 h + i of a block's keys is its token 8 h + 4 a + i: then a lane has the scores of 8 neighbouring tokens
 // of each block, which is what a product takes of their weights, and of a channel's values with one read.
+// What bounds it: a wave's chain of products, maximum, exponentials, products, 0.92 us for a stage of 32 tokens of 128 channels with one
+// workgroup on a compute unit, 1.6 with two, where products alone take 0.32 each; scores of the next stage multiplied under this one's
+// weights took 1.16.  Where 64 rows are enough, two waves over 32 other tokens take 1.3 and 1.7 us for 64 tokens.  8 heads of 128:
+// 2048 rows behind 6144 347 us, 0.69 PFLOP/s, 1.04 with the weights' second product (a large bf16 product reaches 1.21); 9 rows
+// behind 131071 102 us, 5.3 TB/s with the join.
 // LDS of 32 tokens: [block][keys, values], as the pool has them but for the order of 16-byte pieces, in which lanes that read together
 // find theirs in different banks: a key's piece c at c ^ (token), a channel's half u of its tokens at u ^ (channel / 4 % 2).
 template <int HD, int WR>
@@ -783,7 +795,8 @@ __global__ __launch_bounds__(kPagesWaves * 64, 2) void pages_attend_wide_kernel(
 }
 
 // The splits of a workgroup's rows joined apart: workgroup (cache head, some rows of a client's group), a thread 4 channels of a row and of
-// every `shares`-th split, 8 at a time.  The shares of a task are joined through LDS in order.
+// every `shares`-th split, 8 at a time.  The shares of a task are joined through LDS in order.  Bound by trips to memory, 1.7 us for 8 splits:
+// 64 splits of 36 rows (8 heads of 128) 6.9 us with eight threads a task, 13 to 15 with one; 2 to 4 splits 6.3.
 template <int HD, typename T, int ROWS>
 __global__ __launch_bounds__(256) void pages_join_kernel(PagesAttend a, PagesClients clients, PagesJoin join) {
   constexpr int TPR = HD / 4, ROW = HD + kPagesPartPad, PER = 256 / TPR, BATCH = 8;
