@@ -120,10 +120,17 @@ inline PagesNeeds pages_plan(const PagesClient* cl, int n, int dtype, int head_d
   if (longest == 0) return need;
   const double token_bytes = 2. * head_dim * (dtype == PIPESD_F32 ? 4 : 2), row_bytes = 4. * (head_dim + kPagesPartPad);
   auto best = [&](int tiles, int64_t* span) {
-    const PagesCost cost = pages_cost(tiles, dtype, head_dim);
+    PagesCost cost = pages_cost(tiles, dtype, head_dim);
     const int64_t room = (int64_t)cost.resident * n_cu, cut = std::max<int64_t>(1, longest - kPagesSplitSlack);
-    double walked = 0, time = 1e300;  // walked: by all workgroups, tokens
-    for (int i = 0; i < n; ++i) walked += (double)n_kv_heads * sets(cl[i], tiles) * cl[i].len;
+    double walked = 0, worked = 0, time = 1e300;  // tokens: walked by all workgroups, and by waves that have rows
+    for (int i = 0; i < n; ++i) {
+      const double tokens = (double)n_kv_heads * cl[i].len;
+      walked += tokens * sets(cl[i], tiles);
+      worked += tokens * (((int64_t)group * cl[i].n_rows + 31) / 32 * 2) / tiles;
+    }
+    // (waves of eight tiles that have no rows leave the compute unit to others: 16 clients of up to 33 rows behind up to 4096 49 us, 52 with
+    // four tiles)
+    if (tiles == 8) cost.full = cost.alone + (cost.full - cost.alone) * worked / walked;
     // (workgroups that walk the same tokens do it side by side: what the second one asks for is often not in the caches yet)
     const double memory = std::max(once / kPagesMemory + std::min(once, walked - once) / kPagesCaches, walked / kPagesCaches) * token_bytes;
     int64_t last = 0;
