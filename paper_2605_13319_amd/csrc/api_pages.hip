@@ -13,7 +13,7 @@ namespace {
 struct PagesSeq {
   int32_t len = 0;
   std::vector<int32_t> blocks;  // in token order
-  std::vector<int32_t> sent;    // what the device has in the client's block table
+  std::vector<int32_t> sent;    // what the device has in the client's block table; -1: not known (all of them, where a launch failed)
   bool in_pass = false;         // of the pass that append and attend work on
 };
 template <class F>
@@ -239,6 +239,7 @@ static int pages_not_recorded(hipStream_t st) {
 // whether the device lacks entries of a client's block table, from one on
 static bool pages_unsent(const PagesSeq& s, int32_t from) {
   if (s.sent.size() < s.blocks.size()) return true;
+  if (!s.blocks.empty() && s.sent[0] < 0) return true;
   return !std::equal(s.blocks.begin() + from, s.blocks.end(), s.sent.begin() + from);
 }
 
@@ -255,34 +256,39 @@ static int pages_send(pipesd_pages* pg, int32_t n, const int32_t* seq_ids, const
     b.n = b.trees = b.own = rows = 0;
     return PIPESD_OK;
   };
-  for (size_t i = 0; own && i < pg->from.size(); ++i) {
-    if (b.own == kPagesOwnPerLaunch)
-      if (int rc = flush()) return rc;
-    b.own_from[b.own] = pg->from[i];
-    b.own_to[b.own++] = pg->to[i];
-  }
-  for (int32_t k = 0; k < n; ++k) {
-    PagesSeq& s = pg->seqs[seq_ids[k]];
-    const int32_t off = pg->table_off(seq_ids[k]), nb = (int32_t)s.blocks.size();
-    if ((int32_t)s.sent.size() < nb) s.sent.resize(nb, -1);
-    for (int32_t i = from ? from[k] : 0; i < nb; ++i) {
-      if (s.sent[i] == s.blocks[i]) continue;
-      if (b.n == kPagesEntriesPerLaunch)
+  auto all = [&]() -> int {
+    for (size_t i = 0; own && i < pg->from.size(); ++i) {
+      if (b.own == kPagesOwnPerLaunch)
         if (int rc = flush()) return rc;
-      b.at[b.n] = off + i;
-      b.v[b.n++] = s.sent[i] = s.blocks[i];
+      b.own_from[b.own] = pg->from[i];
+      b.own_to[b.own++] = pg->to[i];
     }
-  }
-  for (size_t i = 0; parents && i < trees.size(); ++i) {
-    const PagesClient& c = trees[i];
-    if (b.trees == kPagesPerLaunch || rows + c.n_rows > kPagesParentsPerLaunch)
-      if (int rc = flush()) return rc;
-    b.row_off[b.trees] = c.row_off;
-    b.n_rows[b.trees] = c.n_rows;
-    b.before[b.trees++] = c.len - c.n_rows;
-    for (int32_t r = 0; r < c.n_rows; ++r) b.parent[rows++] = (int16_t)parents[c.row_off + r];
-  }
-  return flush();
+    for (int32_t k = 0; k < n; ++k) {
+      PagesSeq& s = pg->seqs[seq_ids[k]];
+      const int32_t off = pg->table_off(seq_ids[k]), nb = (int32_t)s.blocks.size();
+      if ((int32_t)s.sent.size() < nb) s.sent.resize(nb, -1);
+      for (int32_t i = from && nb > 0 && s.sent[0] >= 0 ? from[k] : 0; i < nb; ++i) {
+        if (s.sent[i] == s.blocks[i]) continue;
+        if (b.n == kPagesEntriesPerLaunch)
+          if (int rc = flush()) return rc;
+        b.at[b.n] = off + i;
+        b.v[b.n++] = s.sent[i] = s.blocks[i];
+      }
+    }
+    for (size_t i = 0; parents && i < trees.size(); ++i) {
+      const PagesClient& c = trees[i];
+      if (b.trees == kPagesPerLaunch || rows + c.n_rows > kPagesParentsPerLaunch)
+        if (int rc = flush()) return rc;
+      b.row_off[b.trees] = c.row_off;
+      b.n_rows[b.trees] = c.n_rows;
+      b.before[b.trees++] = c.len - c.n_rows;
+      for (int32_t r = 0; r < c.n_rows; ++r) b.parent[rows++] = (int16_t)parents[c.row_off + r];
+    }
+    return flush();
+  };
+  const int rc = all();
+  for (int32_t k = 0; rc && k < n; ++k) std::fill(pg->seqs[seq_ids[k]].sent.begin(), pg->seqs[seq_ids[k]].sent.end(), -1);
+  return rc;
 }
 
 // tokens (block * 16 + place) or blocks from pg->from to pg->to, some per launch
@@ -406,7 +412,6 @@ extern "C" int pipesd_pages_extend(pipesd_pages* pg, int32_t n_seqs, const int32
     if (pg->pool && (rc = launch())) {
       for (int32_t i = n_seqs - 1; i >= 0; --i) {  // (backwards: the free blocks' order too is as it was)
         PagesSeq& s = pg->seqs[seq_ids[i]];
-        if ((int32_t)s.sent.size() > had[i]) std::fill(s.sent.begin() + had[i], s.sent.end(), -1);
         pages_release(pg, s, s.len - n_new[i]);
         if (own[i] >= 0) {
           pg->drop(s.blocks.back());
@@ -556,6 +561,7 @@ extern "C" int pipesd_pages_fork(pipesd_pages* pg, int32_t n_seqs, const int32_t
       t.len = len ? len[i] : s.len;
       t.blocks.assign(s.blocks.begin(), s.blocks.begin() + pages_blocks(t.len));
       for (int32_t b : t.blocks) ++pg->users[b];
+      if (pg->pool && pages_unsent(s, 0) && !rc) rc = pages_send(pg, 1, &seq_ids[i], nullptr, false, {}, nullptr, st);
       if (pg->pool && pages_unsent(t, 0)) {
         f.from[f.n] = pg->table_off(seq_ids[i]);
         f.to[f.n] = pg->table_off(into[i]);
@@ -615,10 +621,7 @@ extern "C" int pipesd_pages_copy(pipesd_pages* pg, int32_t n_seqs, const int32_t
     if (!pg->pool) return PIPESD_OK;
     int rc = pages_moves(pg, true, st);
     if (!rc) rc = pages_send(pg, n_seqs, into, nullptr, false, {}, nullptr, st);
-    if (rc) {
-      pages_clear_targets(pg, n_seqs, into);
-      for (int32_t i = 0; i < n_seqs; ++i) std::fill(pg->seqs[into[i]].sent.begin(), pg->seqs[into[i]].sent.end(), -1);
-    }
+    if (rc) pages_clear_targets(pg, n_seqs, into);
     return rc;
   });
 }
@@ -716,7 +719,6 @@ extern "C" int pipesd_pages_compact(pipesd_pages* pg, int32_t n_seqs, const int3
           pg->drop(s.blocks[replaced[j].at]);
           s.blocks[replaced[j].at] = replaced[j].blk;
           ++pg->users[replaced[j].blk];
-          std::fill(s.sent.begin(), s.sent.end(), -1);
         }
         return rc;
       }

@@ -1,0 +1,133 @@
+"""Several things at once: caches and decisions on two streams, the most clients that a pass may have and clients without new rows among them,
+a whole layer and a decision over a large vocabulary recorded in one graph."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2605_13319_amd import nav
+from tests.test_gpu_pages import check_rows, fill, make_cache, random_rows, random_tree, reference, sees, shape_of
+from tests.test_gpu_tree_accept import expect, make_case
+
+gpu = pytest.mark.gpu
+
+
+@gpu
+def test_two_caches_and_decisions_on_two_streams():
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    sides = []
+    for i, st in enumerate(streams):
+        n, rows = (5000, 12) if i == 0 else (90, 40)
+        dtype = ("bf16", "f32")[i]
+        with torch.cuda.stream(st):
+            pg = make_cache(shape_of(8, 2, 128, dtype), 2, 700)
+            k, v = (random_rows(n + rows, 2, 128, dtype, 10 * i + j) for j in (1, 2))
+            q = random_rows(rows, 8, 128, dtype, 10 * i + 3)
+            fill(pg, 0, 0, k, v, n)
+            case = make_case(50 + i, 40, 30011 if i == 0 else 900, 3, True)
+            sides.append((pg, k, v, q, n, random_tree(rows, i), case, nav.tree_workspace(1, 40), [x.cuda() for x in (k[n:], v[n:], q)],
+                          [torch.from_numpy(x).cuda() for x in case[:2]]))
+    torch.cuda.synchronize()
+    outs = [[], []]
+    for _ in range(6):
+        for i, st in enumerate(streams):
+            pg, k, v, q, n, tree, case, work, (nk, nv, qd), (p, dq) = sides[i]
+            with torch.cuda.stream(st):
+                pg.extend([0], [len(tree)], tree)
+                pg.append(0, nk, nv)
+                outs[i].append((pg.attend(0, qd), nav.tree_accept(p, dq, *case[2:], distinct=True, workspace=work)))
+                pg.truncate([0], [n])
+    torch.cuda.synchronize()
+    for i in range(2):
+        pg, k, v, q, n, tree, case, *_ = sides[i]
+        want, decided = reference(q, k, v, sees(n, tree)), expect([case], True)
+        for rows, got in outs[i]:
+            check_rows(rows, *want, ("bf16", "f32")[i])
+            assert got.cpu().tolist() == decided
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_256_clients_some_without_new_rows(dtype):
+    nq, nkv, dim = 8, 2, 64
+    rng = np.random.default_rng(4)
+    before = rng.integers(0, 70, 256).tolist()
+    rows = [0 if c % 3 == 1 else int(x) for c, x in enumerate(rng.integers(1, 7, 256))]
+    ks, vs = ([random_rows(b + r, nkv, dim, dtype, 2 * c + j) for c, (b, r) in enumerate(zip(before, rows))] for j in (0, 1))
+    pg = make_cache(shape_of(nq, nkv, dim, dtype), 256, 256 * 6)
+    pg.extend(list(range(256)), before)
+    pg.append(0, torch.cat([k[:b] for k, b in zip(ks, before)]).cuda(), torch.cat([v[:b] for v, b in zip(vs, before)]).cuda())
+    order = rng.permutation(256).tolist()
+    trees = {c: random_tree(rows[c], c) if rows[c] else [] for c in order}
+    pg.extend(order, [rows[c] for c in order], [p for c in order for p in trees[c]])
+    pg.append(0, torch.cat([ks[c][before[c]:] for c in order]).cuda(), torch.cat([vs[c][before[c]:] for c in order]).cuda())
+    q = random_rows(sum(rows), nq, dim, dtype, 999)
+    out = pg.attend(0, q.cuda())
+    at = 0
+    for c in order:
+        if rows[c]:
+            check_rows(out[at:at + rows[c]], *reference(q[at:at + rows[c]], ks[c], vs[c], sees(before[c], trees[c])), dtype)
+        at += rows[c]
+    assert [pg.length(c) for c in range(256)] == [b + r for b, r in zip(before, rows)]
+
+
+@gpu
+def test_a_layer_and_a_decision_in_one_graph():
+    nq, nkv, dim, before, rows = 16, 4, 128, 2500, 30
+    pg = make_cache(shape_of(nq, nkv, dim), 2, 300)
+    k, v = (random_rows(before, nkv, dim, "bf16", j) for j in (1, 2))
+    fill(pg, 0, 0, k, v, before)
+    tree = random_tree(rows, 4)
+    case = make_case(61, rows, 20021, 4, True)
+    nk, nv, q = (random_rows(rows, h, dim, "bf16", j).cuda() for h, j in ((nkv, 3), (nkv, 4), (nq, 5)))
+    p, dq = (torch.from_numpy(x).cuda() for x in case[:2])
+    out, work = torch.empty_like(q), nav.tree_workspace(1, rows)
+    result = torch.zeros(1, rows + 1, dtype=torch.int32, device="cuda")
+    pg.extend([0], [rows], tree)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pg.append(0, nk, nv)
+        pg.attend(0, q, out=out)
+        nav.tree_accept(p, dq, *case[2:], distinct=True, result=result, workspace=work)
+        back = pg.read([0], [before - 20], [20 + rows])
+    for seed in range(5):
+        for x, h, j in ((nk, nkv, 3), (nv, nkv, 4), (q, nq, 5)):
+            x.copy_(random_rows(rows, h, dim, "bf16", 100 * seed + j))
+        other = make_case(70 + seed, rows, 20021, 4, True)
+        p.copy_(torch.from_numpy(other[0]))
+        dq.copy_(torch.from_numpy(other[1]))
+        graph.replay()
+        torch.cuda.synchronize()
+        kk, vv = torch.cat([k, nk.cpu()]), torch.cat([v, nv.cpu()])
+        check_rows(out, *reference(q.cpu(), kk, vv, sees(before, tree)), "bf16")
+        assert result.cpu().tolist() == expect([(other[0], other[1], *case[2:])], True)
+        for got, want in zip(back, (kk, vv)):
+            assert torch.equal(got[0].cpu(), want[before - 20:])
+        # eager decisions and appends between the replays, to the same rows
+        assert nav.tree_accept(p, dq, *case[2:], distinct=True).cpu().tolist() == result.cpu().tolist()
+        pg.append(0, nv, nk)
+
+
+@gpu
+def test_a_refused_recording_changes_nothing():
+    """Blocks that the device knows may come again while a stream is recorded, also behind a call that was refused for others."""
+    nq, nkv, dim = 4, 1, 64
+    pg = make_cache(shape_of(nq, nkv, dim), 1, 60)
+    k, v = (random_rows(100, nkv, dim, "bf16", j) for j in (1, 2))
+    q = random_rows(40, nq, dim, "bf16", 3).cuda()
+    fill(pg, 0, 0, k, v, 60)
+    pg.truncate([0], [20])
+    nk, nv, out = k[60:].cuda(), v[60:].cuda(), torch.empty_like(q)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for rows in (500, 60):  # (scratch has to grow; blocks that the client did not have)
+            with pytest.raises(nav.PipesdError) as e:
+                pg.extend([0], [rows])
+            assert e.value.status == nav.ESTATE and pg.length(0) == 20 and pg.free_blocks() == 58
+        pg.extend([0], [40])  # (20 .. 59: the blocks of before)
+        pg.append(0, nk, nv)
+        pg.attend(0, q, out=out)
+    for _ in range(2):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        check_rows(out, *reference(q.cpu(), torch.cat([k[:20], k[60:]]), torch.cat([v[:20], v[60:]]), sees(20, list(range(-1, 39)))), "bf16")
