@@ -217,43 +217,43 @@ hipError_t launch_pages_read(int dtype, const KvView& v, int layer0, int n_layer
 }
 
 // ------------------------------------------------------------------------------------------------
-// move: workgroup (16 bytes of a token's key, or as many channels of its value; layer and head), a thread a token.  What the tokens of
-// a launch are moved over may be other tokens of it: all are read first, by the workgroup that writes them, and no wait between
-// workgroups is needed.  Values cost a load of 2 bytes a channel: made for the rows of trees (some tens of tokens of four layers 4.4 us, latency);
-// moves of thousands of tokens run at 0.9 TB/s.
+// move: workgroup (a cache line of a token's key, or some channels of its value; layer and head), for keys eight threads a token, for
+// values one.  What the tokens of a launch are moved over may be other tokens of it: all are read first, by the workgroup that writes
+// them, and no wait between workgroups is needed.  Made for the rows of trees: some tens of tokens of four layers 4 us (latency), 448
+// tokens of four layers and 8 heads of 64 6.0 us, 1.2 TB/s; with 16 bytes of a key to a workgroup, which eight chiplets' caches then fetch
+// and write apart, 15 to 20.
 // ------------------------------------------------------------------------------------------------
 template <int HD, typename T>
 __global__ __launch_bounds__(kPagesMovesPerLaunch) void pages_move_kernel(KvView v, int layer0, PagesMoves m) {
   typedef Piece<T, HD> P;
+  constexpr int SLICE = 8, SLICES = P::kOfRow / SLICE;  // pieces of a key that a workgroup has: a cache line
   const int tid = threadIdx.x, layer = layer0 + blockIdx.y / v.n_kv_heads, kvh = blockIdx.y % v.n_kv_heads;
-  const bool values = blockIdx.x >= P::kOfRow;
-  const int e = (blockIdx.x % P::kOfRow) * P::kElems;
-  T* part = (T*)v.pool + (int64_t)layer * v.layer_stride + (values ? v.v_offset : 0) + (int64_t)kvh * kBlockTokens * HD;
-  auto at = [&](int place) {
-    const int t = place % kBlockTokens;
-    return part + (int64_t)(place / kBlockTokens) * v.block_elems + (values ? e * kBlockTokens + t : t * HD + e);
-  };
-  uint4 x = make_uint4(0, 0, 0, 0);
-  T* xs = (T*)&x;
-  if (tid < m.n) {
-    const T* from = at(m.from[tid]);
-    if (values) {
+  T* keys = (T*)v.pool + (int64_t)layer * v.layer_stride + (int64_t)kvh * kBlockTokens * HD;
+  if (blockIdx.x < SLICES) {
+    const int e = (blockIdx.x * SLICE + tid % SLICE) * P::kElems, per = blockDim.x / SLICE;
+    auto at = [&](int place) { return (piece_t*)(keys + (int64_t)(place / kBlockTokens) * v.block_elems + place % kBlockTokens * HD + e); };
+    piece_t x[SLICE];
 #pragma unroll
-      for (int j = 0; j < P::kElems; ++j) xs[j] = from[j * kBlockTokens];
-    } else {
-      x = *(const uint4*)from;
-    }
+    for (int j = 0; j < SLICE; ++j) x[j] = *at(m.from[min(j * per + tid / SLICE, m.n - 1)]);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < SLICE; ++j)
+      if (j * per + tid / SLICE < m.n) *at(m.to[j * per + tid / SLICE]) = x[j];
+    return;
   }
+  const int e = (blockIdx.x - SLICES) * P::kElems;
+  auto at = [&](int place) { return keys + v.v_offset + (int64_t)(place / kBlockTokens) * v.block_elems + e * kBlockTokens + place % kBlockTokens; };
+  T xs[P::kElems];
+  const T* from = at(m.from[min(tid, m.n - 1)]);
+#pragma unroll
+  for (int j = 0; j < P::kElems; ++j) xs[j] = from[j * kBlockTokens];
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (tid < m.n) {
     T* to = at(m.to[tid]);
-    if (values) {
 #pragma unroll
-      for (int j = 0; j < P::kElems; ++j) to[j * kBlockTokens] = xs[j];
-    } else {
-      *(uint4*)to = x;
-    }
+    for (int j = 0; j < P::kElems; ++j) to[j * kBlockTokens] = xs[j];
   }
 }
 
@@ -264,7 +264,7 @@ hipError_t launch_pages_move(int dtype, const KvView& v, int n_layers, const Pag
     by_type(dtype, v.head_dim, [&](auto hd, auto t) {
       typedef decltype(t) T;
       constexpr int HD = decltype(hd)::value;
-      pages_move_kernel<HD, T><<<dim3(2 * Piece<T, HD>::kOfRow, nl * v.n_kv_heads), (m.n + 63) / 64 * 64, 0, st>>>(v, l0, m);
+      pages_move_kernel<HD, T><<<dim3(Piece<T, HD>::kOfRow / 8 + Piece<T, HD>::kOfRow, nl * v.n_kv_heads), (m.n + 63) / 64 * 64, 0, st>>>(v, l0, m);
     });
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

@@ -818,8 +818,11 @@ class PageCache:
         (ids, n, _ids, _), (f, m, _first, _) = _numbers(seqs), _numbers(first)
         if n != m or n != len(kept):
             raise ValueError(f"{n} clients, {m} beginnings, {len(kept)} lists of tokens")
-        (c, _nc, _count, _), (k, _nk, _kept, _) = _numbers([len(x) for x in kept]), _numbers([int(t) for x in kept for t in x])
-        self._call(_lib.pipesd_pages_compact, "pipesd_pages_compact", n, ids, f, c, k)
+        c, _nc, _count, _ = _numbers([len(x) for x in kept])
+        tokens = array("i")  # (what is no integer it refuses)
+        for x in kept:
+            tokens += array("i", x)
+        self._call(_lib.pipesd_pages_compact, "pipesd_pages_compact", n, ids, f, c, tokens.buffer_info()[0] if tokens else None)
 
     def truncate(self, seqs: Sequence[int], lengths: Sequence[int]) -> None:
         """Forget the clients' tokens from lengths[i] on."""

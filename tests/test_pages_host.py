@@ -5,6 +5,7 @@ import random
 
 import numpy as np
 import pytest
+import torch
 
 from paper_2605_13319_amd import inputs as I
 from paper_2605_13319_amd import nav
@@ -259,3 +260,17 @@ def test_decisions_that_are_refused():
         nav.tree_accept(torch.zeros(3, 4), None, [0, 0, 0], [-1, 0, 0], None)
     with pytest.raises(ValueError):
         nav.tree_accept(torch.zeros(3, 4), None, [0, 0], [-1, 0, 0], None)
+
+
+def test_kept_tokens_of_any_kind_of_integers():
+    pg = cache(2, 20)
+    for kept in ([1, 4, 7], (1, 4, 7), range(1, 8, 3), np.array([1, 4, 7]), np.array([1, 4, 7], dtype=np.int16), torch.tensor([1, 4, 7])):
+        pg.extend([0], [30])
+        pg.compact([0], [3], [kept])
+        assert pg.length(0) == 6
+        pg.truncate([0], [0])
+    pg.extend([0], [30])
+    for kept in ([1.0, 4.0], np.array([1.0]), ["1"], [2 ** 40]):
+        with pytest.raises((TypeError, OverflowError)):
+            pg.compact([0], [3], [kept])
+    assert pg.length(0) == 30
