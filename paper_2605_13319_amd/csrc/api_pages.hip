@@ -619,8 +619,9 @@ extern "C" int pipesd_pages_copy(pipesd_pages* pg, int32_t n_seqs, const int32_t
       }
     }
     if (!pg->pool) return PIPESD_OK;
-    int rc = pages_moves(pg, true, st);
-    if (!rc) rc = pages_send(pg, n_seqs, into, nullptr, false, {}, nullptr, st);
+    const bool few = pg->from.size() <= (size_t)kPagesOwnPerLaunch;  // (go with the tables' entries: a launch less)
+    int rc = few ? PIPESD_OK : pages_moves(pg, true, st);
+    if (!rc) rc = pages_send(pg, n_seqs, into, nullptr, few, {}, nullptr, st);
     if (rc) pages_clear_targets(pg, n_seqs, into);
     return rc;
   });
