@@ -131,3 +131,26 @@ def test_a_refused_recording_changes_nothing():
         graph.replay()
         torch.cuda.synchronize()
         check_rows(out, *reference(q.cpu(), torch.cat([k[:20], k[60:]]), torch.cat([v[:20], v[60:]]), sees(20, list(range(-1, 39)))), "bf16")
+
+
+@gpu
+@pytest.mark.parametrize("tokens", [1, 16, 500, 512, 513, 9001])
+def test_copies_of_few_and_many_blocks(tokens):
+    """Into clients that held something else; the source goes on by itself."""
+    pg = make_cache(shape_of(4, 2, 64, layers=3), 4, 4 * 600)
+    rows = [[random_rows(tokens + 20, 2, 64, "bf16", 10 * layer + j) for j in (1, 2)] for layer in range(3)]
+    old = random_rows(300, 2, 64, "bf16", 77).cuda()
+    pg.extend([2, 1], [150, 150])
+    pg.append(0, old, old)
+    pg.extend([0], [tokens])
+    for layer in range(3):
+        pg.append(layer, *(x[:tokens].cuda() for x in rows[layer]))
+    pg.copy([0, 0], [1, 2], [tokens, tokens - tokens // 3])
+    pg.extend([0], [20])
+    for layer in range(3):
+        pg.append(layer, *(x[tokens:].cuda() for x in rows[layer]))
+    pg.fork([0], [3])
+    for client, n in ((0, tokens + 20), (1, tokens), (2, tokens - tokens // 3), (3, tokens + 20)):
+        for j, got in enumerate(pg.read([client], [0], [n])):
+            assert torch.equal(got.cpu(), torch.stack([rows[layer][j][:n] for layer in range(3)]))
+    assert [pg.seq_blocks(c) for c in (1, 2)] == [-(-tokens // 16), -(-(tokens - tokens // 3) // 16)]
