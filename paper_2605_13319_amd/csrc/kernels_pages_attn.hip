@@ -383,16 +383,17 @@ __global__ __launch_bounds__(kPagesFewWaves * 64, 2) void pages_attend_kernel(Pa
         if ((who >> (16 * gg)) & 0xffff) apart_of |= 1u << (NX * gg + x);
     }
   };
-  // those values, for the rows that see them (LDS: the wave's own states, which nobody reads before its walk has ended)
+  // those values, for the rows that see them (LDS: the wave's own states, which nobody reads before its walk has ended; the block is asked
+  // for: the lanes may have the next 64 steps' already)
   float* scratch = lds + (size_t)w * TILES * 16 * ROW;
-  auto add_apart = [&](Running<HT>& r, const float (&p)[NX], uint32_t sees, uint32_t apart_of, int i) {
+  auto add_apart = [&](Running<HT>& r, const float (&p)[NX], uint32_t sees, uint32_t apart_of, int tok0) {
 #pragma unroll
     for (int x = 0; x < NX; ++x) scratch[c * 33 + token_of(x)] = p[x];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll 1
     for (uint32_t left = apart_of; left != 0; left &= left - 1) {
       const int tok = __builtin_ctz(left);
-      const T* from = (const T*)(block_base(i, NB == 2 ? tok >> 4 : 0) + a.view.v_offset * (int)sizeof(T)) + (tok & 15);
+      const T* from = (const T*)head_base + (int64_t)wk.table[(tok0 + tok) / kBlockTokens] * a.view.block_elems + a.view.v_offset + tok % kBlockTokens;
       const float pt = scratch[c * 33 + tok];
 #pragma unroll
       for (int j = 0; j < HT; ++j)
@@ -480,7 +481,7 @@ __global__ __launch_bounds__(kPagesFewWaves * 64, 2) void pages_attend_kernel(Pa
     settle(run);
     if (apart_of != 0) {
 #pragma unroll
-      for (int t = 0; t < TILES; ++t) add_apart(run[t], p[t], sees[t], apart_of, i);
+      for (int t = 0; t < TILES; ++t) add_apart(run[t], p[t], sees[t], apart_of, tok0);
     }
     request_values(i + SETS, SET);
   };
