@@ -517,6 +517,8 @@ int pipesd_pages_append(pipesd_pages *pg, int32_t layer, const void *k, int64_t 
  * q . k / sqrt(head_dim) over the tokens that a row sees, query head g reads head g / (n_q_heads / n_kv_heads) of the cache.  out may be q
  * itself (the same address and stride); otherwise no row of out shares memory with one of q (columns of one wider matrix do not).
  * What tokens hold that a row does not see, infinities and NaN among them, does not reach it.
+ * An infinity among the values that it sees is one of its result's channel: NaN beside NaN or one of the other sign, or where its token's
+ * weight vanishes in fp32.
  * A row's result depends on what it sees alone.  Into how many pieces a context is cut, and so the order of sums, goes by the
  * lengths and numbers of rows of all clients of the pass; the same pass gives the same bits.
  * EINVAL: also out over q where that is not allowed; ESTATE: no pass that can attend, no pool. */

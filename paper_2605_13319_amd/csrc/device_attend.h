@@ -83,6 +83,14 @@ struct Running {
     for (int j = 0; j < HT; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   __device__ __forceinline__ float maximum() const { return moves == -INFINITY ? -INFINITY : -neg_m; }
+  __device__ __forceinline__ bool no_number() const {
+    bool none = false;
+#pragma unroll
+    for (int j = 0; j < HT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) none |= __builtin_isunordered(acc[j][e], acc[j][e + 1]);
+    return none;
+  }
   // The maximum moves only when a score passes it by 2^8 (any scale will do for fp32 sums: most steps then need no exchange
   // between lanes and no rescaling).
   __device__ __forceinline__ void move_to(float top, float c1) {  // all lanes

@@ -184,6 +184,84 @@ __device__ __forceinline__ bool not_finite(T x) {
   else return (x & 0x7f80u) == 0x7f80u;
 }
 
+// In a step that all rows see, an infinity is multiplied with both pieces of a bf16 model's weights, which is no number where the lower one
+// is zero or of the other sign.  A wave whose sums are none comes by here with its states: such a sum holds a value that is not finite, so
+// it is what all of those give, weighted once more.  (Lane (c, g): row c, channels 16 j + 4 g + ...  What it needs it finds again: registers
+// that the walk kept for it would cost the walk more.)
+template <int HD, int TILES>
+__device__ __forceinline__ void weigh_infinities(const PagesAttend& a, const PagesClients& clients, float* state, int first, int step, int end) {
+  constexpr int HT = HD / 16, ROW = HD + kPagesPartPad;
+  int lane = threadIdx.x & 63, item = blockIdx.y, kvh = blockIdx.x;
+  asm volatile("" : "+v"(lane), "+s"(item), "+s"(kvh));  // (found again, not kept)
+  const PagesWork<HD, uint16_t> wk(a, clients, find_item(clients, item, lane), kvh, TILES);
+  const int c = lane & 15, g = lane >> 4, before = wk.len - wk.n_rows;
+  const KvView& view = wk.a.view;
+  const uint16_t* keys = (const uint16_t*)view.pool + (int64_t)wk.a.layer * view.layer_stride + (int64_t)wk.kvh * kBlockTokens * HD;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll 1
+  for (int t = 0; t < TILES; ++t) {
+    const TileRow tr = wk.row(wk.first_row + t * 16 + c);
+    const uint16_t* q = (const uint16_t*)wk.a.q + tr.row * wk.a.q_stride + tr.head * HD;
+    float* mine = state + (t * 16 + c) * ROW;
+    const float m = mine[HD];
+    f32x4 o[HT];
+#pragma unroll
+    for (int j = 0; j < HT; ++j) {
+      o[j] = *(f32x4*)(mine + j * 16 + 4 * g);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[j][e] = o[j][e] != o[j][e] ? 0.f : o[j][e];
+    }
+#pragma unroll 1
+    for (int tok0 = first; tok0 < end; tok0 += step) {
+      // bit x: a channel of token tok0 + x (lane: channels 16 j + c, tokens 8 g .. + 7)
+      uint32_t odd = 0;
+      const int piece = tok0 + 8 * g;
+      const uint16_t* v = keys + view.v_offset + (int64_t)wk.table[piece < wk.len ? piece / kBlockTokens : 0] * view.block_elems + c * kBlockTokens + piece % kBlockTokens;
+#pragma unroll 1
+      for (int j = 0; j < HT; ++j) {
+        const uint4 x = *(const uint4*)(v + j * 16 * kBlockTokens);
+        const uint16_t* xs = (const uint16_t*)&x;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) odd |= not_finite(xs[i]) && piece + i < wk.len ? 1u << (8 * g + i) : 0u;
+      }
+      uint32_t sees = ~0u;
+      if (wk.a.masks == nullptr) {
+        const int n = before + 1 + tr.row - wk.row_off - tok0;
+        sees = n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
+      } else if (tok0 >= (before & ~31)) {
+        sees = wk.a.masks[(size_t)tr.row * kPagesMaskWords + min((tok0 - (before & ~31)) >> 5, kPagesMaskWords - 1)];
+      }
+#pragma unroll 1
+      for (int tok = 0; tok < 32; ++tok) {
+        if (__ballot((odd >> tok) & 1) == 0) continue;
+        const uint16_t* key = keys + (int64_t)wk.table[(tok0 + tok) / kBlockTokens] * view.block_elems;
+        const uint16_t* val = key + view.v_offset + (tok0 + tok) % kBlockTokens;
+        key += (tok0 + tok) % kBlockTokens * HD;
+        float score = 0.f;
+#pragma unroll
+        for (int i = 0; i < HD / 32; ++i) {
+          const k4u32x4 x = *(const k4u32x4*)(q + g * (HD / 4) + i * 8), y = *(const k4u32x4*)(key + g * (HD / 4) + i * 8);
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            score = fmaf(__uint_as_float(x[d] << 16), __uint_as_float(y[d] << 16), score);
+            score = fmaf(__uint_as_float(x[d] & 0xffff0000u), __uint_as_float(y[d] & 0xffff0000u), score);
+          }
+        }
+        const float p = __builtin_amdgcn_exp2f(fmaf(fold_groups(score, LaneAdd{}), attend_scale<HD>(), -m));
+#pragma unroll
+        for (int j = 0; j < HT; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint16_t x = val[(j * 16 + 4 * g + e) * kBlockTokens];
+            if (not_finite(x) && ((sees >> tok) & 1)) o[j][e] += p * bf16_bits_to_f32(x);
+          }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < HT; ++j) *(f32x4*)(mine + j * 16 + 4 * g) = o[j];
+  }
+}
+
 // ---- few rows: waves share one or two tiles of 16 ----
 // Eight waves take every eighth step of the span, 32 tokens of bf16 numbers or 16 of fp32 ones.  Of a step a lane (c, g) has the scores of
 // query row c with 8 or 4 tokens:
@@ -292,9 +370,8 @@ __global__ __launch_bounds__(kPagesFewWaves * 64, 2) void pages_attend_kernel(Pa
   // used until they are.
   k4u32x4 k[SETS][NB][NK], v[SETS][NV];
   const char* head_base = (const char*)((const T*)a.view.pool + (int64_t)a.layer * a.view.layer_stride + (int64_t)kvh * kBlockTokens * HD);
-  auto block_base = [&](int i, int tt) {
-    return head_base + (int64_t)__builtin_amdgcn_readlane(step_blk[tt], i & 63) * a.view.block_elems * (int)sizeof(T);
-  };
+  auto at_block = [&](int blk) { return head_base + (int64_t)blk * a.view.block_elems * (int)sizeof(T); };
+  auto block_base = [&](int i, int tt) { return at_block(__builtin_amdgcn_readlane(step_blk[tt], i & 63)); };
   auto request_keys = [&](int i, int set) {
     if (i >= nsteps) return;
     if (i > 0 && (i & 63) == 0) load_blocks(i);
@@ -393,7 +470,7 @@ __global__ __launch_bounds__(kPagesFewWaves * 64, 2) void pages_attend_kernel(Pa
 #pragma unroll 1
     for (uint32_t left = apart_of; left != 0; left &= left - 1) {
       const int tok = __builtin_ctz(left);
-      const T* from = (const T*)head_base + (int64_t)wk.table[(tok0 + tok) / kBlockTokens] * a.view.block_elems + a.view.v_offset + tok % kBlockTokens;
+      const T* from = (const T*)(at_block(wk.table[(unsigned)(tok0 + tok) / kBlockTokens]) + a.view.v_offset * (int)sizeof(T)) + tok % kBlockTokens;
       const float pt = scratch[c * 33 + tok];
 #pragma unroll
       for (int j = 0; j < HT; ++j)
@@ -491,7 +568,9 @@ __global__ __launch_bounds__(kPagesFewWaves * 64, 2) void pages_attend_kernel(Pa
     if constexpr (SETS == 2)
       if (i + 1 < nsteps) step(i + 1, std::integral_constant<int, 1>{});
   }
-
+  bool none = false;  // (fp32 weights are one piece)
+#pragma unroll
+  for (int t = 0; !F32 && t < TILES; ++t) none |= run[t].no_number();
   float(*states)[TILES * 16][ROW] = (float(*)[TILES * 16][ROW])lds;  // [wave][row] its channels, its maximum and sum
 #pragma unroll
   for (int t = 0; t < TILES; ++t) {
@@ -499,6 +578,9 @@ __global__ __launch_bounds__(kPagesFewWaves * 64, 2) void pages_attend_kernel(Pa
     for (int j = 0; j < HT; ++j) *(f32x4*)&states[w][t * 16 + c][j * 16 + 4 * g] = run[t].acc[j];
     const float l = fold_groups(run[t].l, LaneAdd{});
     if (g == 0) *(f32x2*)&states[w][t * 16 + c][HD] = f32x2{partial_maximum(run[t].maximum(), l), l};
+  }
+  if constexpr (!F32) {
+    if (__builtin_expect(lo > first && __ballot(none) != 0, 0)) weigh_infinities<HD, TILES>(a, clients, &states[w][0][0], first, STEP, end);
   }
   __syncthreads();
   join_waves<HD, T, TILES * 16, WAVES, NT>(wk, it.split, clients.apart, lds, tid);
@@ -606,6 +688,7 @@ __global__ __launch_bounds__(kPagesWaves * 64, 2) void pages_attend_wide_kernel(
       return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
     }
     const int at = (tok0 - (before & ~31)) >> 5;
+    if (at < 0) return ~0u;
     if (at >= AHEAD) return words[min(at, kPagesMaskWords - 1)];
     uint32_t word = early[0];
 #pragma unroll
@@ -617,11 +700,7 @@ __global__ __launch_bounds__(kPagesWaves * 64, 2) void pages_attend_wide_kernel(
   };
 
   f32x16 acc[1][HT];
-#pragma unroll
-  for (int j = 0; j < HT; ++j)
-#pragma unroll
-    for (int x = 0; x < 16; ++x) acc[0][j][x] = 0.f;
-  float neg_m = 0.f, moves = -INFINITY, l = 0.f;  // as of a Running
+  float neg_m, moves, l;  // as of a Running
   auto maximum = [&] { return moves == -INFINITY ? -INFINITY : -neg_m; };
   const float c1 = attend_scale<HD>();
 
@@ -745,24 +824,42 @@ __global__ __launch_bounds__(kPagesWaves * 64, 2) void pages_attend_wide_kernel(
   };
 
   constexpr int PER = SHARES * COPIES;  // copies of a stage that a wave has on their way
-#pragma unroll
-  for (int i = 0; i < RING - 1; ++i)
-    if (i < nstages) copy(i);
-#pragma unroll
-  for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(q[s]));  // (here: a wait in the walk would be one for copies, which the compiler does not count)
-#pragma unroll
-  for (int i = 0; i < AHEAD; ++i) asm volatile("" : "+v"(early[i]));
 #pragma unroll 1
-  for (int i = 0; i < nstages; ++i) {
-    if (RING == 3 && i + 1 < nstages) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(PER) : "memory");
-    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();  // the stage has landed, and what the next copies go over has been read
-    if (i + RING - 1 < nstages) copy(i + RING - 1);
-    const int tok0 = span0 + i * STAGE + share * 32;
-    if (!idle && tok0 < end) {
-      const char* at = (const char*)lds + (i % RING) * W::kStage + share * 4 * W::kPart;
-      step(at, tok0);
+  for (;;) {  // once, and again where sums are no numbers behind steps that all rows see (see weigh_infinities): then such values are apart in all
+#pragma unroll
+    for (int j = 0; j < HT; ++j)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) acc[0][j][x] = 0.f;
+    neg_m = l = 0.f;
+    moves = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < RING - 1; ++i)
+      if (i < nstages) copy(i);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(q[s]));  // (here: a wait in the walk would be one for copies, which the compiler does not count)
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) asm volatile("" : "+v"(early[i]));
+#pragma unroll 1
+    for (int i = 0; i < nstages; ++i) {
+      if (RING == 3 && i + 1 < nstages) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(PER) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();  // the stage has landed, and what the next copies go over has been read
+      if (i + RING - 1 < nstages) copy(i + RING - 1);
+      const int tok0 = span0 + i * STAGE + share * 32;
+      if (!idle && tok0 < end) {
+        const char* at = (const char*)lds + (i % RING) * W::kStage + share * 4 * W::kPart;
+        step(at, tok0);
+      }
     }
+    if (lo <= span0) break;
+    bool none = false;
+#pragma unroll
+    for (int j = 0; j < HT; ++j)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) none |= acc[0][j][x] != acc[0][j][x];
+    if (!__syncthreads_or(none)) break;
+    lo = 0;
+    load_blocks(0);
   }
   if constexpr (SHARES == 1) {  // the rows are the wave's own
     l = fold32(l, LaneAdd{});

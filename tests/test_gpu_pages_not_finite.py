@@ -75,3 +75,55 @@ def test_blocks_of_the_64th_step(bad, heads, before, rows):
             v[before + row, row % 8, (5 + row) % heads[2]] = bad
 
     run(heads, "f32", before, rows, random_tree(rows, 3), spoil)
+
+
+# Passes over texts with infinities: all kinds of workgroups, with and without splits.  In bf16 every walk over one is made twice.
+TEXTS = [((8, 2, 64), 300, 1), ((8, 2, 128), 300, 17), ((32, 8, 128), 2048, 64), ((8, 2, 128), 20000, 9), ((32, 8, 64), 500, 300),
+         ((32, 8, 128), 9000, 300), ((16, 2, 64), 20000, 33)]
+
+
+def test_the_texts_reach_every_kind_of_workgroup(plan):  # noqa: F811
+    got = {(t, n > 1) for heads, before, rows in TEXTS for t, n, _ in kinds(plan, heads, "bf16", [before], [rows])}
+    assert {t for t, _ in got} == {1, 2, 4, 8} and {s for _, s in got} == {True, False}
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,before,rows", TEXTS)
+@pytest.mark.parametrize("form", ["chain", "tree"])
+def test_infinities_of_the_text(heads, before, rows, dtype, form):
+    """Anywhere in the text: infinities of either sign in channels of their own, of both signs and NaN in others."""
+    if form == "tree" and rows > 256:
+        rows = 256
+
+    def spoil(v):
+        tokens, dim = v.shape[0], v.shape[2]
+        for i, t in enumerate(range(3, before, max(11, before // 40))):
+            v[t, i % v.shape[1], i % 7] = math.inf
+            v[t + 1, 0, 8 + i % 7] = -math.inf
+            v[t + 2, -1, dim - 1 - i % 3] = math.inf if i % 2 else -math.inf
+        v[before // 2, 0, 20] = math.nan
+        assert tokens > before
+
+    run(heads, dtype, before, rows, random_tree(rows, rows) if form == "tree" else None, spoil)
+
+
+@gpu
+@pytest.mark.parametrize("heads,before,rows", TEXTS)
+def test_one_infinity_wherever_it_lies(heads, before, rows):
+    for t in (0, before // 3, before - 33, before - 1):
+        for bad in (math.inf, -math.inf):
+            run(heads, "bf16", before, rows, None, lambda v: v[t, :, 5].fill_(bad))
+
+
+def test_the_long_text_is_walked_in_more_than_64_steps(plan):  # noqa: F811
+    assert kinds(plan, (256, 256, 64), "bf16", [17000], [9]) == [(1, 1, 0)] and 17000 > 65 * 256
+
+
+@gpu
+def test_infinities_of_a_walk_of_more_than_64_steps():
+    def spoil(v):
+        for i, t in enumerate(range(62 * 256 - 40, 65 * 256, 37)):
+            v[t, i * 31 % 256, i % 64] = math.inf
+
+    run((256, 256, 64), "bf16", 17000, 9, None, spoil)
