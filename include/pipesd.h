@@ -480,8 +480,8 @@ int pipesd_kv4_seq_blocks(const pipesd_kv4 *kv, int32_t seq, int32_t *n_blocks);
  * whole multiples of 16 bytes.
  *
  * Recorded into a graph, pipesd_pages_append, pipesd_pages_attend and pipesd_pages_read do at every replay what they did for the lengths,
- * block tables and trees of the recording: replay while the clients hold the blocks that they held then, and, of a pass with
- * trees, before another pass with trees begins.  On a stream that is being recorded pipesd_pages_extend returns ESTATE and changes
+ * block tables and trees of the recording: replay while the clients hold the blocks that they held then, pipesd_pages_append while
+ * nobody else holds those of the rows, and, of a pass with trees, before another pass with trees begins.  On a stream that is being recorded pipesd_pages_extend returns ESTATE and changes
  * nothing if it would have to write block tables, trees or tokens or grow scratch (it has not where rows of a chain that were taken back
  * come again), and so do pipesd_pages_fork, pipesd_pages_copy and pipesd_pages_compact (unless no token changes its place). */
 typedef struct pipesd_pages pipesd_pages;
@@ -510,7 +510,8 @@ int pipesd_pages_destroy(pipesd_pages *pg);
 int pipesd_pages_extend(pipesd_pages *pg, int32_t n_seqs, const int32_t *seq_ids, const int32_t *n_new, const int32_t *parents, void *stream);
 
 /* Put the pass's keys and values of one layer into the cache: k, v device [rows][n_kv_heads * head_dim], rows k_stride and v_stride
- * elements apart.  ESTATE: no pass, or no pool. */
+ * elements apart.  ESTATE: no pass, or no pool, or another client has become a copy by pipesd_pages_fork that has some of the pass's
+ * rows (they are its text, too: append all layers first). */
 int pipesd_pages_append(pipesd_pages *pg, int32_t layer, const void *k, int64_t k_stride, const void *v, int64_t v_stride, void *stream);
 
 /* Attention of the pass's queries over one layer of the cache: q, out device [rows][n_q_heads * head_dim], softmax of
@@ -532,7 +533,7 @@ int pipesd_pages_read(const pipesd_pages *pg, int32_t n_seqs, const int32_t *seq
 /* Client into[i] becomes the first len[i] tokens of client seq_ids[i] (NULL: all of them) and loses what it held.  A client may be several
  * times among seq_ids; into is pairwise distinct and shares no client with seq_ids.
  *   fork  shares the blocks: no token is copied until one of the clients writes behind a text that ends inside a block;
- *   copy  takes as many blocks of its own.
+ *   copy  takes as many blocks of its own (with what has been appended so far of a pass that is not over).
  * ESTATE: a length beyond the client's, a stream being recorded; ENOMEM (copy): too few free blocks (what the targets hold alone
  * counts).  If a launch fails (EHIP) the targets are empty. */
 int pipesd_pages_fork(pipesd_pages *pg, int32_t n_seqs, const int32_t *seq_ids, const int32_t *into, const int32_t *len, void *stream);

@@ -50,6 +50,7 @@ struct pipesd_pages {
   std::vector<PagesLaunch> launches, next_launches;
   std::vector<int32_t> had, own, from, to;   // (a call's own)
   bool pass_open = false, attends = false, trees = false;
+  bool rows_shared = false;  // a client outside the pass has become a copy, in the same blocks, of some of the pass's rows
 
   int32_t table_off(int32_t seq) const { return seq * n_blocks; }
   KvView view() const {
@@ -427,6 +428,7 @@ extern "C" int pipesd_pages_extend(pipesd_pages* pg, int32_t n_seqs, const int32
     pg->launches.swap(launches);
     pg->attends = attends;
     pg->trees = trees;
+    pg->rows_shared = false;
     pg->pass_open = true;
     return PIPESD_OK;
   });
@@ -448,7 +450,7 @@ static void pages_add_range(PagesRanges& r, int32_t table_off, int32_t first, in
 extern "C" int pipesd_pages_append(pipesd_pages* pg, int32_t layer, const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* stream) {
   if (!pg || layer < 0 || layer >= pg->cfg.n_layers) return PIPESD_EINVAL;
   if (!pages_rows_ok(pg->cfg, k, k_stride, pg->cfg.n_kv_heads) || !pages_rows_ok(pg->cfg, v, v_stride, pg->cfg.n_kv_heads)) return PIPESD_EINVAL;
-  if (!pg->pool || !pg->pass_open) return PIPESD_ESTATE;
+  if (!pg->pool || !pg->pass_open || pg->rows_shared) return PIPESD_ESTATE;
   PagesRanges r;
   r.n = r.most = 0;
   for (size_t i = 0; i < pg->pass.size(); ++i) {
@@ -575,6 +577,10 @@ extern "C" int pipesd_pages_fork(pipesd_pages* pg, int32_t n_seqs, const int32_t
         if (e != hipSuccess && !rc) rc = hip_fail(e, "forking clients of a paged cache");
         f.n = f.most = 0;
       }
+    }
+    for (int32_t i = 0; !rc && i < n_seqs; ++i) {
+      if (!pg->seqs[seq_ids[i]].in_pass) continue;
+      for (const PagesClient& c : pg->pass) pg->rows_shared = pg->rows_shared || (c.seq == seq_ids[i] && pg->seqs[into[i]].len > c.len - c.n_rows);
     }
     if (rc) {
       pages_clear_targets(pg, n_seqs, into);

@@ -806,7 +806,7 @@ class PageCache:
 
     def fork(self, seqs: Sequence[int], into: Sequence[int], lengths: Optional[Sequence[int]] = None) -> None:
         """Client into[i] becomes the first lengths[i] tokens (None: all) of client seqs[i], in the same blocks; who writes into a shared
-        one gets its own first."""
+        one gets its own first.  Rows of a pass that another client has become a copy of cannot be appended any more."""
         self._become(_lib.pipesd_pages_fork, "pipesd_pages_fork", seqs, into, lengths)
 
     def copy(self, seqs: Sequence[int], into: Sequence[int], lengths: Optional[Sequence[int]] = None) -> None:
