@@ -39,16 +39,17 @@ __device__ __forceinline__ float plain(float x) {  // in an ordinary register
 
 // n / m for 0 <= n < 2^20, 1 <= m, rinv = 1 / m to within an ulp: (n + 0.5) / m is at least 0.5 / m from an integer, more than
 // the roundings' 2^-22 (n + 0.5) / m.  (An integer division is 30 instructions, and code is what a short call waits for.)
-__device__ __forceinline__ int div_by(int n, float rinv) { return (int)(((float)n + 0.5f) * rinv); }
+__host__ __device__ __forceinline__ int div_by(int n, float rinv) { return (int)(((float)n + 0.5f) * rinv); }
 
-// the rows of a tile: lane's column
+// The rows of a tile: lane's column.  Columns behind the last row are that row once more: the workgroup's own, where the last heads of a row may
+// be another's, which may have written its results over the queries.
 struct TileRow {
   int row, head;  // of the pass; of the model
   bool live;
 };
-__device__ __forceinline__ TileRow tile_row(int rr, int group, float group_rinv, int n_rows, int row_off, int kvh) {
-  const int r = div_by(rr, group_rinv);
-  return TileRow{row_off + min(r, n_rows - 1), kvh * group + rr - r * group, r < n_rows};
+__host__ __device__ __forceinline__ TileRow tile_row(int rr, int group, float group_rinv, int n_rows, int row_off, int kvh) {
+  const int last = n_rows * group - 1, at = rr < last ? rr : last, r = div_by(at, group_rinv);
+  return TileRow{row_off + r, kvh * group + at - r * group, rr <= last};
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {  // (through fmaxf the compiler quiets every operand first)
   float d;
