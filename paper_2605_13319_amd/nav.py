@@ -656,9 +656,9 @@ class KV4Cache:
             raise ValueError(f"{n} clients, {nf} and {nc} ends of ranges")
         size = (2, max(n_layers, 0), max(rows, 0), s.n_kv_heads, s.head_dim)
         k, v = torch.empty(size, dtype=self.dtype, device=self.device).unbind(0)
-        # (a tensor of no elements has no address)
-        _check(_lib.pipesd_kv4_read(self.handle, n, ids, f, c, layer0, n_layers, k.data_ptr() or self.pool.data_ptr(),
-                                    v.data_ptr() or self.pool.data_ptr(), self._stream()), "pipesd_kv4_read")
+        spare = 256 if self.pool is None else self.pool.data_ptr()  # (a tensor of no elements has no address)
+        _check(_lib.pipesd_kv4_read(self.handle, n, ids, f, c, layer0, n_layers, k.data_ptr() or spare, v.data_ptr() or spare, self._stream()),
+               "pipesd_kv4_read")
         return k, v
 
     def evict(self, seqs: Sequence[int], into: Sequence[int], keep: int, recent: int, mass, kept=None):
@@ -792,9 +792,8 @@ class PageCache:
             raise ValueError(f"{n} clients, {nf} and {nc} ends of ranges")
         size = (2, max(n_layers, 0), max(rows, 0), s.n_kv_heads, s.head_dim)
         k, v = torch.empty(size, dtype=self.dtype, device=self.device).unbind(0)
-        # (a tensor of no elements has no address)
-        self._call(_lib.pipesd_pages_read, "pipesd_pages_read", n, ids, f, c, layer0, n_layers, k.data_ptr() or self.pool.data_ptr(),
-                                      v.data_ptr() or self.pool.data_ptr())
+        spare = 256 if self.pool is None else self.pool.data_ptr()  # (a tensor of no elements has no address)
+        self._call(_lib.pipesd_pages_read, "pipesd_pages_read", n, ids, f, c, layer0, n_layers, k.data_ptr() or spare, v.data_ptr() or spare)
         return k, v
 
     def _become(self, call, name: str, seqs, into, lengths) -> None:
