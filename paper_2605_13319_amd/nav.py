@@ -847,7 +847,8 @@ class PageCache:
 
 
 def tree_workspace(n_seqs: int, rows: int, device: str = "cuda:0"):
-    """What calls of tree_accept for up to n_seqs clients of up to `rows` rows in all need; one for calls that may overlap each."""
+    """A workspace of tree_accept.  One serves calls of any number of clients and rows (what is said of them here changes nothing), one call at a
+    time; calls that may overlap need one each."""
     return torch.zeros(_lib.pipesd_tree_accept_workspace(), dtype=torch.uint8, device=device)
 
 
