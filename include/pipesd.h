@@ -506,7 +506,7 @@ int pipesd_pages_destroy(pipesd_pages *pg);
  * pipesd_pages_create provided for grow the handle's scratch, which waits for the device; what it was before stays, for calls
  * recorded with it, until pipesd_pages_destroy.
  * ENOMEM: the pool has too few free blocks (one for a last block that other clients hold as well, too), or the scratch cannot grow;
- * ESTATE: see above, of streams being recorded. */
+ * ESTATE: see above, of streams being recorded.  If a launch fails (EHIP) the clients are as they were, and no pass is open. */
 int pipesd_pages_extend(pipesd_pages *pg, int32_t n_seqs, const int32_t *seq_ids, const int32_t *n_new, const int32_t *parents, void *stream);
 
 /* Put the pass's keys and values of one layer into the cache: k, v device [rows][n_kv_heads * head_dim], rows k_stride and v_stride
@@ -542,7 +542,8 @@ int pipesd_pages_copy(pipesd_pages *pg, int32_t n_seqs, const int32_t *seq_ids, 
 /* Of what client seq_ids[i] (pairwise distinct) holds from token first[i] on, n_kept[i] tokens stay, in their order, side by side: those
  * first[i] + kept[j], kept host, rising, one client's after the other's (NULL if there are none).  The others are forgotten, and
  * the blocks behind given back.  In place; a block with other users that would be written is replaced by a free one (ENOMEM if there
- * are too few).  ESTATE: first[i] or a kept token beyond the client's length, see above of streams being recorded. */
+ * are too few).  ESTATE: first[i] or a kept token beyond the client's length, see above of streams being recorded.  If a launch fails
+ * (EHIP) the clients keep their lengths, tokens from first[i] on may have been moved, and no pass is open. */
 int pipesd_pages_compact(pipesd_pages *pg, int32_t n_seqs, const int32_t *seq_ids, const int32_t *first, const int32_t *n_kept, const int32_t *kept,
                          void *stream);
 

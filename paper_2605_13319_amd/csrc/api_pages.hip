@@ -292,6 +292,13 @@ static int pages_send(pipesd_pages* pg, int32_t n, const int32_t* seq_ids, const
   return rc;
 }
 
+// What is left of a call whose launches failed, or were said to have (an error from before is the next launch's): clients whose bookkeeping
+// is as it was get their block tables as they were, and a pass whose trees the device may have lost is over.
+static void pages_take_back(pipesd_pages* pg, int32_t n, const int32_t* seq_ids, hipStream_t st) {
+  pages_close_pass(pg);
+  (void)pages_send(pg, n, seq_ids, nullptr, false, {}, nullptr, st);
+}
+
 // tokens (block * 16 + place) or blocks from pg->from to pg->to, some per launch
 static int pages_moves(pipesd_pages* pg, bool blocks, hipStream_t st) {
   PagesMoves m;
@@ -420,6 +427,7 @@ extern "C" int pipesd_pages_extend(pipesd_pages* pg, int32_t n_seqs, const int32
         }
       }
       undo_own();
+      if (rc == PIPESD_EHIP) pages_take_back(pg, n_seqs, seq_ids, st);
       return rc;
     }
     pages_close_pass(pg);
@@ -727,6 +735,7 @@ extern "C" int pipesd_pages_compact(pipesd_pages* pg, int32_t n_seqs, const int3
           s.blocks[replaced[j].at] = replaced[j].blk;
           ++pg->users[replaced[j].blk];
         }
+        if (rc == PIPESD_EHIP) pages_take_back(pg, n_seqs, seq_ids, st);
         return rc;
       }
     }
