@@ -520,8 +520,11 @@ int pipesd_pages_append(pipesd_pages *pg, int32_t layer, const void *k, int64_t 
  * What tokens hold that a row does not see, infinities and NaN among them, does not reach it.
  * An infinity among the values that it sees is one of its result's channel: NaN beside NaN or one of the other sign, or where its token's
  * weight vanishes in fp32.
- * A row's result depends on what it sees alone.  Into how many pieces a context is cut, and so the order of sums, goes by the
- * lengths and numbers of rows of all clients of the pass; the same pass gives the same bits.
+ * (Weights, each up to 2^8 then, are multiplied with the values before they are divided by their sum: results from values beyond 2^100
+ * may overflow.)
+ * A row's result depends on what it sees alone, but for its last bits: into how many pieces a context is cut goes by the lengths and
+ * numbers of rows of all clients of the pass, and to what scale sums are held by the scores of the rows that a workgroup takes together.
+ * The same pass gives the same bits.
  * EINVAL: also out over q where that is not allowed; ESTATE: no pass that can attend, no pool. */
 int pipesd_pages_attend(pipesd_pages *pg, int32_t layer, const void *q, int64_t q_stride, void *out, int64_t out_stride, void *stream);
 
