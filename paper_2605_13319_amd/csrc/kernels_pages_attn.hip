@@ -187,7 +187,8 @@ __device__ __forceinline__ bool not_finite(T x) {
 // In a step that all rows see, an infinity is multiplied with both pieces of a bf16 model's weights, which is no number where the lower one
 // is zero or of the other sign.  A wave whose sums are none comes by here with its states: such a sum holds a value that is not finite, so
 // it is what all of those give, weighted once more.  (Lane (c, g): row c, channels 16 j + 4 g + ...  What it needs it finds again: registers
-// that the walk kept for it would cost the walk more.)
+// that the walk kept for it would spill in the walk.)  8 heads of 128, 9 rows behind 2048 tokens: 11.3 us, 13.2 with an infinity, 22.5 with
+// one in every 64th token, 106 where all values are NaN.  The test for it costs calls without any 0.1 to 0.3 us.
 template <int HD, int TILES>
 __device__ __forceinline__ void weigh_infinities(const PagesAttend& a, const PagesClients& clients, float* state, int first, int step, int end) {
   constexpr int HT = HD / 16, ROW = HD + kPagesPartPad;
@@ -824,8 +825,10 @@ __global__ __launch_bounds__(kPagesWaves * 64, 2) void pages_attend_wide_kernel(
   };
 
   constexpr int PER = SHARES * COPIES;  // copies of a stage that a wave has on their way
+  // Once, and again where sums are no numbers behind steps that all rows see (see weigh_infinities): then such values are apart in all.  9 rows
+  // behind 131071 tokens 103 us, 159 with an infinity, 322 with one in every 64th token.
 #pragma unroll 1
-  for (;;) {  // once, and again where sums are no numbers behind steps that all rows see (see weigh_infinities): then such values are apart in all
+  for (;;) {
 #pragma unroll
     for (int j = 0; j < HT; ++j)
 #pragma unroll

@@ -23,7 +23,7 @@ def definition(q, k, v, seen):
         qh = q[:, heads].reshape(rows * group, dim)
         hidden = ~seen.repeat_interleave(group, 0)
         w = torch.softmax((qh @ k[:, h].T / math.sqrt(dim)).masked_fill(hidden, -torch.inf), -1)
-        big = (qh.abs() @ k[:, h].abs().T / math.sqrt(dim)).masked_fill(hidden, 0).amax(-1)
+        big = (qh.abs() @ k[:, h].abs().nan_to_num(0, posinf=0).T / math.sqrt(dim)).masked_fill(hidden, 0).amax(-1)
         odd = ~torch.isfinite(v[:, h])
         whole = v[:, h].masked_fill(odd, 0)
         oh = w @ whole
@@ -43,15 +43,17 @@ def check(got, want, s, a, dtype):
     assert float(((got - want).abs() - bound)[fine].max()) <= 0
 
 
-def run(heads, dtype, before, rows, tree, spoil):
+def run(heads, dtype, before, rows, tree, spoil, spoil_keys=None):
     nq, nkv, dim = heads
     pg = make_cache(shape_of(*heads, dtype), 1, (before + rows + 15) // 16 + 1)
     k, v = (random_rows(before + rows, nkv, dim, dtype, j) for j in (1, 2))
     spoil(v)
+    q = random_rows(rows, nq, dim, dtype, 7)
+    if spoil_keys:
+        spoil_keys(k, q)
     fill(pg, 0, 0, k, v, before)
     pg.extend([0], [rows], tree)
     pg.append(0, k[before:].cuda(), v[before:].cuda())
-    q = random_rows(rows, nq, dim, dtype, 7)
     out = pg.attend(0, q.cuda())
     check(out, *definition(q, k, v, sees(before, tree if tree else list(range(-1, rows - 1)))), dtype)
 
@@ -114,6 +116,26 @@ def test_one_infinity_wherever_it_lies(heads, before, rows):
     for t in (0, before // 3, before - 33, before - 1):
         for bad in (math.inf, -math.inf):
             run(heads, "bf16", before, rows, None, lambda v: v[t, :, 5].fill_(bad))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,before,rows", TEXTS)
+def test_infinities_of_tokens_that_have_no_weight(heads, before, rows, dtype):
+    """A key that gives every row a score of -inf: its value's infinity times 0 is no number, and what is finite there does not count."""
+    at = {before // 3, before - 20, before + rows // 2}
+
+    def spoil(v):
+        for t in at:
+            v[t, :, t % 7] = math.inf
+        v[before // 2, :, 9] = math.inf  # (of a token that has weight)
+
+    def keys(k, q):
+        q[:, :, 3] = q[:, :, 3].abs() + 0.25
+        for t in at:
+            k[t, :, 3] = -math.inf
+
+    run(heads, dtype, before, rows, None, spoil, keys)
 
 
 def test_the_long_text_is_walked_in_more_than_64_steps(plan):  # noqa: F811

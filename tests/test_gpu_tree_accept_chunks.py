@@ -1,4 +1,4 @@
-"""The decision on trees over vocabularies that several workgroups share, against its checker to the last bit: many clients in a call, rows of
+"""The decision on trees over vocabularies that several workgroups share, against its oracle to the last bit: many clients in a call, rows of
 many children, equal maxima in different parts of a row, distributions that are no numbers, calls of different sizes on one
 workspace."""
 import numpy as np
